@@ -57,8 +57,10 @@ typedef enum {
                                 scratch (bsr_scratch_size) that has not been lent with bsr_set_scratch */
     BSR_ERR_HIP = 8,         /* a HIP runtime call failed (launch, copy), or bsr_create() found no host memory for its plan */
     BSR_ERR_UNSUPPORTED = 9, /* the requested kernel path cannot handle this block shape */
-    BSR_ERR_SCRATCH_LIMIT = 10 /* bsr_spmm_static(): the product needs more scratch than the library's built-in
+    BSR_ERR_SCRATCH_LIMIT = 10,/* bsr_spmm_static(): the product needs more scratch than the library's built-in
                                   BSR_STATIC_SCRATCH_BYTES */
+    BSR_ERR_OVERLAP = 11,    /* a buffer that is written overlaps another one of the call */
+    BSR_ERR_DEVICE = 12      /* the handle was created on another device than the current one (bsr_spmm_epilogue, bsr_adamw_*) */
 } bsr_status;
 
 /* Which kernel family bsr_spmm_ex() uses. */
@@ -150,6 +152,63 @@ void bsr_destroy(bsr_matrix* W);
  */
 bsr_status bsr_spmm(const bsr_matrix* W, int64_t m, const void* X_dev, void* Y_dev,
                     bsr_dtype y_dtype, void* hip_stream);
+
+/*
+ * The product with what a layer does to it before it is stored (bsr_spmm_epilogue), in the same launches:
+ *     z = (X W^T)[i][j] + bias[j]            Z[i][j] = z                       if z_dev
+ *     y = act(z)                             or z * act'(Z0[i][j])             with through_dev = Z0
+ *     Y[i][j] = y + R[i][j]                                                    if residual_dev = R
+ * In training, Z is what the activation's gradient is taken at (bsr_epilogue_backward); `through` takes a gradient through
+ * the activation in front of the layer whose W^T is multiplied: Y = (G W) * act'(Z0).  All of it is fp32 arithmetic on the
+ * accumulated sum; what is stored is rounded once, to nearest-even, and act(z) sees the z before that rounding.
+ *   act             BSR_ACT_*: none; max(z, 0); z Phi(z), Phi the normal distribution's integral (relative error below
+ *                   1e-6); z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2; z / (1 + exp(-z))
+ *   bias_dev        DEVICE, n elements of bias_dtype (W's dtype or BSR_F32), or NULL
+ *   residual_dev    DEVICE, m rows of n elements of y_dtype, `residual_ld` elements apart (0: n, contiguous), or NULL
+ *   through_dev     DEVICE, Z0, m*n elements of y_dtype, or NULL; not read where act is BSR_ACT_NONE (slope 1)
+ *   z_dev           DEVICE, m*n elements of y_dtype, every one written, or NULL
+ * Fill unused members with zeros.  A NaN stays a NaN; at an infinite z the activations' and slopes' limits are taken.
+ */
+typedef enum { BSR_ACT_NONE = 0, BSR_ACT_RELU = 1, BSR_ACT_GELU = 2, BSR_ACT_GELU_TANH = 3, BSR_ACT_SILU = 4 } bsr_act;
+typedef struct {
+    bsr_act act;
+    bsr_dtype bias_dtype;
+    const void* bias_dev;
+    const void* residual_dev;
+    int64_t residual_ld;
+    const void* through_dev;
+    void* z_dev;
+} bsr_epilogue;
+
+/*
+ * As bsr_spmm() -- the same kernels, choices (bsr_tune() included), streams and captures -- with `epilogue` (HOST, read
+ * during the call).  Y and Z must overlap neither each other nor any input (a residual is not added in place).
+ * Errors: as bsr_spmm(), plus NULL (epilogue), DTYPE (act, bias_dtype), SHAPE (residual_ld below n, or m * residual_ld
+ * >= 2^37), ALIGN (a pointer not 16-byte aligned, or rows of a residual that are neither contiguous nor multiples of
+ * 16 bytes apart), OVERLAP, DEVICE.
+ */
+bsr_status bsr_spmm_epilogue(const bsr_matrix* W, int64_t m, const void* X_dev, void* Y_dev, bsr_dtype y_dtype,
+                             const bsr_epilogue* epilogue, void* hip_stream);
+
+/*
+ * The gradient of that epilogue, from G = dL/dY:
+ *     dZ[i][j] = G[i][j] * act'(Z[i][j])          db[j] = sum over i of dZ[i][j]
+ * dZ is what the layer's own gradients are taken of -- bsr_sddmm(W, dZ, X), bsr_spmm(handle of W^T, dZ) -- and db is the
+ * bias's.  (The residual's gradient is G itself.)  One pass over G and Z; the sums are fp32, of dZ before its rounding, and
+ * added in a fixed order (no atomics).
+ *   G_dev, Z_dev   DEVICE, m*n elements of g_dtype, row-major; Z_dev is not read where act is BSR_ACT_NONE (may be NULL)
+ *   DZ_dev         DEVICE, m*n elements of dz_dtype (g_dtype, or any type where g_dtype is BSR_F32), or NULL; it may be
+ *                  G_dev or Z_dev itself where the types are the same
+ *   DB_dev         DEVICE, n floats, or NULL (not both NULL); m == 0: zeros
+ *   workspace_dev  DEVICE, bsr_epilogue_backward_workspace_size() bytes (0: none, it may be NULL), overwritten; read only
+ *                  where DB_dev is given.  Calls that may run at the same time, replayed graphs among them, need one each.
+ * Asynchronous on hip_stream.  Errors: NULL, SHAPE (m or n negative, m >= 2^30, n >= 2^31 - 512, or m*n >= 2^40), DTYPE,
+ * ALIGN (a pointer not 16-byte aligned), WORKSPACE, OVERLAP, HIP.
+ */
+bsr_status bsr_epilogue_backward_workspace_size(int64_t m, int64_t n, size_t* bytes);
+bsr_status bsr_epilogue_backward(int64_t m, int64_t n, bsr_act act, bsr_dtype g_dtype, const void* G_dev, const void* Z_dev,
+                                 bsr_dtype dz_dtype, void* DZ_dev, float* DB_dev, void* workspace_dev, size_t workspace_bytes,
+                                 void* hip_stream);
 
 /*
  * Scratch.  Some kernels need device memory beyond X, W and Y for the duration of one product:
@@ -294,6 +353,85 @@ bsr_status bsr_sddmm_ws(const bsr_matrix* W, int64_t m, const void* G_dev, const
 #define BSR_STATIC_SCRATCH_BYTES (8u << 20)
 bsr_status bsr_spmm_static(const bsr_matrix* W, int64_t m, const void* X_dev, void* Y_dev,
                            bsr_dtype y_dtype, void* hip_stream);
+
+/*
+ * One AdamW step over many tensors in as few launches as they have kinds (type, gradient's type, master copy or not): the
+ * step from the gradients that bsr_sddmm() and bsr_epilogue_backward() make to the block values that bsr_spmm() reads, those
+ * of W^T with them.  With g the gradient times grad_scale, t the step's number (from 1):
+ *     m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
+ *     p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32 whatever the types.
+ *   param_dev      DEVICE, count elements of dtype (block_data of a W, a bias, ...), updated
+ *   master_dev     DEVICE, count floats, or NULL: the parameter in fp32 (16-bit types only); it is updated and param_dev is
+ *                  its nearest-even rounding.  Without one a 16-bit parameter is rounded up or down at random so that its mean
+ *                  is kept: most updates are below half its last place
+ *   grad_dev       DEVICE, count elements of grad_dtype (dtype or BSR_F32), read
+ *   exp_avg_dev, exp_avg_sq_dev
+ *                  DEVICE, m and v, updated: count floats each or, with 8-bit states, count bytes each.  Zeros to begin with
+ *   scales_dev     8-bit states: DEVICE, three floats for each 256 elements begun, updated; zeros to begin with
+ *   bs_r, bs_c, t_param_dev, t_perm_host
+ *                  with t_param_dev (else all 0): the tensor is a W's blocks [stored blocks][bs_r][bs_c], t_param_dev
+ *                  (DEVICE) the blocks of its transpose as bsr_transpose_values() orders them, written anew by every step;
+ *                  t_perm_host (HOST, read during bsr_adamw_create only) is bsr_transpose_pattern()'s perm
+ * 8-bit states, in groups of 256 elements from a tensor's start.  m: an e4m3 number times a scale, rounded to nearest-even.
+ * v: 0, or 2^(start + (code - 1) spacing), code 1 .. 255, from the group's smallest positive v (at least 2^-40 of the largest)
+ * to its largest, rounded up or down at random so that its mean is kept (a step changes v by less than half the spacing:
+ * rounded to nearest it would stop).  The random numbers are a hash of seed, step, the tensor's place in the list and the
+ * element's in the tensor: the same call on the same values gives the same bits.  The update itself sees m and v before
+ * their rounding.
+ * Not finite gradients: they reach p, and with 8-bit states the moments of their whole group; a loop that scales its loss
+ * looks for them and sets grad_scale_dev to 0, for which nothing is written.
+ */
+typedef struct bsr_adamw bsr_adamw;     /* opaque handle: the list of tensors (device pointers not owned) */
+typedef struct {
+    int64_t count;
+    bsr_dtype dtype, grad_dtype;
+    void* param_dev;
+    float* master_dev;
+    const void* grad_dev;
+    void* exp_avg_dev;
+    void* exp_avg_sq_dev;
+    float* scales_dev;
+    float weight_decay;
+    int32_t bs_r, bs_c;
+    void* t_param_dev;
+    const int32_t* t_perm_host;
+} bsr_adamw_tensor;
+
+/* A step's settings.  The *_dev members (DEVICE scalars, or NULL) take the place of the values beside them when the step runs:
+ * a step captured into a graph reads its number, rate and scale at every replay. */
+typedef struct {
+    double lr, beta1, beta2, eps;       /* 0 <= beta < 1, lr and eps >= 0 */
+    int64_t step;                       /* t >= 1 */
+    float grad_scale;                   /* 1: gradients as they are; 0: the step is skipped */
+    uint32_t seed;
+    const float* lr_dev;
+    const int64_t* step_dev;
+    const float* grad_scale_dev;
+} bsr_adamw_hyper;
+
+/*
+ * bsr_adamw_workspace_size  bytes of DEVICE workspace for the tables of a list (> 0, a multiple of 256)
+ * bsr_adamw_create          checks the list (`tensors`, HOST) and uploads its tables to workspace_dev on hip_stream; the
+ *                           device buffers and the workspace stay the caller's, must outlive the handle and keep their
+ *                           places; everything a step writes must be apart from every other buffer of the list.  Not for a
+ *                           stream that is being captured.  state_bits: 32 or 8, of all its tensors.  *out is NULL on error
+ * bsr_adamw_step            one step, asynchronous on hip_stream (steps on other streams wait for the upload on the device);
+ *                           steps of one handle must not overlap in time.  A captured step may be replayed
+ * bsr_adamw_moments         m and v as values of `dtype`: exp_avg_out[i], exp_avg_sq_out[i] (HOST arrays of DEVICE pointers,
+ *                           count elements each, or NULL: not wanted) for tensor i of the list
+ * bsr_adamw_destroy         frees the handle's host memory (after waiting for the upload); NULL is accepted
+ * Errors: NULL; SHAPE (sizes, blocks that do not make up a tensor, settings out of range, 2^36 elements in all); DTYPE
+ * (state_bits too); ALIGN (16 bytes, scales and scalars their own size); INDEX (t_perm_host is no permutation);
+ * WORKSPACE; OVERLAP; UNSUPPORTED (a block that bsr_transpose_values refuses); DEVICE; HIP.
+ */
+bsr_status bsr_adamw_workspace_size(int64_t n_tensors, const bsr_adamw_tensor* tensors, int32_t state_bits, size_t* bytes);
+bsr_status bsr_adamw_create(bsr_adamw** out, int64_t n_tensors, const bsr_adamw_tensor* tensors, int32_t state_bits,
+                            void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+bsr_status bsr_adamw_step(const bsr_adamw* opt, const bsr_adamw_hyper* hyper, void* hip_stream);
+bsr_status bsr_adamw_moments(const bsr_adamw* opt, bsr_dtype dtype, void* const* exp_avg_out, void* const* exp_avg_sq_out,
+                             void* hip_stream);
+void bsr_adamw_destroy(bsr_adamw* opt);
 
 /*
  * Measurement helper for the benchmark, not part of the product (no passage of the paper defines it): one

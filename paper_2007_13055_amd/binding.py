@@ -1,6 +1,6 @@
 """Binding for libbsr_spmm.so: same names as the C entry points, marshalling only.
 
-The products (bsr_spmm, bsr_spmm_ex, bsr_spmm_static, bsr_sddmm) go through the native module _binding, whose calls cost
+The products (bsr_spmm, bsr_spmm_ex, bsr_spmm_static, bsr_spmm_epilogue, bsr_epilogue_backward, bsr_sddmm) go through the native module _binding, whose calls cost
 about what the launch itself does; everything called once per matrix goes through ctypes."""
 from __future__ import annotations
 
@@ -15,6 +15,31 @@ _LIB_PATH = os.path.join(_HERE, "libbsr_spmm.so")
 BSR_F32, BSR_F16, BSR_BF16 = 0, 1, 2
 PATH_AUTO, PATH_WAVE, PATH_MFMA = 0, 1, 2
 _DTYPE_CODE = {"f32": BSR_F32, "f16": BSR_F16, "bf16": BSR_BF16}
+
+
+
+class Epilogue(ctypes.Structure):
+    """bsr_epilogue of the C header."""
+    _fields_ = [("act", ctypes.c_int), ("bias_dtype", ctypes.c_int), ("bias_dev", ctypes.c_void_p),
+                ("residual_dev", ctypes.c_void_p), ("residual_ld", ctypes.c_int64), ("through_dev", ctypes.c_void_p),
+                ("z_dev", ctypes.c_void_p)]
+
+
+class AdamWTensor(ctypes.Structure):
+    """bsr_adamw_tensor of the C header."""
+    _fields_ = [("count", ctypes.c_int64), ("dtype", ctypes.c_int), ("grad_dtype", ctypes.c_int),
+                ("param_dev", ctypes.c_void_p), ("master_dev", ctypes.c_void_p), ("grad_dev", ctypes.c_void_p),
+                ("exp_avg_dev", ctypes.c_void_p), ("exp_avg_sq_dev", ctypes.c_void_p), ("scales_dev", ctypes.c_void_p),
+                ("weight_decay", ctypes.c_float), ("bs_r", ctypes.c_int32), ("bs_c", ctypes.c_int32),
+                ("t_param_dev", ctypes.c_void_p), ("t_perm_host", ctypes.c_void_p)]
+
+
+class AdamWHyper(ctypes.Structure):
+    """bsr_adamw_hyper of the C header."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("step", ctypes.c_int64), ("grad_scale", ctypes.c_float), ("seed", ctypes.c_uint32),
+                ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p), ("grad_scale_dev", ctypes.c_void_p)]
+
 
 _lib = None
 _native = None                             # the module _binding, bound to _lib
@@ -60,13 +85,24 @@ def load_library():
     lib.bsr_transpose_pattern.argtypes = [i64, i64, i32, i32, i64, vp, vp, vp, vp, vp]
     lib.bsr_transpose_values.argtypes = [ctypes.c_int, i32, i32, i64, vp, vp, vp, vp]
     lib.bsr_sddmm.argtypes = [vp, i64, vp, vp, vp, ctypes.c_int, vp]
+    lib.bsr_spmm_epilogue.argtypes = [vp, i64, vp, vp, ctypes.c_int, ctypes.POINTER(Epilogue), vp]
+    lib.bsr_epilogue_backward_workspace_size.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    lib.bsr_epilogue_backward.argtypes = [i64, i64, ctypes.c_int, ctypes.c_int, vp, vp, ctypes.c_int, vp, vp, vp, sz, vp]
+    lib.bsr_adamw_workspace_size.argtypes = [i64, ctypes.POINTER(AdamWTensor), i32, ctypes.POINTER(sz)]
+    lib.bsr_adamw_create.argtypes = [ctypes.POINTER(vp), i64, ctypes.POINTER(AdamWTensor), i32, vp, sz, vp]
+    lib.bsr_adamw_step.argtypes = [vp, ctypes.POINTER(AdamWHyper), vp]
+    lib.bsr_adamw_moments.argtypes = [vp, ctypes.c_int, ctypes.POINTER(vp), ctypes.POINTER(vp), vp]
+    lib.bsr_adamw_destroy.argtypes = [vp]
+    lib.bsr_adamw_destroy.restype = None
     lib.bsr_probe_mfma.argtypes = [ctypes.c_int, i32, vp, vp, ctypes.POINTER(ctypes.c_double)]
     lib.bsr_probe_mfma.restype = ctypes.c_int
     lib.bsr_status_string.argtypes = [ctypes.c_int]
     lib.bsr_status_string.restype = ctypes.c_char_p
     for f in ("bsr_validate", "bsr_workspace_size", "bsr_create", "bsr_spmm", "bsr_spmm_ex", "bsr_spmm_static",
               "bsr_query_path", "bsr_scratch_size", "bsr_set_scratch", "bsr_tune", "bsr_tune_result",
-              "bsr_transpose_pattern", "bsr_transpose_values", "bsr_sddmm"):
+              "bsr_transpose_pattern", "bsr_transpose_values", "bsr_sddmm", "bsr_spmm_epilogue",
+              "bsr_epilogue_backward_workspace_size", "bsr_epilogue_backward", "bsr_adamw_workspace_size", "bsr_adamw_create",
+              "bsr_adamw_step", "bsr_adamw_moments"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -87,7 +123,8 @@ def _native_module():
                            "`python -m paper_2007_13055_amd.build`") from e
     _binding.bind(*(ctypes.cast(f, ctypes.c_void_p).value
                     for f in (lib.bsr_spmm_ex, lib.bsr_spmm_static, lib.bsr_sddmm_ws, lib.bsr_scratch_size,
-                              lib.bsr_sddmm_workspace_size)), BsrError)
+                              lib.bsr_sddmm_workspace_size, lib.bsr_spmm_epilogue, lib.bsr_epilogue_backward,
+                              lib.bsr_epilogue_backward_workspace_size)), BsrError)
     _native = _binding
     return _native
 
@@ -255,6 +292,25 @@ def bsr_spmm(W: BsrMatrix, X, Y=None, y_dtype=None):
     return _native.spmm(W, W._core, X, Y, y_dtype, PATH_AUTO)
 
 
+def bsr_spmm_epilogue(W: BsrMatrix, X, Y=None, y_dtype=None, *, bias=None, act="none", residual=None, through=None, Z=None,
+                      keep_z=False):
+    """Y = act(X W^T + bias) + residual, or (X W^T + bias) * act'(through) + residual, in the product's own launches.
+
+    act "none" | "relu" | "gelu" | "gelu_tanh" | "silu"; bias (n,) of W's dtype or fp32; residual (m, n) of the result's
+    type, its rows contiguous; through (m, n): the sums that the activation in front of the layer was given, whose slope the
+    result is multiplied by.  Z: a buffer for the sums (bias added) before the activation; keep_z: a new one.  Returns Y, or
+    (Y, Z) where Z or keep_z is given.  Y and Z must not overlap each other or an input."""
+    return _native.spmm_epilogue(W, W._core, X, Y, y_dtype, bias, act, residual, through, Z, keep_z)
+
+
+def bsr_epilogue_backward(G, Z=None, act="none", DZ=None, dz_dtype=None, DB=None, *, need_dz=True, need_db=True):
+    """(DZ, DB) = (G * act'(Z), the sums of its columns in fp32): what bsr_spmm_epilogue's activation and bias have as
+    gradients, from G = dL/dY and the Z that it kept.  dz_dtype: G's type, or any where G is fp32.  DZ may be G or Z itself.
+    Without an activation dZ is G: G is returned unless its type changes or a DZ is given.  need_dz, need_db: leave out the
+    one or the other (None in its place)."""
+    return _native_module().epilogue_backward(G, Z, act, DZ, dz_dtype, DB, need_dz, need_db)
+
+
 STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -320,3 +376,166 @@ def bsr_query_path(W: BsrMatrix, m: int) -> int:
     if st != 0:
         raise BsrError(st, "bsr_query_path")
     return int(out.value)
+
+
+class BsrAdamW:
+    """Owns the tensors of one list (parameters, gradients, moments, ...; they must outlive the C handle) and the handle.
+
+    params, grads, master, exp_avg, exp_avg_sq, scales: lists in the order given to bsr_adamw_create (None where a tensor has
+    none)."""
+
+    def __init__(self, state_bits, params, grads, master, exp_avg, exp_avg_sq, scales):
+        self.state_bits, self.params, self.grads, self.master = state_bits, params, grads, master
+        self.exp_avg, self.exp_avg_sq, self.scales = exp_avg, exp_avg_sq, scales
+        self.handle, self.device, self._keep = None, None, []
+
+    def close(self):
+        if self.handle:
+            load_library().bsr_adamw_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _adamw_buffer(t, what, dtypes, count, device):
+    """t, checked: a contiguous tensor of `count` elements of one of the types on `device`."""
+    if t.dtype not in dtypes or t.numel() != count or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what} must be contiguous, of {count} elements of {' or '.join(map(str, dtypes))}, on {device}")
+    return t
+
+
+def bsr_adamw_create(params, grads, *, weight_decay=0.0, state_bits=32, moments=None, master=None, transposed=None) -> BsrAdamW:
+    """The handle of AdamW steps over a list of tensors on the current GPU.
+
+    params, grads: contiguous tensors of any shapes, f32, f16 or bf16; a gradient has its parameter's type or fp32 and is read
+    by every step from where it is (let bsr_sddmm and bsr_epilogue_backward write there).  weight_decay: one number or one a
+    tensor.  state_bits: 32 or 8 (e4m3 and logarithmic codes with scales for each 256 elements).  master: True (fp32 copies
+    of the 16-bit parameters, made here) or a list of fp32 tensors and None; without one a 16-bit parameter is rounded at
+    random so that its mean is kept.  moments: None (zeros), or per tensor (m, v) or, for 8 bits, (m codes, v codes, scales):
+    fp32, or uint8 and (groups of 256, 3) fp32.  transposed: None, or per tensor None or (t, perm): the tensor is a W's
+    block_data (stored blocks, bs_r, bs_c), t the handle or the block_data of its transpose, which every step brings up to
+    date, perm from bsr_transpose_pattern."""
+    import torch
+    lib = load_library()
+    params, grads = list(params), list(grads)
+    n = len(params)
+    if len(grads) != n or (moments is not None and len(moments) != n) or (transposed is not None and len(transposed) != n) or \
+            (isinstance(master, (list, tuple)) and len(master) != n):
+        raise ValueError("one gradient (pair of moments, master copy, transpose) a parameter is wanted")
+    if state_bits not in (32, 8):
+        raise ValueError("state_bits must be 32 or 8")
+    decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(v) for v in weight_decay]
+    if len(decay) != n:
+        raise ValueError("one weight_decay, or one a parameter, is wanted")
+    device = torch.device("cuda", torch.cuda.current_device())
+    f32 = torch.float32
+    code, zeros = (torch.uint8, f32)[state_bits == 32], lambda count, dtype: torch.zeros(count, dtype=dtype, device=device)
+    opt = BsrAdamW(state_bits, params, grads, [None] * n, [None] * n, [None] * n, [None] * n)
+    opt.device = device
+    table = (AdamWTensor * max(n, 1))()
+    for i, (p, g) in enumerate(zip(params, grads)):
+        count = p.numel()
+        _adamw_buffer(p, f"params[{i}]", (f32, torch.float16, torch.bfloat16), count, device)
+        _adamw_buffer(g, f"grads[{i}]", (p.dtype, f32), count, device)
+        own = master[i] if isinstance(master, (list, tuple)) else (p.detach().to(f32, copy=True) if master and p.dtype != f32 else None)
+        opt.master[i] = None if own is None else _adamw_buffer(own, f"master[{i}]", (f32,), count, device)
+        groups = -(-count // 256)
+        given = moments[i] if moments is not None else None
+        if given is None:
+            given = (zeros(count, code), zeros(count, code)) + ((zeros((groups, 3), f32),) if state_bits == 8 else ())
+        if len(given) != (2 if state_bits == 32 else 3):
+            raise ValueError(f"moments[{i}]: (m, v), for 8 bits (m, v, scales)")
+        opt.exp_avg[i] = _adamw_buffer(given[0], f"moments[{i}][0]", (code,), count, device)
+        opt.exp_avg_sq[i] = _adamw_buffer(given[1], f"moments[{i}][1]", (code,), count, device)
+        if state_bits == 8:
+            opt.scales[i] = _adamw_buffer(given[2], f"moments[{i}][2]", (f32,), 3 * groups, device)
+        t = table[i]
+        t.count, t.dtype, t.grad_dtype, t.weight_decay = count, _DTYPE_CODE[_dtype_name(p)], _DTYPE_CODE[_dtype_name(g)], decay[i]
+        t.param_dev, t.grad_dev = p.data_ptr(), g.data_ptr()
+        t.master_dev = None if own is None else own.data_ptr()
+        t.exp_avg_dev, t.exp_avg_sq_dev = opt.exp_avg[i].data_ptr(), opt.exp_avg_sq[i].data_ptr()
+        t.scales_dev = opt.scales[i].data_ptr() if state_bits == 8 else None
+        turned = transposed[i] if transposed is not None else None
+        if turned is not None:
+            copy, perm = turned
+            copy = copy.block_data if isinstance(copy, BsrMatrix) else copy
+            if p.dim() != 3 or tuple(copy.shape) != (p.shape[0], p.shape[2], p.shape[1]):
+                raise ValueError(f"transposed[{i}]: (stored blocks, bs_c, bs_r) for a parameter (stored blocks, bs_r, bs_c)")
+            _adamw_buffer(copy, f"transposed[{i}]", (p.dtype,), count, device)
+            perm = _i32(perm.cpu().numpy() if isinstance(perm, torch.Tensor) else perm)
+            if perm.shape[0] != p.shape[0]:
+                raise ValueError(f"transposed[{i}]: one entry of perm a stored block")
+            if count:
+                t.bs_r, t.bs_c, t.t_param_dev, t.t_perm_host = int(p.shape[1]), int(p.shape[2]), copy.data_ptr(), perm.ctypes.data
+            opt._keep += [copy, perm]
+    size = ctypes.c_size_t(0)
+    st = lib.bsr_adamw_workspace_size(n, table, state_bits, ctypes.byref(size))
+    if st != 0:
+        raise BsrError(st, "bsr_adamw_workspace_size")
+    workspace = torch.empty(size.value, dtype=torch.uint8, device=device)
+    opt._keep.append(workspace)
+    handle = ctypes.c_void_p()
+    st = lib.bsr_adamw_create(ctypes.byref(handle), n, table, state_bits, workspace.data_ptr(), workspace.numel(),
+                              torch.cuda.current_stream().cuda_stream)
+    if st != 0:
+        raise BsrError(st, "bsr_adamw_create")
+    opt.handle = handle
+    return opt
+
+
+def _device_scalar(t, what, dtype, device):
+    if t.dtype != dtype or t.numel() != 1 or t.device != device:
+        raise ValueError(f"{what} on the GPU must be one {dtype} on {device}")
+    return t.data_ptr()
+
+
+def bsr_adamw_step(opt: BsrAdamW, step, *, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, grad_scale=1.0, seed=0):
+    """One step on torch's current stream, updating opt's parameters, master copies, moments and transposes in place.
+
+    step counts from 1.  step, lr and grad_scale may be GPU tensors of one int64, fp32 and fp32, which a step captured into a
+    graph reads at every replay; a grad_scale of 0 skips the step.  seed: of the random roundings."""
+    import torch
+    h = AdamWHyper(beta1=betas[0], beta2=betas[1], eps=eps, seed=int(seed) & 0xFFFFFFFF)
+    if isinstance(step, torch.Tensor):
+        h.step_dev = _device_scalar(step, "step", torch.int64, opt.device)
+    else:
+        h.step = int(step)
+    if isinstance(lr, torch.Tensor):
+        h.lr_dev = _device_scalar(lr, "lr", torch.float32, opt.device)
+    else:
+        h.lr = lr
+    if isinstance(grad_scale, torch.Tensor):
+        h.grad_scale_dev = _device_scalar(grad_scale, "grad_scale", torch.float32, opt.device)
+    else:
+        h.grad_scale = grad_scale
+    st = load_library().bsr_adamw_step(opt.handle, ctypes.byref(h), torch.cuda.current_stream().cuda_stream)
+    if st != 0:
+        raise BsrError(st, "bsr_adamw_step")
+
+
+def bsr_adamw_moments(opt: BsrAdamW, dtype="f32", out=None):
+    """[(m, v), ...]: the moments as values of `dtype` ("f32" | "f16" | "bf16"), whatever they are held in; out: such a list to
+    fill (of one type, each entry of it a tensor, a pair's tensors of a parameter's number of elements)."""
+    import torch
+    if out is None:
+        new = lambda p: torch.empty(p.numel(), dtype=_torch_dtype(dtype), device=opt.device)  # noqa: E731
+        out = [(new(p), new(p)) for p in opt.params]
+    else:
+        out = [tuple(pair) for pair in out]
+        if len(out) != len(opt.params) or any(len(pair) != 2 for pair in out):
+            raise ValueError("out: a pair of tensors a parameter")
+        if out:
+            dtype = _dtype_name(out[0][0])
+        for i, (pair, p) in enumerate(zip(out, opt.params)):
+            for t in pair:
+                _adamw_buffer(t, f"out[{i}]", (_torch_dtype(dtype),), p.numel(), opt.device)
+    n = len(out)
+    ms, vs = ((ctypes.c_void_p * max(n, 1))(*(pair[k].data_ptr() for pair in out)) for k in (0, 1))
+    st = load_library().bsr_adamw_moments(opt.handle, _DTYPE_CODE[dtype], ms, vs, torch.cuda.current_stream().cuda_stream)
+    if st != 0:
+        raise BsrError(st, "bsr_adamw_moments")
+    return out

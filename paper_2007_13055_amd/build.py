@@ -105,7 +105,7 @@ def build_binding(force: bool = True) -> str:
     return BINDING
 
 
-def build(force: bool = True, jobs: int = 4, plain: bool = False) -> str:
+def build(force: bool = True, jobs: int = 8, plain: bool = False) -> str:
     """Compile every .hip file and link the shared library (plain: the checking build); returns its path."""
     os.makedirs(OBJDIR_PLAIN if plain else OBJDIR, exist_ok=True)
     with ThreadPoolExecutor(max_workers=jobs) as ex:

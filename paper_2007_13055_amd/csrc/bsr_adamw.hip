@@ -1,0 +1,688 @@
+// One AdamW step over many tensors at once: the step that turns the gradients of the stored blocks (bsr_sddmm) into the
+// blocks that the next product reads (bsr_spmm), and the stored values of W^T with them (bsr_transpose_values).
+//
+//     m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
+//     p = p (1 - lr decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+//
+// Work split: the tensors are cut into chunks of 4096 elements, a workgroup each, listed in a table that bsr_adamw_create()
+// uploads once; a launch takes all the chunks of one kind (type, gradient's type, master copy or not), so a model of one kind
+// is one launch however many tensors it has.  A wavefront takes 256 elements at a time, four neighbouring ones a lane.
+//
+// 8-bit moments.  The 256 elements of a wavefront share three fp32 scales:
+//   m   e4m3 code times scale, scale = (largest |m|) / 448, rounded to nearest-even (a step changes m by a tenth of g - m,
+//       above half a step of the code).
+//   v   code c: 0 is zero, 1 .. 255 are low * 2^((c - 1) spacing): evenly spaced in log2 v from the smallest positive v of the
+//       256 (at least 2^-40 of the largest) to the largest, so no positive v becomes 0, which would blow its update up.  A step
+//       changes v by 0.1 % of g^2 - v (beta2 = 0.999), while codes are some 1 to 10 % apart: rounded to nearest, v would stop
+//       after its first few dozen steps.  Between two codes the upper one is taken with the probability that keeps the mean.
+// A 16-bit parameter without a master copy is rounded the same way: an update is mostly below half its last place.  The random
+// bits are a hash of the seed, the step, the tensor's number and the element's, so a step can be repeated bit for bit.
+//
+// The stored values of W^T: the chunk's new values pass through LDS and leave in the order of W^T's blocks, 16 bytes a
+// thread, where a block's size divides the chunk; for other blocks bsr_transpose_values() is launched behind.
+//
+// What bounds it: memory, 28 bytes an element with a master copy and fp32 moments of bf16 parameters.
+#include <algorithm>
+#include <cmath>
+#include <limits>
+#include <memory>
+#include <new>
+#include <stdexcept>
+
+#include "bsr_mfma_common.h"
+
+using namespace bsr_dev;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChunk = 4096;                          // elements of a workgroup
+constexpr int kShared = 256;                          // elements that share scales: one pass of a wavefront
+constexpr int kPasses = kChunk / (4 * kThreads);
+constexpr float kTop8 = 448.f;                        // largest e4m3 number
+
+// A tensor as the kernels see it.
+struct tensor_desc {
+    void* param;
+    float* master;
+    const void* grad;
+    void* m;
+    void* v;
+    float* scales;
+    void* transposed;                                 // null: none, or not written here
+    const int32_t* place;                             // [stored blocks]: where each block's transpose goes
+    int64_t count;
+    float decay;
+    uint32_t number;                                  // in the caller's list
+    int32_t r_log, c_log;                             // log2 of the block's sides
+    int64_t pad;
+};
+static_assert(sizeof(tensor_desc) == 96, "uploaded as words");
+
+struct step_args {
+    float lr, beta1, beta2, one1, one2, eps;          // one1 = 1 - beta1
+    float rate, root;                                 // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t); where step_dev is null
+    float log1, log2;                                 // natural logarithms of the betas
+    float grad_scale;
+    uint32_t key;                                     // of the seed and the step
+    uint32_t seed;
+    const float* lr_dev;
+    const int64_t* step_dev;
+    const float* grad_scale_dev;
+};
+
+// Two rounds of xor-shift and multiply.
+__host__ __device__ __forceinline__ uint32_t mix(uint32_t x)
+{
+    x ^= x >> 16;
+    x *= 0xBB67AE85u;
+    x ^= x >> 15;
+    x *= 0x6A09E667u;
+    return x ^ (x >> 16);
+}
+__host__ __device__ __forceinline__ uint32_t step_key(uint32_t seed, uint64_t step) { return mix(seed + 0x9E3779B1u * (uint32_t)step); }
+
+template <int CTRL> __device__ __forceinline__ float dpp(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+}
+// Largest v of the wavefront, in every lane (the steps of a sum over 64 lanes).
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = fmaxf(v, dpp<0xB1>(v));
+    v = fmaxf(v, dpp<0x4E>(v));
+    v = fmaxf(v, dpp<0x141>(v));
+    v = fmaxf(v, dpp<0x140>(v));
+    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401F)));
+    const float lo = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 0));
+    const float hi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 32));
+    return fmaxf(lo, hi);
+}
+
+// Four elements at p, `n` of them there (at least one).
+template <typename T> __device__ __forceinline__ void load4(float (&v)[4], const T* __restrict__ p, int n)
+{
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    if (n >= 4) {
+        const t4 t = *reinterpret_cast<const t4*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)t[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = e < n ? (float)p[e] : 0.f;
+    }
+}
+template <typename T> __device__ __forceinline__ void put4(T* __restrict__ p, const T (&v)[4], int n)
+{
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    if (n >= 4) {
+        *reinterpret_cast<t4*>(p) = t4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) p[e] = v[e];
+    }
+}
+// Four codes, packed
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* __restrict__ p, int n)
+{
+    if (n >= 4) return *reinterpret_cast<const uint32_t*>(p);
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < n) w |= (uint32_t)p[e] << (8 * e);
+    return w;
+}
+__device__ __forceinline__ void put_codes(uint8_t* __restrict__ p, uint32_t w, int n)
+{
+    if (n >= 4) { *reinterpret_cast<uint32_t*>(p) = w; return; }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < n) p[e] = (uint8_t)(w >> (8 * e));
+}
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ void decode_first(float (&m)[4], uint32_t codes, float scale)
+{
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    m[0] = a.x * scale; m[1] = a.y * scale; m[2] = b.x * scale; m[3] = b.y * scale;
+}
+__device__ __forceinline__ void decode_second(float (&v)[4], uint32_t codes, float start, float spacing)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t c = (codes >> (8 * e)) & 255u;
+        v[e] = c ? __builtin_amdgcn_exp2f(fmaf((float)c - 1.f, spacing, start)) : 0.f;
+    }
+}
+
+// fp32 to 16 bits, away from zero with the probability that keeps the mean; `random`: 16 random bits.
+__device__ __forceinline__ bf16_t round_at_random(bf16_t, float x, uint32_t random)
+{
+    uint32_t u = __builtin_bit_cast(uint32_t, x);
+    if ((u & 0x7F800000u) != 0x7F800000u) u += random & 0xFFFFu;      // infinities and NaN as they are
+    else if (u & 0x007FFFFFu) u |= 0x00400000u;
+    return __builtin_bit_cast(bf16_t, (uint16_t)(u >> 16));
+}
+__device__ __forceinline__ f16_t round_at_random(f16_t, float x, uint32_t random)
+{
+    // steps of fp16 at x: 2^(exponent - 10), 2^-24 among its subnormal numbers; x in such steps keeps 13 bits behind the point
+    const int exponent = max((int)((__builtin_bit_cast(uint32_t, x) >> 23) & 255u) - 127, -14);
+    if (exponent > 15) return (f16_t)x;
+    const float steps = ldexpf(fabsf(x), 10 - exponent);
+    const float whole = floorf(steps + (float)(random & 0x1FFFu) * (1.f / 8192.f));
+    return (f16_t)copysignf(ldexpf(whole, exponent - 10), x);
+}
+
+// T: the parameter's type, GT: the gradient's, BITS: of the moments.
+template <typename T, typename GT, int BITS, bool MASTER>
+__global__ __launch_bounds__(kThreads) void bsr_adamw_chunks(const tensor_desc* __restrict__ tensors, const int2* __restrict__ chunks, step_args h)
+{
+    __shared__ __attribute__((aligned(16))) T turned[kChunk];
+    const int2 where = chunks[blockIdx.x];            // {tensor, chunk of it}
+    const tensor_desc& d = tensors[where.x];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t first = (int64_t)where.y * kChunk;
+    const int there = (int)min(d.count - first, (int64_t)kChunk);   // elements of this chunk
+
+    float grad_scale = h.grad_scale, lr = h.lr, rate = h.rate, root = h.root;
+    uint32_t key = h.key;
+    if (h.grad_scale_dev) {
+        grad_scale = *h.grad_scale_dev;
+        if (grad_scale == 0.f) return;                // the step is skipped: whole grid
+    }
+    if (h.lr_dev) lr = *h.lr_dev;
+    if (h.step_dev) {
+        const int64_t t = *h.step_dev;
+        root = __builtin_amdgcn_rsqf(-expm1f((float)t * h.log2));
+        rate = -1.f / expm1f((float)t * h.log1);
+        key = step_key(h.seed, (uint64_t)t);
+    }
+    rate *= lr;
+    const float keep = 1.f - lr * d.decay;
+    const uint32_t base = mix(d.number + key) + (uint32_t)first;
+
+    T* const param = static_cast<T*>(d.param) + first;
+    float* const master = MASTER ? d.master + first : nullptr;
+    const GT* const grad = static_cast<const GT*>(d.grad) + first;
+
+#pragma unroll
+    for (int q = 0; q < kPasses; ++q) {
+        const int at = (q * 4 + wave) * kShared + lane * 4, n = there - at;   // n <= 0: nothing for this lane
+        if ((q * 4 + wave) * kShared >= there) break; // uniform
+        float p[4], g[4], m[4], v[4], scale[3] = {0.f, 0.f, 0.f};
+        const int64_t block = (first + (q * 4 + wave) * kShared) / kShared;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = g[e] = m[e] = v[e] = 0.f;
+        if (n > 0) {
+            load4(g, grad + at, n);
+            if constexpr (MASTER) load4(p, master + at, n);
+            else load4(p, param + at, n);
+            if constexpr (BITS == 32) {
+                load4(m, static_cast<const float*>(d.m) + first + at, n);
+                load4(v, static_cast<const float*>(d.v) + first + at, n);
+            }
+        }
+        if constexpr (BITS == 8) {
+#pragma unroll
+            for (int e = 0; e < 3; ++e) scale[e] = d.scales[3 * block + e];
+            if (n > 0) {
+                decode_first(m, load_codes(static_cast<const uint8_t*>(d.m) + first + at, n), scale[0]);
+                decode_second(v, load_codes(static_cast<const uint8_t*>(d.v) + first + at, n), scale[1], scale[2]);
+            }
+        }
+        T stored[4];
+        uint32_t bits[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float ge = g[e] * grad_scale;
+            m[e] = fmaf(h.one1, ge, h.beta1 * m[e]);
+            v[e] = fmaf(h.one2 * ge, ge, h.beta2 * v[e]);
+            const float down = fmaf(__builtin_amdgcn_sqrtf(v[e]), root, h.eps);
+            p[e] = fmaf(-rate * m[e], __builtin_amdgcn_rcpf(down), p[e] * keep);
+            // fp32 numbers, of which the stored ones are roundings: left to itself the compiler rounds the exact sum to fp16
+            asm("" : "+v"(p[e]));
+            bits[e] = mix(base + (uint32_t)(at + e));
+            if constexpr (MASTER || std::is_same<T, float>::value) stored[e] = from_f32<T>(p[e]);
+            else stored[e] = round_at_random(T{}, p[e], mix(bits[e] + 0x3C6EF373u));
+        }
+        if (n > 0) {
+            put4(param + at, stored, n);
+            if constexpr (MASTER) put4(master + at, p, n);
+            if constexpr (BITS == 32) {
+                put4(static_cast<float*>(d.m) + first + at, m, n);
+                put4(static_cast<float*>(d.v) + first + at, v, n);
+            }
+        }
+        if (d.transposed) {                           // uniform
+            typedef T t4 __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<t4*>(turned + at) = t4{stored[0], stored[1], stored[2], stored[3]};
+        }
+        if constexpr (BITS == 8) {
+            constexpr float kLeast = 0x1p-120f;
+            float top_m = 0.f, top_v = 0.f, low_v = std::numeric_limits<float>::infinity();
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < n) {
+                    top_m = fmaxf(top_m, fabsf(m[e]));
+                    top_v = fmaxf(top_v, v[e]);
+                    if (v[e] >= kLeast) low_v = fminf(low_v, v[e]);
+                }
+            top_m = wave_max(top_m);
+            top_v = wave_max(top_v);
+            low_v = -wave_max(-low_v);
+            scale[0] = top_m >= 0x1p-100f ? top_m * (1.f / kTop8) : 0.f;
+            const float inverse = top_m >= 0x1p-100f ? kTop8 / top_m : 0.f;
+            int packed = __builtin_amdgcn_cvt_pk_fp8_f32(m[0] * inverse, m[1] * inverse, 0, false);
+            packed = __builtin_amdgcn_cvt_pk_fp8_f32(m[2] * inverse, m[3] * inverse, packed, true);
+            const bool some = top_v >= kLeast;
+            scale[1] = some ? __builtin_amdgcn_logf(fmaxf(low_v, top_v * 0x1p-40f)) : 0.f;      // log2
+            scale[2] = some ? fmaxf((__builtin_amdgcn_logf(top_v) - scale[1]) * (1.f / 254.f), 0x1p-12f) : 0x1p-12f;
+            const float per = 1.f / scale[2], step = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(scale[2]) - 1.f);
+            uint32_t codes = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float place = floorf((__builtin_amdgcn_logf(v[e]) - scale[1]) * per);
+                const float below = fminf(fmaxf(place, 0.f), 253.f);
+                const float up = fmaf(v[e], __builtin_amdgcn_exp2f(-fmaf(below, scale[2], scale[1])), -1.f) * step;
+                const uint32_t code = (uint32_t)below + 1u + ((float)(bits[e] >> 8) * 0x1p-24f < up ? 1u : 0u);
+                codes |= (v[e] >= kLeast ? code : 0u) << (8 * e);
+            }
+            if (n > 0) {
+                put_codes(static_cast<uint8_t*>(d.m) + first + at, (uint32_t)packed, n);
+                put_codes(static_cast<uint8_t*>(d.v) + first + at, codes, n);
+            }
+            if (lane < 3) d.scales[3 * block + lane] = lane == 0 ? scale[0] : lane == 1 ? scale[1] : scale[2];
+        }
+    }
+    if (!d.transposed) return;                        // uniform
+    __syncthreads();
+    // Blocks are whole in the chunk.  Element e of a block of W^T is (c, a) = (e / bs_r, e mod bs_r).
+    constexpr int V = 16 / (int)sizeof(T);
+    const int r_log = d.r_log, c_log = d.c_log, e_log = r_log + c_log;
+    T* const out = static_cast<T*>(d.transposed);
+    const int64_t block0 = first >> e_log;
+    if ((1 << r_log) >= V) {
+        for (int u = threadIdx.x * V; u < there; u += kThreads * V) {
+            const int b = u >> e_log, e = u & ((1 << e_log) - 1), c = e >> r_log, a = e & ((1 << r_log) - 1);
+            typedef T tv __attribute__((ext_vector_type(V)));
+            tv w;
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[i] = turned[(b << e_log) + ((a + i) << c_log) + c];
+            *reinterpret_cast<tv*>(out + ((int64_t)d.place[block0 + b] << e_log) + e) = w;
+        }
+    } else {
+        for (int u = threadIdx.x; u < there; u += kThreads) {
+            const int b = u >> e_log, e = u & ((1 << e_log) - 1), c = e >> r_log, a = e & ((1 << r_log) - 1);
+            out[((int64_t)d.place[block0 + b] << e_log) + e] = turned[(b << e_log) + (a << c_log) + c];
+        }
+    }
+}
+
+constexpr int kOutputs = 64;                          // tensors of a launch
+struct output_ptrs { void* m[kOutputs]; void* v[kOutputs]; };
+
+// The moments as values of type O.
+template <typename O, int BITS>
+__global__ __launch_bounds__(kThreads) void bsr_adamw_values(const tensor_desc* __restrict__ tensors, const int2* __restrict__ chunks, int first_tensor,
+                                                             output_ptrs outs)
+{
+    const int2 where = chunks[blockIdx.x];
+    const tensor_desc& d = tensors[where.x];
+    O* const m_out = static_cast<O*>(outs.m[where.x - first_tensor]);
+    O* const v_out = static_cast<O*>(outs.v[where.x - first_tensor]);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t first = (int64_t)where.y * kChunk;
+    const int there = (int)min(d.count - first, (int64_t)kChunk);
+#pragma unroll
+    for (int q = 0; q < kPasses; ++q) {
+        const int at = (q * 4 + wave) * kShared + lane * 4, n = there - at;
+        if (n <= 0) break;
+        const int64_t block = (first + (q * 4 + wave) * kShared) / kShared;
+        float m[4], v[4];
+        if constexpr (BITS == 32) {
+            load4(m, static_cast<const float*>(d.m) + first + at, n);
+            load4(v, static_cast<const float*>(d.v) + first + at, n);
+        } else {
+            const float* s = d.scales + 3 * block;
+            decode_first(m, load_codes(static_cast<const uint8_t*>(d.m) + first + at, n), s[0]);
+            decode_second(v, load_codes(static_cast<const uint8_t*>(d.v) + first + at, n), s[1], s[2]);
+        }
+        O a[4], b[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { a[e] = from_f32<O>(m[e]); b[e] = from_f32<O>(v[e]); }
+        if (m_out) put4(m_out + first + at, a, n);
+        if (v_out) put4(v_out + first + at, b, n);
+    }
+}
+
+size_t size_of(bsr_dtype t) { return t == BSR_F32 ? 4 : 2; }
+bool known(bsr_dtype t) { return (int)t >= (int)BSR_F32 && (int)t <= (int)BSR_BF16; }
+size_t words_of(size_t bytes) { return (bytes + 255) / 256 * 64; }
+int log2_of(int64_t v) { int l = 0; while (((int64_t)1 << l) < v) ++l; return l; }
+// Whether the step's own kernel writes the transposes of such blocks: they are whole in a chunk.
+bool turns(const bsr_adamw_tensor& t) { return kChunk % ((int64_t)t.bs_r * t.bs_c) == 0; }
+// Whether bsr_transpose_values() takes them: sides of whole 16-byte pieces, or blocks that fit its LDS.
+bool transposable(const bsr_adamw_tensor& t)
+{
+    const int64_t u = 16 / (int64_t)size_of(t.dtype), block = (int64_t)t.bs_r * t.bs_c;
+    if (t.bs_r % u == 0 && t.bs_c % u == 0 && t.count / (u * u) < ((int64_t)1 << 31)) return true;
+    return block <= 32 * 1024 && (size_t)t.bs_r * (size_t)(t.bs_c + 1) * size_of(t.dtype) <= 64 * 1024;
+}
+
+}  // namespace
+
+struct bsr_adamw {
+    int bits = 32, device = 0;
+    std::vector<bsr_adamw_tensor> tensors;            // the caller's, in the order of the table (by kind)
+    std::vector<int64_t> number;                      // their places in the caller's list
+    std::vector<int32_t> first_chunk;                 // of each, and the end
+    struct launch_t { int kind; int32_t first, count; };
+    std::vector<launch_t> launches;
+    struct behind_t { size_t tensor; const int32_t* perm; };   // transposes that are launches of their own
+    std::vector<behind_t> behind;
+    const tensor_desc* descs = nullptr;               // device
+    const int2* chunks = nullptr;
+    std::vector<int32_t> host;                        // kept for the asynchronous upload
+    hipEvent_t uploaded = nullptr;
+    mutable std::atomic<bool> landed{false};
+};
+
+namespace {
+
+// {type, gradient in fp32, master copy}
+int kind_of(const bsr_adamw_tensor& t) { return ((int)t.dtype * 2 + (t.grad_dtype == BSR_F32)) * 2 + (t.master_dev != nullptr); }
+
+bsr_status check_sizes(int64_t n, const bsr_adamw_tensor* tensors, int32_t state_bits)
+{
+    if (n < 0 || n >= ((int64_t)1 << 24)) return BSR_ERR_SHAPE;
+    if (n > 0 && !tensors) return BSR_ERR_NULL;
+    if (state_bits != 32 && state_bits != 8) return BSR_ERR_DTYPE;
+    int64_t chunks = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        const bsr_adamw_tensor& t = tensors[i];
+        if (t.count < 0 || t.count >= ((int64_t)1 << 40)) return BSR_ERR_SHAPE;
+        if (!known(t.dtype) || (t.grad_dtype != t.dtype && t.grad_dtype != BSR_F32) || (t.master_dev && t.dtype == BSR_F32)) return BSR_ERR_DTYPE;
+        if (t.t_param_dev) {
+            if (t.bs_r <= 0 || t.bs_c <= 0 || t.count % ((int64_t)t.bs_r * t.bs_c) != 0 ||
+                t.count / ((int64_t)t.bs_r * t.bs_c) >= ((int64_t)1 << 31)) return BSR_ERR_SHAPE;
+            if (!turns(t) && !transposable(t)) return BSR_ERR_UNSUPPORTED;
+        }
+        chunks += (t.count + kChunk - 1) / kChunk;
+        if (chunks >= ((int64_t)1 << 24)) return BSR_ERR_SHAPE;   // a launch has below 2^32 threads
+    }
+    return BSR_OK;
+}
+
+size_t workspace_words(int64_t n, const bsr_adamw_tensor* tensors)
+{
+    size_t words = words_of((size_t)n * sizeof(tensor_desc)), chunks = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        const bsr_adamw_tensor& t = tensors[i];
+        chunks += (size_t)((t.count + kChunk - 1) / kChunk);
+        if (t.t_param_dev) words += words_of((size_t)(t.count / ((int64_t)t.bs_r * t.bs_c)) * 4);
+    }
+    return std::max<size_t>(words + words_of(chunks * sizeof(int2)), 64);
+}
+
+// Whether everything that a step writes is apart from everything else of the list.
+bool apart(int64_t n, const bsr_adamw_tensor* tensors, int32_t bits, const byte_range& workspace)
+{
+    struct item { uintptr_t from, to; bool written; };
+    std::vector<item> all;
+    auto add = [&](const void* p, size_t bytes, bool written) {
+        if (p && bytes) all.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written});
+    };
+    add(workspace.p, workspace.bytes, true);
+    for (int64_t i = 0; i < n; ++i) {
+        const bsr_adamw_tensor& t = tensors[i];
+        const size_t c = (size_t)t.count, s = size_of(t.dtype);
+        add(t.param_dev, c * s, true);
+        add(t.t_param_dev, c * s, true);
+        add(t.master_dev, c * 4, true);
+        add(t.exp_avg_dev, c * (size_t)(bits / 8), true);
+        add(t.exp_avg_sq_dev, c * (size_t)(bits / 8), true);
+        if (bits == 8) add(t.scales_dev, (c + kShared - 1) / kShared * 12, true);
+        add(t.grad_dev, c * size_of(t.grad_dtype), false);
+    }
+    std::sort(all.begin(), all.end(), [](const item& a, const item& b) { return a.from < b.from; });
+    uintptr_t end = 0, written_end = 0;               // of what begins before
+    for (const item& x : all) {
+        if (x.from < (x.written ? end : written_end)) return false;
+        end = std::max(end, x.to);
+        if (x.written) written_end = std::max(written_end, x.to);
+    }
+    return true;
+}
+
+bsr_status create_adamw(bsr_adamw** out, int64_t n, const bsr_adamw_tensor* tensors, int32_t state_bits, void* workspace_dev,
+                        size_t workspace_bytes, hipStream_t stream)
+{
+    bsr_status st = check_sizes(n, tensors, state_bits);
+    if (st != BSR_OK) return st;
+    if (!workspace_dev) return BSR_ERR_NULL;
+    if (!aligned16(workspace_dev)) return BSR_ERR_ALIGN;
+    const size_t words = workspace_words(n, tensors);
+    if (workspace_bytes < words * 4) return BSR_ERR_WORKSPACE;
+    for (int64_t i = 0; i < n; ++i) {
+        const bsr_adamw_tensor& t = tensors[i];
+        if (t.count == 0) continue;
+        if (!t.param_dev || !t.grad_dev || !t.exp_avg_dev || !t.exp_avg_sq_dev || (state_bits == 8 && !t.scales_dev) ||
+            (t.t_param_dev && !t.t_perm_host)) return BSR_ERR_NULL;
+        for (const void* p : {(const void*)t.param_dev, (const void*)t.master_dev, t.grad_dev, (const void*)t.exp_avg_dev,
+                              (const void*)t.exp_avg_sq_dev, (const void*)t.t_param_dev})
+            if (!aligned16(p)) return BSR_ERR_ALIGN;
+        if (reinterpret_cast<uintptr_t>(t.scales_dev) & 3u) return BSR_ERR_ALIGN;
+    }
+    if (!apart(n, tensors, state_bits, {workspace_dev, words * 4})) return BSR_ERR_OVERLAP;
+    std::unique_ptr<bsr_adamw> opt(new bsr_adamw);
+    opt->bits = state_bits;
+    std::vector<int64_t> order((size_t)n);
+    for (int64_t i = 0; i < n; ++i) order[(size_t)i] = i;
+    std::stable_sort(order.begin(), order.end(), [&](int64_t a, int64_t b) { return kind_of(tensors[a]) < kind_of(tensors[b]); });
+    opt->host.assign(words, 0);
+    int32_t* const dev = static_cast<int32_t*>(workspace_dev);
+    const size_t chunks_at = words_of((size_t)n * sizeof(tensor_desc));
+    size_t chunk = 0, total = 0;
+    for (int64_t i = 0; i < n; ++i) total += (size_t)((tensors[i].count + kChunk - 1) / kChunk);
+    size_t at = chunks_at + words_of(total * sizeof(int2));
+    for (int64_t s = 0; s < n; ++s) {
+        const bsr_adamw_tensor& t = tensors[order[(size_t)s]];
+        opt->first_chunk.push_back((int32_t)chunk);
+        const int32_t mine = (int32_t)((t.count + kChunk - 1) / kChunk);
+        for (int32_t c = 0; c < mine; ++c, ++chunk) {
+            opt->host[chunks_at + 2 * chunk] = (int32_t)s;
+            opt->host[chunks_at + 2 * chunk + 1] = c;
+        }
+        if (mine) {
+            if (opt->launches.empty() || opt->launches.back().kind != kind_of(t)) opt->launches.push_back({kind_of(t), (int32_t)chunk - mine, 0});
+            opt->launches.back().count += mine;
+        }
+        tensor_desc d{};
+        d.param = t.param_dev; d.master = t.master_dev; d.grad = t.grad_dev; d.m = t.exp_avg_dev; d.v = t.exp_avg_sq_dev;
+        d.scales = t.scales_dev; d.count = t.count; d.decay = t.weight_decay; d.number = (uint32_t)order[(size_t)s];
+        if (t.t_param_dev && t.count) {
+            const int64_t blocks = t.count / ((int64_t)t.bs_r * t.bs_c);
+            std::vector<char> seen((size_t)blocks, 0);
+            const bool here = turns(t);
+            for (int64_t q = 0; q < blocks; ++q) {    // block perm[q] of W goes to place q of W^T
+                const int32_t p = t.t_perm_host[q];
+                if (p < 0 || p >= blocks || seen[(size_t)p]) return BSR_ERR_INDEX;
+                seen[(size_t)p] = 1;
+                if (here) opt->host[at + (size_t)p] = (int32_t)q;
+                else opt->host[at + (size_t)q] = p;
+            }
+            if (here) {
+                d.transposed = t.t_param_dev;
+                d.place = dev + at;
+                d.r_log = log2_of(t.bs_r);
+                d.c_log = log2_of(t.bs_c);
+            } else {
+                opt->behind.push_back({(size_t)s, dev + at});
+            }
+            at += words_of((size_t)blocks * 4);
+        }
+        std::memcpy(opt->host.data() + (size_t)s * (sizeof(tensor_desc) / 4), &d, sizeof d);
+        opt->tensors.push_back(t);
+        opt->tensors.back().t_perm_host = nullptr;    // read during the call only
+        opt->number.push_back(order[(size_t)s]);
+    }
+    opt->first_chunk.push_back((int32_t)chunk);
+    opt->descs = reinterpret_cast<const tensor_desc*>(dev);
+    opt->chunks = reinterpret_cast<const int2*>(dev + chunks_at);
+    if (hipGetDevice(&opt->device) != hipSuccess) return BSR_ERR_HIP;
+    if (n > 0 && (is_capturing(stream) || !upload_words(dev, opt->host, stream, opt->uploaded, opt->landed))) {
+        if (opt->uploaded) (void)hipEventDestroy(opt->uploaded);
+        (void)hipGetLastError();
+        return BSR_ERR_HIP;
+    }
+    *out = opt.release();
+    return BSR_OK;
+}
+
+template <typename T, typename GT, bool MASTER>
+bsr_status launch_kind(const bsr_adamw* opt, const bsr_adamw::launch_t& l, const step_args& h, hipStream_t stream)
+{
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)l.count), dim3(kThreads), 0, stream, opt->descs, opt->chunks + l.first, h);
+        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    };
+    return opt->bits == 8 ? go(bsr_adamw_chunks<T, GT, 8, MASTER>) : go(bsr_adamw_chunks<T, GT, 32, MASTER>);
+}
+
+template <typename T>
+bsr_status launch_type(const bsr_adamw* opt, const bsr_adamw::launch_t& l, const step_args& h, hipStream_t stream)
+{
+    const bool f32_grad = (l.kind >> 1) & 1, master = l.kind & 1;
+    if (master) return f32_grad ? launch_kind<T, float, true>(opt, l, h, stream) : launch_kind<T, T, true>(opt, l, h, stream);
+    return f32_grad ? launch_kind<T, float, false>(opt, l, h, stream) : launch_kind<T, T, false>(opt, l, h, stream);
+}
+
+bool on_its_device(const bsr_adamw* opt)
+{
+    int dev = -1;
+    return hipGetDevice(&dev) == hipSuccess && dev == opt->device;
+}
+
+}  // namespace
+
+extern "C" {
+
+bsr_status bsr_adamw_workspace_size(int64_t n_tensors, const bsr_adamw_tensor* tensors, int32_t state_bits, size_t* bytes)
+{
+    if (!bytes) return BSR_ERR_NULL;
+    *bytes = 0;
+    const bsr_status st = check_sizes(n_tensors, tensors, state_bits);
+    if (st == BSR_OK) *bytes = workspace_words(n_tensors, tensors) * 4;
+    return st;
+}
+
+bsr_status bsr_adamw_create(bsr_adamw** out, int64_t n_tensors, const bsr_adamw_tensor* tensors, int32_t state_bits, void* workspace_dev,
+                            size_t workspace_bytes, void* hip_stream)
+{
+    if (!out) return BSR_ERR_NULL;
+    *out = nullptr;
+    try {
+        return create_adamw(out, n_tensors, tensors, state_bits, workspace_dev, workspace_bytes, (hipStream_t)hip_stream);
+    } catch (const std::bad_alloc&) {                 // no host memory for the tables
+        return BSR_ERR_HIP;
+    } catch (const std::length_error&) {
+        return BSR_ERR_SHAPE;
+    }
+}
+
+void bsr_adamw_destroy(bsr_adamw* opt)
+{
+    if (!opt) return;
+    if (opt->uploaded) {                              // the upload reads the handle's host buffer
+        (void)hipEventSynchronize(opt->uploaded);
+        (void)hipEventDestroy(opt->uploaded);
+        (void)hipGetLastError();
+    }
+    delete opt;
+}
+
+bsr_status bsr_adamw_step(const bsr_adamw* opt, const bsr_adamw_hyper* hyper, void* hip_stream)
+{
+    if (!opt || !hyper) return BSR_ERR_NULL;
+    const bsr_adamw_hyper& y = *hyper;
+    // (negated: NaN is refused too)
+    if (!(y.beta1 >= 0 && y.beta1 < 1) || !(y.beta2 >= 0 && y.beta2 < 1) || !(y.eps >= 0) || (!y.step_dev && y.step < 1) ||
+        (!y.lr_dev && !(y.lr >= 0)) || (!y.grad_scale_dev && y.grad_scale != y.grad_scale)) return BSR_ERR_SHAPE;
+    for (const void* p : {(const void*)y.lr_dev, (const void*)y.grad_scale_dev})
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return BSR_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(y.step_dev) & 7u) return BSR_ERR_ALIGN;
+    if (!on_its_device(opt)) return BSR_ERR_DEVICE;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    order_after_upload(stream, opt->uploaded, opt->landed);
+    step_args h{};
+    h.lr = (float)y.lr;
+    h.beta1 = (float)y.beta1;
+    h.beta2 = (float)y.beta2;
+    h.one1 = (float)(1.0 - y.beta1);
+    h.one2 = (float)(1.0 - y.beta2);
+    h.eps = (float)y.eps;
+    h.log1 = (float)std::log(y.beta1);
+    h.log2 = (float)std::log(y.beta2);
+    if (!y.step_dev) {
+        h.rate = (float)(1.0 / (1.0 - std::pow(y.beta1, (double)y.step)));
+        h.root = (float)(1.0 / std::sqrt(1.0 - std::pow(y.beta2, (double)y.step)));
+        h.key = step_key(y.seed, (uint64_t)y.step);
+    }
+    h.grad_scale = y.grad_scale;
+    h.seed = y.seed;
+    h.lr_dev = y.lr_dev;
+    h.step_dev = y.step_dev;
+    h.grad_scale_dev = y.grad_scale_dev;
+    if (!y.grad_scale_dev && y.grad_scale == 0.f) return BSR_OK;
+    for (const auto& l : opt->launches) {
+        const int type = l.kind >> 2;
+        const bsr_status st = type == BSR_F32 ? launch_kind<float, float, false>(opt, l, h, stream)
+                            : type == BSR_F16 ? launch_type<f16_t>(opt, l, h, stream) : launch_type<bf16_t>(opt, l, h, stream);
+        if (st != BSR_OK) return st;
+    }
+    for (const auto& b : opt->behind) {
+        const bsr_adamw_tensor& t = opt->tensors[b.tensor];
+        const bsr_status st = bsr_transpose_values(t.dtype, t.bs_r, t.bs_c, t.count / ((int64_t)t.bs_r * t.bs_c), b.perm, t.param_dev,
+                                                   t.t_param_dev, hip_stream);
+        if (st != BSR_OK) return st;
+    }
+    return BSR_OK;
+}
+
+bsr_status bsr_adamw_moments(const bsr_adamw* opt, bsr_dtype dtype, void* const* exp_avg_out, void* const* exp_avg_sq_out, void* hip_stream)
+{
+    if (!opt || !exp_avg_out || !exp_avg_sq_out) return BSR_ERR_NULL;
+    if (!known(dtype)) return BSR_ERR_DTYPE;
+    const size_t n = opt->tensors.size();
+    for (size_t i = 0; i < n; ++i)
+        if (!aligned16(exp_avg_out[i]) || !aligned16(exp_avg_sq_out[i])) return BSR_ERR_ALIGN;
+    if (!on_its_device(opt)) return BSR_ERR_DEVICE;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    order_after_upload(stream, opt->uploaded, opt->landed);
+    for (size_t s = 0; s < n; s += kOutputs) {
+        const size_t end = std::min(n, s + kOutputs);
+        const int32_t first = opt->first_chunk[s], count = opt->first_chunk[end] - first;
+        if (count == 0) continue;
+        output_ptrs outs{};
+        for (size_t i = s; i < end; ++i) {
+            outs.m[i - s] = exp_avg_out[opt->number[i]];
+            outs.v[i - s] = exp_avg_sq_out[opt->number[i]];
+        }
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), 0, stream, opt->descs, opt->chunks + first, (int)s, outs);
+            return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        };
+        const bool eight = opt->bits == 8;
+        const bsr_status st = dtype == BSR_F32 ? (eight ? go(bsr_adamw_values<float, 8>) : go(bsr_adamw_values<float, 32>))
+                            : dtype == BSR_F16 ? (eight ? go(bsr_adamw_values<f16_t, 8>) : go(bsr_adamw_values<f16_t, 32>))
+                                               : (eight ? go(bsr_adamw_values<bf16_t, 8>) : go(bsr_adamw_values<bf16_t, 32>));
+        if (st != BSR_OK) return st;
+    }
+    return BSR_OK;
+}
+
+}  // extern "C"

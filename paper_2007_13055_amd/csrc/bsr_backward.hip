@@ -1,0 +1,212 @@
+// The gradient of the product's epilogue:  dZ = G * act'(Z),  db[j] = sum over i of dZ[i][j]  (fp32, before its rounding).
+//
+// One pass over G and Z: a lane keeps V neighbouring columns (16 bytes of G where its rows are whole multiples of that, else
+// one element) and walks down the rows of its workgroup's chunk, storing dZ and adding up V sums in registers.  LPR lanes
+// cover a row of a strip, so a matrix of few columns still has 256 / LPR rows per workgroup in flight.  The sums of a workgroup's rows
+// are added through LDS as a tree, those of the chunks of rows by a second, small launch in a fixed order: no atomics, the
+// same bits every time.
+//
+// What bounds it: memory.  It moves 2 or 3 matrices and computes some 20 operations an element.
+#include <algorithm>
+
+#include "bsr_epilogue.h"
+
+using namespace bsr_dev;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMostChunks = 256;
+
+struct backward_shape {
+    int v;                                            // columns of a lane
+    int lpr_log;                                      // log2 of the lanes of a row of a strip
+    int strips, chunks, rows;                         // workgroups along n and m, rows of a chunk
+};
+
+// The split of an m x n matrix, v columns a lane.
+backward_shape split(int64_t m, int64_t n, int v)
+{
+    backward_shape s{v, 0, 1, 1, 0};
+    const int64_t units = (n + v - 1) / v;
+    while (s.lpr_log < 6 && (1 << s.lpr_log) < units) ++s.lpr_log;
+    s.strips = (int)((units + (1 << s.lpr_log) - 1) >> s.lpr_log);
+    const int64_t slots = kThreads >> s.lpr_log;      // rows in flight
+    // about 1024 workgroups, four for every CU, of at least two rows a lane
+    int64_t chunks = std::min<int64_t>(std::max<int64_t>(1024 / s.strips, 1), (m + 2 * slots - 1) / (2 * slots));
+    chunks = std::min<int64_t>(std::max<int64_t>(chunks, 1), kMostChunks);
+    s.rows = (int)((m + chunks - 1) / chunks);
+    s.rows = (int)((s.rows + slots - 1) / slots * slots);
+    s.chunks = (int)((m + s.rows - 1) / s.rows);
+    return s;
+}
+
+template <typename G, typename O, int V, bool SUMS>
+__global__ __launch_bounds__(kThreads) void bsr_backward_pass(const G* g, const G* z, O* dz, float* __restrict__ partial,
+                                                              int m, int n, int lpr_log, int rows, int act)
+{
+    __shared__ float red[SUMS ? kThreads * V : 1];
+    const int tid = threadIdx.x, lpr = 1 << lpr_log, slots = kThreads >> lpr_log;
+    const int col = (int)((blockIdx.x << lpr_log) + (tid & (lpr - 1))) * V;
+    const int first = (int)blockIdx.y * rows, end = min(first + rows, m);
+    float sum[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = 0.f;
+    if (col < n) {
+        constexpr int U = V == 1 ? 8 : 4;             // rows whose loads are in flight
+        const int step = slots;
+        int i = first + (tid >> lpr_log);
+        auto rows_of = [&](auto count, int i) {
+            constexpr int K = decltype(count)::value;
+            float gv[K][V], zv[K][V];
+#pragma unroll
+            for (int u = 0; u < K; ++u) {
+                const size_t at = (size_t)(i + u * step) * (size_t)n + (size_t)col;
+                load_run<G>(gv[u], g + at);
+                if (z) load_run<G>(zv[u], z + at);
+            }
+            if (z)
+                with_act(act, [&](auto a) {
+#pragma unroll
+                    for (int u = 0; u < K; ++u)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            gv[u][e] *= act_slope<decltype(a)::value>(zv[u][e]);
+                            // an fp32 number whether or not it is summed: without the sums the compiler would round the
+                            // exact product to fp16 in one instruction, and dZ would hang on what else is wanted
+                            asm("" : "+v"(gv[u][e]));
+                        }
+                });
+#pragma unroll
+            for (int u = 0; u < K; ++u) {
+                if (dz) store_run<O>(dz + (size_t)(i + u * step) * (size_t)n + (size_t)col, gv[u]);
+                if constexpr (SUMS)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) sum[e] += gv[u][e];
+            }
+        };
+        for (; i + (U - 1) * step < end; i += U * step) rows_of(std::integral_constant<int, U>{}, i);
+        for (; i < end; i += step) rows_of(std::integral_constant<int, 1>{}, i);
+    }
+    if constexpr (SUMS) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) red[tid * V + e] = sum[e];
+        for (int half = kThreads / 2; half >= lpr; half >>= 1) {
+            __syncthreads();
+            if (tid < half)
+#pragma unroll
+                for (int e = 0; e < V; ++e) red[tid * V + e] += red[(tid + half) * V + e];
+        }
+        __syncthreads();
+        for (int t = tid; t < lpr * V; t += kThreads) {
+            const int c = (int)(blockIdx.x << lpr_log) * V + t;
+            if (c < n) partial[(size_t)blockIdx.y * (size_t)n + c] = red[t];
+        }
+    }
+}
+
+// db[j] = sum of partial[c][j] over the chunks: 64 columns a workgroup, four shares of the chunks.
+__global__ __launch_bounds__(256) void bsr_backward_sums(const float* __restrict__ partial, float* __restrict__ db, int n, int chunks)
+{
+    __shared__ float red[4][64];
+    const int lane = threadIdx.x & 63, share = threadIdx.x >> 6, col = (int)blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (col < n) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        int c = share;
+        for (; c + 12 < chunks; c += 16)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] += partial[(size_t)(c + 4 * u) * (size_t)n + col];
+        for (; c < chunks; c += 4) v[0] += partial[(size_t)c * (size_t)n + col];
+        s = (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    red[share][lane] = s;
+    __syncthreads();
+    if (share == 0 && col < n) db[col] = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+}
+
+// Elements of 16 bytes.
+int wide_columns(bsr_dtype g_dtype) { return g_dtype == BSR_F32 ? 4 : 8; }
+
+template <typename G, typename O>
+bsr_status launch_types(const backward_shape& s, int64_t m, int64_t n, bsr_act act, const void* g, const void* z, void* dz, float* db,
+                        float* ws, hipStream_t stream)
+{
+    float* out = s.chunks > 1 ? ws : db;
+    auto go = [&](auto v_tag, auto sums_tag) -> bsr_status {
+        constexpr int V = decltype(v_tag)::value;
+        constexpr bool SUMS = decltype(sums_tag)::value;
+        hipLaunchKernelGGL((bsr_backward_pass<G, O, V, SUMS>), dim3((unsigned)s.strips, (unsigned)s.chunks), dim3(kThreads), 0, stream,
+                           (const G*)g, (const G*)z, (O*)dz, out, (int)m, (int)n, s.lpr_log, s.rows, (int)act);
+        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    };
+    auto with_v = [&](auto sums_tag) {
+        return s.v == 1 ? go(std::integral_constant<int, 1>{}, sums_tag) : go(std::integral_constant<int, std::is_same<G, float>::value ? 4 : 8>{}, sums_tag);
+    };
+    const bsr_status st = db ? with_v(std::true_type{}) : with_v(std::false_type{});
+    if (st != BSR_OK || !db || s.chunks == 1) return st;
+    hipLaunchKernelGGL(bsr_backward_sums, dim3((unsigned)((n + 63) / 64)), dim3(256), 0, stream, ws, db, (int)n, s.chunks);
+    return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+}
+
+bool sizes_fit(int64_t m, int64_t n) { return m >= 0 && n >= 0 && m < ((int64_t)1 << 30) && n < ((int64_t)1 << 31) - 512; }
+
+}  // namespace
+
+extern "C" {
+
+bsr_status bsr_epilogue_backward_workspace_size(int64_t m, int64_t n, size_t* bytes)
+{
+    if (!bytes) return BSR_ERR_NULL;
+    *bytes = 0;
+    if (!sizes_fit(m, n)) return BSR_ERR_SHAPE;
+    if (m == 0 || n == 0) return BSR_OK;
+    int chunks = 1;
+    for (int v : {1, 4, 8})
+        if (n % v == 0) chunks = std::max(chunks, split(m, n, v).chunks);
+    if (chunks > 1) *bytes = ((size_t)chunks * (size_t)n * sizeof(float) + 255) & ~(size_t)255;
+    return BSR_OK;
+}
+
+bsr_status bsr_epilogue_backward(int64_t m, int64_t n, bsr_act act, bsr_dtype g_dtype, const void* G_dev, const void* Z_dev,
+                                 bsr_dtype dz_dtype, void* DZ_dev, float* DB_dev, void* workspace_dev, size_t workspace_bytes,
+                                 void* hip_stream)
+{
+    if (!sizes_fit(m, n)) return BSR_ERR_SHAPE;
+    if ((int)g_dtype < 0 || (int)g_dtype > (int)BSR_BF16 || (int)dz_dtype < 0 || (int)dz_dtype > (int)BSR_BF16 || !known_act(act))
+        return BSR_ERR_DTYPE;
+    if (dz_dtype != g_dtype && g_dtype != BSR_F32) return BSR_ERR_DTYPE;
+    if (n == 0) return BSR_OK;
+    if (m > 0 && (!G_dev || (act != BSR_ACT_NONE && !Z_dev))) return BSR_ERR_NULL;
+    if (!DZ_dev && !DB_dev) return BSR_ERR_NULL;
+    if (m > 0 && n >= ((int64_t)1 << 40) / m) return BSR_ERR_SHAPE;
+    const void* Z = act == BSR_ACT_NONE ? nullptr : Z_dev;
+    for (const void* p : {G_dev, Z, (const void*)DZ_dev, (const void*)DB_dev, (const void*)workspace_dev})
+        if (!aligned16(p)) return BSR_ERR_ALIGN;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    if (m == 0) {                                     // no rows: the sums are zero
+        if (!DB_dev) return BSR_OK;
+        hipLaunchKernelGGL(bsr_backward_sums, dim3((unsigned)((n + 63) / 64)), dim3(256), 0, stream, DB_dev, DB_dev, (int)n, 0);
+        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    }
+    const backward_shape s = split(m, n, n % wide_columns(g_dtype) == 0 ? wide_columns(g_dtype) : 1);
+    size_t need = DB_dev && s.chunks > 1 ? (size_t)s.chunks * (size_t)n * sizeof(float) : 0;
+    if (need && (!workspace_dev || workspace_bytes < need)) return BSR_ERR_WORKSPACE;
+    const size_t elements = (size_t)m * (size_t)n, g_size = g_dtype == BSR_F32 ? 4 : 2, dz_size = dz_dtype == BSR_F32 ? 4 : 2;
+    const byte_range g{G_dev, elements * g_size}, z{Z, elements * g_size}, dz{DZ_dev, elements * dz_size},
+        db{DB_dev, (size_t)n * sizeof(float)}, ws{need ? workspace_dev : nullptr, need};
+    // dZ may take the place of G or of Z, element by element
+    const bool in_place = dz_dtype == g_dtype;
+    if ((overlap(dz, g) && !(in_place && DZ_dev == G_dev)) || (overlap(dz, z) && !(in_place && DZ_dev == Z))) return BSR_ERR_OVERLAP;
+    for (const byte_range& r : {g, z, dz})
+        if (overlap(db, r) || overlap(ws, r)) return BSR_ERR_OVERLAP;
+    if (overlap(db, ws)) return BSR_ERR_OVERLAP;
+    float* part = static_cast<float*>(workspace_dev);
+    if (g_dtype == BSR_F16) return launch_types<f16_t, f16_t>(s, m, n, act, G_dev, Z, DZ_dev, DB_dev, part, stream);
+    if (g_dtype == BSR_BF16) return launch_types<bf16_t, bf16_t>(s, m, n, act, G_dev, Z, DZ_dev, DB_dev, part, stream);
+    if (dz_dtype == BSR_F16) return launch_types<float, f16_t>(s, m, n, act, G_dev, Z, DZ_dev, DB_dev, part, stream);
+    if (dz_dtype == BSR_BF16) return launch_types<float, bf16_t>(s, m, n, act, G_dev, Z, DZ_dev, DB_dev, part, stream);
+    return launch_types<float, float>(s, m, n, act, G_dev, Z, DZ_dev, DB_dev, part, stream);
+}
+
+}  // extern "C"

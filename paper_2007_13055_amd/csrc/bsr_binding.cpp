@@ -22,6 +22,9 @@ bsr_status (*g_spmm_static)(const bsr_matrix*, int64_t, const void*, void*, bsr_
 bsr_status (*g_sddmm)(const bsr_matrix*, int64_t, const void*, const void*, void*, bsr_dtype, void*, size_t, void*) = nullptr;
 bsr_status (*g_sddmm_workspace)(const bsr_matrix*, int64_t, size_t*) = nullptr;
 bsr_status (*g_scratch_size)(const bsr_matrix*, int64_t, size_t*) = nullptr;
+bsr_status (*g_spmm_epilogue)(const bsr_matrix*, int64_t, const void*, void*, bsr_dtype, const bsr_epilogue*, void*) = nullptr;
+bsr_status (*g_backward)(int64_t, int64_t, bsr_act, bsr_dtype, const void*, const void*, bsr_dtype, void*, float*, void*, size_t, void*) = nullptr;
+bsr_status (*g_backward_workspace)(int64_t, int64_t, size_t*) = nullptr;
 PyObject* g_error = nullptr;                          // BsrError(status, where)
 
 // What the calls need to know of a matrix; owned by the Python object that owns the handle.
@@ -283,17 +286,208 @@ PyObject* sddmm(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
-// bind(address of bsr_spmm_ex, bsr_spmm_static, bsr_sddmm_ws, bsr_scratch_size, bsr_sddmm_workspace_size, BsrError)
+// Code of an activation's name (None: none), -1 with KeyError(name).
+int act_code(PyObject* name)
+{
+    static const char* const names[] = {"none", "relu", "gelu", "gelu_tanh", "silu"};
+    if (name == Py_None) return BSR_ACT_NONE;
+    if (PyUnicode_Check(name)) {
+        const char* s = PyUnicode_AsUTF8(name);
+        if (!s) return -1;
+        for (int i = 0; i < 5; ++i)
+            if (!strcmp(s, names[i])) return i;
+    }
+    PyErr_SetObject(PyExc_KeyError, name);
+    return -1;
+}
+
+// Whether the kernels of this call may touch the tensor: they run on the current device's current stream.
+bool here(const at::Tensor& t, const char* what)
+{
+    if (t.is_cuda() && t.get_device() == c10::hip::current_device()) return true;
+    PyErr_Format(PyExc_ValueError, "%s must be on the current GPU", what);
+    return false;
+}
+
+// An optional contiguous (rows, cols) tensor of type `code` on the current GPU; false with an error set.
+bool matrix_of(PyObject* obj, const char* what, int64_t rows, int64_t cols, int code, const at::Tensor** out)
+{
+    *out = nullptr;
+    if (obj == Py_None) return true;
+    const at::Tensor* t = nullptr;
+    if (!tensor_of(obj, what, &t)) return false;
+    if (!dims2(*t, rows, cols) || !t->is_contiguous() || t->scalar_type() != kTypes[code]) {
+        PyErr_Format(PyExc_ValueError, "%s must be a contiguous (%lld, %lld) tensor of the result's type", what, (long long)rows, (long long)cols);
+        return false;
+    }
+    *out = t;
+    return here(*t, what);
+}
+
+// spmm_epilogue(W, core, X, Y or None, y_dtype or None, bias or None, act or None, residual or None, through or None,
+//               Z or None, keep_z) -> Y, or (Y, Z) where Z or keep_z is given
+PyObject* spmm_epilogue(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 11) return value_error("spmm_epilogue takes 11 arguments");
+    core_object* c = core_of(a[1]);
+    const at::Tensor *X = nullptr, *Y = nullptr, *bias = nullptr, *residual = nullptr, *through = nullptr, *Z = nullptr;
+    if (!c || !tensor_of(a[2], "X", &X)) return nullptr;
+    if (X->dim() != 2 || X->size(1) != c->k) return value_error("X must be (m, k)");
+    const int x_code = type_code(*X, a[2]);
+    if (x_code < 0) return nullptr;
+    if (x_code != c->dtype || !X->is_contiguous()) return value_error("X must be contiguous and of W's dtype");
+    if (!here(*X, "X")) return nullptr;
+    const int64_t m = X->size(0);
+    const int y_code = name_code(a[4], c->dtype);
+    if (y_code < 0) return nullptr;
+    bsr_epilogue ep{};
+    const int act = act_code(a[6]);
+    if (act < 0) return nullptr;
+    ep.act = (bsr_act)act;
+    if (a[5] != Py_None) {
+        if (!tensor_of(a[5], "bias", &bias)) return nullptr;
+        const int code = type_code(*bias, a[5]);
+        if (code < 0) return nullptr;
+        if (bias->dim() != 1 || bias->size(0) != c->n || !bias->is_contiguous() || (code != c->dtype && code != BSR_F32))
+            return value_error("bias must be a contiguous (n,) tensor of W's dtype or fp32");
+        if (!here(*bias, "bias")) return nullptr;
+        ep.bias_dev = bias->data_ptr();
+        ep.bias_dtype = (bsr_dtype)code;
+    }
+    if (a[7] != Py_None) {
+        if (!tensor_of(a[7], "residual", &residual)) return nullptr;
+        if (!dims2(*residual, m, c->n) || residual->scalar_type() != kTypes[y_code] ||
+            (c->n > 1 && residual->stride(1) != 1) || (m > 1 && residual->stride(0) < c->n))
+            return value_error("residual must be an (m, n) tensor of the result's type, its rows contiguous");
+        if (!here(*residual, "residual")) return nullptr;
+        ep.residual_dev = residual->data_ptr();
+        ep.residual_ld = m > 1 ? residual->stride(0) : 0;
+    }
+    if (!matrix_of(a[8], "through", m, c->n, y_code, &through) || !matrix_of(a[9], "Z", m, c->n, y_code, &Z) ||
+        !matrix_of(a[3], "Y", m, c->n, y_code, &Y)) return nullptr;
+    if (through) ep.through_dev = through->data_ptr();
+    const int keep_z = PyObject_IsTrue(a[10]);
+    if (keep_z < 0 || !ensure_scratch(a[0], c, m)) return nullptr;
+    at::Tensor fresh_y, fresh_z;
+    if (!Y) {
+        fresh_y = result({m, c->n}, y_code, *X);
+        Y = &fresh_y;
+    }
+    if (!Z && keep_z) {
+        fresh_z = result({m, c->n}, y_code, *X);
+        Z = &fresh_z;
+    }
+    if (Z) ep.z_dev = Z->data_ptr();
+    const void* xp = X->data_ptr();
+    void* yp = Y->data_ptr();
+    bsr_status st;
+    {
+        pybind11::gil_scoped_release no_gil;
+        st = g_spmm_epilogue(c->handle, m, xp, yp, (bsr_dtype)y_code, &ep, stream());
+    }
+    if (st != BSR_OK) return failed(st, "bsr_spmm_epilogue");
+    PyObject* y_obj = a[3];
+    if (y_obj == Py_None) y_obj = THPVariable_Wrap(std::move(fresh_y));
+    else Py_INCREF(y_obj);
+    if (!Z || !y_obj) return y_obj;
+    PyObject* z_obj = a[9];
+    if (z_obj == Py_None) z_obj = THPVariable_Wrap(std::move(fresh_z));
+    else Py_INCREF(z_obj);
+    if (!z_obj) { Py_DECREF(y_obj); return nullptr; }
+    PyObject* pair = PyTuple_Pack(2, y_obj, z_obj);
+    Py_DECREF(y_obj);
+    Py_DECREF(z_obj);
+    return pair;
+    END_HANDLE_TH_ERRORS
+}
+
+// epilogue_backward(G, Z or None, act or None, DZ or None, dz_dtype or None, DB or None, need_dz, need_db) -> (DZ or None, DB or None)
+PyObject* epilogue_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 8) return value_error("epilogue_backward takes 8 arguments");
+    const at::Tensor *G = nullptr, *Z = nullptr, *DZ = nullptr, *DB = nullptr;
+    if (!tensor_of(a[0], "G", &G)) return nullptr;
+    const int g_code = type_code(*G, a[0]);
+    if (g_code < 0) return nullptr;
+    if (G->dim() != 2 || !G->is_contiguous()) return value_error("G must be a contiguous (m, n) tensor");
+    if (!here(*G, "G")) return nullptr;
+    const int64_t m = G->size(0), n = G->size(1);
+    const int act = act_code(a[2]);
+    if (act < 0) return nullptr;
+    if (!matrix_of(a[1], "Z", m, n, g_code, &Z)) return nullptr;
+    if (!Z && act != BSR_ACT_NONE) return value_error("Z must be given unless act is none");
+    const int dz_code = name_code(a[4], g_code);
+    if (dz_code < 0) return nullptr;
+    if (dz_code != g_code && g_code != BSR_F32) return value_error("dz_dtype must be G's type unless that is fp32");
+    if (!matrix_of(a[3], "DZ", m, n, dz_code, &DZ)) return nullptr;
+    if (a[5] != Py_None) {
+        if (!tensor_of(a[5], "DB", &DB)) return nullptr;
+        if (DB->dim() != 1 || DB->size(0) != n || !DB->is_contiguous() || DB->scalar_type() != at::kFloat)
+            return value_error("DB must be a contiguous (n,) fp32 tensor");
+        if (!here(*DB, "DB")) return nullptr;
+    }
+    const int need_dz = PyObject_IsTrue(a[6]), need_db = PyObject_IsTrue(a[7]);
+    if (need_dz < 0 || need_db < 0) return nullptr;
+    // without an activation dZ is G: nothing to compute unless its type changes or a buffer of its own is given
+    const bool dz_is_g = !DZ && need_dz && act == BSR_ACT_NONE && dz_code == g_code;
+    at::Tensor fresh_dz, fresh_db, ws;
+    if (!DZ && need_dz && !dz_is_g) {
+        fresh_dz = result({m, n}, dz_code, *G);
+        DZ = &fresh_dz;
+    }
+    if (!DB && need_db) {
+        fresh_db = result({n}, BSR_F32, *G);
+        DB = &fresh_db;
+    }
+    if (DZ || DB) {
+        size_t ws_bytes = 0;
+        if (DB) {
+            const bsr_status st = g_backward_workspace(m, n, &ws_bytes);
+            if (st != BSR_OK) return failed(st, "bsr_epilogue_backward_workspace_size");
+            if (ws_bytes) ws = at::Tensor(at::detail::empty_cuda({(int64_t)ws_bytes}, at::kByte, G->device(), std::nullopt));
+        }
+        bsr_status st;
+        {
+            pybind11::gil_scoped_release no_gil;
+            st = g_backward(m, n, (bsr_act)act, (bsr_dtype)g_code, G->data_ptr(), Z ? Z->data_ptr() : nullptr, (bsr_dtype)dz_code,
+                            DZ ? DZ->data_ptr() : nullptr, DB ? DB->data_ptr<float>() : nullptr, ws_bytes ? ws.data_ptr() : nullptr,
+                            ws_bytes, stream());
+        }
+        if (st != BSR_OK) return failed(st, "bsr_epilogue_backward");
+    }
+    auto object = [](PyObject* given, at::Tensor& fresh) -> PyObject* {
+        if (given == Py_None && fresh.defined()) return THPVariable_Wrap(std::move(fresh));
+        Py_INCREF(given);
+        return given;
+    };
+    PyObject* dz_obj = dz_is_g ? object(a[0], fresh_dz) : object(a[3], fresh_dz);
+    if (!dz_obj) return nullptr;
+    PyObject* db_obj = object(a[5], fresh_db);
+    if (!db_obj) { Py_DECREF(dz_obj); return nullptr; }
+    PyObject* pair = PyTuple_Pack(2, dz_obj, db_obj);
+    Py_DECREF(dz_obj);
+    Py_DECREF(db_obj);
+    return pair;
+    END_HANDLE_TH_ERRORS
+}
+
+// bind(address of bsr_spmm_ex, bsr_spmm_static, bsr_sddmm_ws, bsr_scratch_size, bsr_sddmm_workspace_size,
+//      bsr_spmm_epilogue, bsr_epilogue_backward, bsr_epilogue_backward_workspace_size, BsrError)
 PyObject* bind(PyObject*, PyObject* args)
 {
-    unsigned long long f[5];
+    unsigned long long f[8];
     PyObject* error = nullptr;
-    if (!PyArg_ParseTuple(args, "KKKKKO", &f[0], &f[1], &f[2], &f[3], &f[4], &error)) return nullptr;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &error)) return nullptr;
     g_spmm = reinterpret_cast<decltype(g_spmm)>(f[0]);
     g_spmm_static = reinterpret_cast<decltype(g_spmm_static)>(f[1]);
     g_sddmm = reinterpret_cast<decltype(g_sddmm)>(f[2]);
     g_scratch_size = reinterpret_cast<decltype(g_scratch_size)>(f[3]);
     g_sddmm_workspace = reinterpret_cast<decltype(g_sddmm_workspace)>(f[4]);
+    g_spmm_epilogue = reinterpret_cast<decltype(g_spmm_epilogue)>(f[5]);
+    g_backward = reinterpret_cast<decltype(g_backward)>(f[6]);
+    g_backward_workspace = reinterpret_cast<decltype(g_backward_workspace)>(f[7]);
     Py_INCREF(error);
     Py_XDECREF(g_error);
     g_error = error;
@@ -305,6 +499,10 @@ PyMethodDef methods[] = {
     {"spmm", reinterpret_cast<PyCFunction>(spmm), METH_FASTCALL, "spmm(W, core, X, Y, y_dtype, path) -> Y"},
     {"spmm_static", reinterpret_cast<PyCFunction>(spmm_static), METH_FASTCALL, "spmm_static(core, X, Y) -> Y"},
     {"sddmm", reinterpret_cast<PyCFunction>(sddmm), METH_FASTCALL, "sddmm(W, core, G, X, D, d_dtype, lend) -> D"},
+    {"spmm_epilogue", reinterpret_cast<PyCFunction>(spmm_epilogue), METH_FASTCALL,
+     "spmm_epilogue(W, core, X, Y, y_dtype, bias, act, residual, through, Z, keep_z) -> Y or (Y, Z)"},
+    {"epilogue_backward", reinterpret_cast<PyCFunction>(epilogue_backward), METH_FASTCALL,
+     "epilogue_backward(G, Z, act, DZ, dz_dtype, DB, need_dz, need_db) -> (DZ, DB)"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Native host path of the binding.", -1, methods};

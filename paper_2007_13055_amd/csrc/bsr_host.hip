@@ -56,7 +56,6 @@ size_t plan_bytes(int64_t R, int64_t nnzb, int32_t bs_r, int32_t bs_c, int64_t k
     return (b + 255) & ~(size_t)255;
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 }  // namespace
 
@@ -656,12 +655,12 @@ bsr_status run_product(const spmm_args& a, bsr_path path, const tune_opts& t)
 
 }  // namespace
 
-bsr_status bsr_spmm_ex(const bsr_matrix* W, int64_t m, const void* X_dev, void* Y_dev,
-                       bsr_dtype y_dtype, bsr_path path, void* hip_stream)
+// A checked product on `path` (AUTO: what bsr_tune() remembered, else the library's choice).
+static bsr_status multiply(const spmm_args& a, bsr_path path)
 {
-    if (path != BSR_PATH_AUTO && path != BSR_PATH_WAVE && path != BSR_PATH_MFMA) return BSR_ERR_UNSUPPORTED;
-    const bsr_status st = check_product_args(W, m, X_dev, Y_dev, y_dtype);
-    if (st != BSR_OK || m == 0 || W->n == 0) return st;
+    const bsr_matrix* W = a.W;
+    const int64_t m = a.m;
+    const bsr_dtype y_dtype = a.y_dtype;
     tune_opts t = W->env_tune;
     if (path == BSR_PATH_AUTO) {
         bool tuned = false;
@@ -675,7 +674,48 @@ bsr_status bsr_spmm_ex(const bsr_matrix* W, int64_t m, const void* X_dev, void* 
             (!W->scratch || W->scratch_bytes < mfma_thin_scratch_bytes(W, m))) tuned = false;
         if (!tuned) { path = auto_path(W, m, y_dtype); if (!t.from_env) t = tune_opts{}; }
     }
-    return run_product(spmm_args{W, m, X_dev, Y_dev, y_dtype, (hipStream_t)hip_stream}, path, t);
+    return run_product(a, path, t);
+}
+
+bsr_status bsr_spmm_ex(const bsr_matrix* W, int64_t m, const void* X_dev, void* Y_dev,
+                       bsr_dtype y_dtype, bsr_path path, void* hip_stream)
+{
+    if (path != BSR_PATH_AUTO && path != BSR_PATH_WAVE && path != BSR_PATH_MFMA) return BSR_ERR_UNSUPPORTED;
+    const bsr_status st = check_product_args(W, m, X_dev, Y_dev, y_dtype);
+    if (st != BSR_OK || m == 0 || W->n == 0) return st;
+    return multiply(spmm_args{W, m, X_dev, Y_dev, y_dtype, (hipStream_t)hip_stream}, path);
+}
+
+bsr_status bsr_spmm_epilogue(const bsr_matrix* W, int64_t m, const void* X_dev, void* Y_dev, bsr_dtype y_dtype,
+                             const bsr_epilogue* epilogue, void* hip_stream)
+{
+    if (!epilogue) return BSR_ERR_NULL;
+    const bsr_status st = check_product_args(W, m, X_dev, Y_dev, y_dtype);
+    if (st != BSR_OK) return st;
+    const bsr_epilogue& e = *epilogue;
+    if (!known_act(e.act) || (e.bias_dev && e.bias_dtype != W->dtype && e.bias_dtype != BSR_F32)) return BSR_ERR_DTYPE;
+    if (m == 0 || W->n == 0) return BSR_OK;
+    const size_t y_size = y_dtype == BSR_F32 ? 4 : 2, x_size = W->dtype == BSR_F32 ? 4 : 2;
+    const int64_t ld = e.residual_ld ? e.residual_ld : W->n;
+    if (e.residual_dev && (ld < W->n || ld >= ((int64_t)1 << 37) / m)) return BSR_ERR_SHAPE;
+    for (const void* p : {e.bias_dev, e.residual_dev, e.through_dev, (const void*)e.z_dev})
+        if (!aligned16(p)) return BSR_ERR_ALIGN;
+    if (e.residual_dev && ld != W->n && (size_t)ld * y_size % 16 != 0) return BSR_ERR_ALIGN;
+    const size_t out = (size_t)m * (size_t)W->n * y_size;
+    const byte_range in[] = {{X_dev, (size_t)m * (size_t)W->k * x_size},
+                             {e.bias_dev, (size_t)W->n * (e.bias_dtype == BSR_F32 ? 4 : 2)},
+                             {e.residual_dev, ((size_t)(m - 1) * (size_t)ld + (size_t)W->n) * y_size},
+                             {e.through_dev, out},
+                             {W->data, (size_t)W->nnzb * (size_t)W->bs_r * (size_t)W->bs_c * x_size}};
+    const byte_range y{Y_dev, out}, z{e.z_dev, out};
+    if (overlap(y, z)) return BSR_ERR_OVERLAP;
+    for (const byte_range& r : in)
+        if (overlap(y, r) || overlap(z, r)) return BSR_ERR_OVERLAP;
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev != W->device) return BSR_ERR_DEVICE;
+    spmm_args a{W, m, X_dev, Y_dev, y_dtype, (hipStream_t)hip_stream};
+    a.epilogue = epilogue;
+    return multiply(a, BSR_PATH_AUTO);
 }
 
 // Candidate settings per kernel family for this W, m and type of result (the search space of bsr_tune).
@@ -823,6 +863,8 @@ const char* bsr_status_string(bsr_status s)
         case BSR_ERR_WORKSPACE: return "workspace smaller than bsr_workspace_size() reports";
         case BSR_ERR_HIP: return "HIP runtime call failed";
         case BSR_ERR_UNSUPPORTED: return "requested kernel path does not support this block shape";
+        case BSR_ERR_DEVICE: return "the handle was created on another device than the current one";
+        case BSR_ERR_OVERLAP: return "a buffer that is written overlaps another one of the call";
         case BSR_ERR_SCRATCH_LIMIT: return "the product needs more scratch than the library's built-in array (BSR_STATIC_SCRATCH_BYTES)";
     }
     return "unknown status";

@@ -200,7 +200,18 @@ struct spmm_args {
     bsr_dtype y_dtype;
     hipStream_t stream;
     int first_slot = 0;                      // tile kernel: leave out the slots before this one (another kernel multiplies them)
+    const bsr_epilogue* epilogue = nullptr;  // what happens to the sums before they are stored (bsr_epilogue.h); null: nothing
 };
+
+// A call's buffers, for the checks of what is written against what else there is.  A null pointer overlaps nothing.
+struct byte_range { const void* p; size_t bytes; };
+inline bool overlap(const byte_range& a, const byte_range& b)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return x && y && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
+inline bool known_act(bsr_act act) { return (int)act >= (int)BSR_ACT_NONE && (int)act <= (int)BSR_ACT_SILU; }
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 tune_opts read_tune_env();
 // Debug mode: checks index_pointer, block_indices and the plan on the device (one launch, a copy and a stream

@@ -16,7 +16,7 @@
 // split, so the sum over c is complete whatever order the instruction takes its k in.
 #include <numeric>
 
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 
@@ -27,12 +27,12 @@ namespace {
 //   MT   result tiles along m per wavefront                    CH = BS_C / (64/MM) contiguous run per lane
 // grid: blockIdx.x = slot + R * (m-tile); slot s works on block-row row_order[s] (longest first).
 // No LDS and no barrier: wavefronts whose rows lie beyond m leave at once.
-template <typename T, typename O, int BS_R, int BS_C, int MT>
+template <typename T, typename O, int BS_R, int BS_C, int MT, typename E>
 __global__ __launch_bounds__(256) void bsr_mfma_direct(const T* __restrict__ X, const T* __restrict__ data,
                                                        const int32_t* __restrict__ indices,
                                                        const int32_t* __restrict__ indptr,
                                                        const int32_t* __restrict__ row_order, O* __restrict__ Y,
-                                                       int m, int k, int n, int R)
+                                                       int m, int k, int n, int R, E ep)
 {
     constexpr int MM = BS_R >= 32 ? 32 : 16;
     constexpr int NA = BS_R / MM;
@@ -94,21 +94,19 @@ __global__ __launch_bounds__(256) void bsr_mfma_direct(const T* __restrict__ X, 
     }
 
     // store: lane holds, for row i, columns r*BS_R + u*MM + (MM==32 ? 8*g + 4*h : 4*h) + 0..3
-    O* yrow_base = Y + (size_t)r * BS_R;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const int i = i_base + t * MM + li;
         if (i < m) {
-            O* yrow = yrow_base + (size_t)i * (size_t)n;
 #pragma unroll
             for (int u = 0; u < NA; ++u) {
                 if constexpr (MM == 32) {
 #pragma unroll
                     for (int g = 0; g < 4; ++g)
-                        store4<O>(yrow + u * 32 + 8 * g + 4 * h, acc[u][t][4 * g], acc[u][t][4 * g + 1],
-                                  acc[u][t][4 * g + 2], acc[u][t][4 * g + 3]);
+                        finish_store4<T, O>(ep, Y, i, r * BS_R + u * 32 + 8 * g + 4 * h, n, acc[u][t][4 * g], acc[u][t][4 * g + 1],
+                                            acc[u][t][4 * g + 2], acc[u][t][4 * g + 3]);
                 } else {
-                    store4<O>(yrow + u * 16 + 4 * h, acc[u][t][0], acc[u][t][1], acc[u][t][2], acc[u][t][3]);
+                    finish_store4<T, O>(ep, Y, i, r * BS_R + u * 16 + 4 * h, n, acc[u][t][0], acc[u][t][1], acc[u][t][2], acc[u][t][3]);
                 }
             }
         }
@@ -127,10 +125,12 @@ bsr_status launch_direct_shape(const spmm_args& a, const tune_opts& tune)
         const int64_t tiles = (m + rows_per_wg - 1) / rows_per_wg;
         const int64_t blocks = tiles * R;
         if (blocks >= ((int64_t)1 << 31) || blocks * 64 * waves >= ((int64_t)1 << 32)) return BSR_ERR_SHAPE;
-        hipLaunchKernelGGL((bsr_mfma_direct<T, O, BS_R, BS_C, MT>), dim3((unsigned)blocks), dim3(64 * waves), 0,
-                           a.stream, (const T*)a.X, (const T*)W->data, W->indices, W->indptr, W->row_order,
-                           (O*)a.Y, m, k, n, R);
-        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        return with_epilogue(a, [&](auto ep) -> bsr_status {
+            hipLaunchKernelGGL((bsr_mfma_direct<T, O, BS_R, BS_C, MT, decltype(ep)>), dim3((unsigned)blocks), dim3(64 * waves), 0,
+                               a.stream, (const T*)a.X, (const T*)W->data, W->indices, W->indptr, W->row_order,
+                               (O*)a.Y, m, k, n, R, ep);
+            return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        });
     };
     // Tile height: enough workgroups to fill 256 CUs several times over when m allows it, taller
     // wavefront tiles (more reuse of each W block) when m is large.

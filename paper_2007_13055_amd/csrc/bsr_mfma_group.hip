@@ -67,7 +67,7 @@
 #include <algorithm>
 #include <numeric>
 
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 
@@ -157,11 +157,11 @@ constexpr int kStageStride = 64 * 4 + 16;             // bytes of a staged row, 
 constexpr int kStage = 64 * kStageStride;
 static_assert(kG * kStage <= kSlots * kTileBytes, "the group's results fit the ring");
 
-template <typename T, typename O>
+template <typename T, typename O, typename E>
 __global__ __launch_bounds__(768) void bsr_mfma_group(const T* __restrict__ X, const T* __restrict__ data,
                                                       const int32_t* __restrict__ recs,
                                                       const int32_t* __restrict__ gdesc, O* __restrict__ Y,
-                                                      int m, int k, int n, int n_groups, int n_sub)
+                                                      int m, int k, int n, int n_groups, int n_sub, E ep)
 {
     typedef __attribute__((address_space(3))) void lds_void;
     typedef __attribute__((address_space(1))) const void glob_void;
@@ -405,6 +405,8 @@ __global__ __launch_bounds__(768) void bsr_mfma_group(const T* __restrict__ X, c
                         v[e] += t[0]; v[e + 1] += t[1]; v[e + 2] += t[2]; v[e + 3] += t[3];
                     }
                 }
+                if constexpr (E::on)
+                    if (i0 + row < m) finish<T, O>(ep, v, i0 + row, r * 64 + pc * EPP, n);
                 u32x4 out;
                 if constexpr (std::is_same<O, float>::value) {
                     out = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
@@ -609,12 +611,14 @@ bsr_status launch_group_types(const spmm_args& a)
     const int n_sub = (m + kSub - 1) / kSub;
     const int64_t grid = (int64_t)((n_sub + kXcds - 1) / kXcds) * kXcds * W->grp_n;
     if (grid <= 0 || grid >= ((int64_t)1 << 31)) return BSR_ERR_UNSUPPORTED;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_group<T, O>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
-    if (attr != hipSuccess) return BSR_ERR_HIP;
-    hipLaunchKernelGGL((bsr_mfma_group<T, O>), dim3((unsigned)grid), dim3(768), kLdsBytes, a.stream, (const T*)a.X,
-                       (const T*)W->data, W->grp_recs, W->grp_desc, (O*)a.Y, m, k, n, W->grp_n, n_sub);
-    return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    return with_epilogue(a, [&](auto ep) -> bsr_status {
+        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_group<T, O, decltype(ep)>),
+                                                           hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+        if (attr != hipSuccess) return BSR_ERR_HIP;
+        hipLaunchKernelGGL((bsr_mfma_group<T, O, decltype(ep)>), dim3((unsigned)grid), dim3(768), kLdsBytes, a.stream, (const T*)a.X,
+                           (const T*)W->data, W->grp_recs, W->grp_desc, (O*)a.Y, m, k, n, W->grp_n, n_sub, ep);
+        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    });
 }
 
 }  // namespace

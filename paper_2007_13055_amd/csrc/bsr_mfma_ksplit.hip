@@ -17,7 +17,7 @@
 // operations complete in order: no barrier.  Loads are buffer loads: a block the wavefront does
 // not have and rows of X past m read as zeros without touching memory, which keeps a wavefront's
 // loads unconditional and their number in flight fixed (two blocks ahead).
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 
@@ -90,11 +90,11 @@ struct ksplit_geom {
 
 // STR > 1: the stored blocks are STR * BS_R rows tall and the workgroup takes strip blockIdx.y of them -- few items
 // otherwise leave most CUs idle while a wavefront works through a whole block by itself.
-template <typename T, typename O, int BS_R, int BS_C, int MM_, int STR>
+template <typename T, typename O, int BS_R, int BS_C, int MM_, int STR, typename E>
 __global__ __launch_bounds__(BS_R == 16 ? 1024 : 512) void bsr_mfma_ksplit(const T* __restrict__ X, const T* __restrict__ data,
                                                        const int32_t* __restrict__ indices,
                                                        const int32_t* __restrict__ row_desc, O* __restrict__ Y,
-                                                       int m, int k, int n, int R, int per, int items)
+                                                       int m, int k, int n, int R, int per, int items, E ep)
 {
     typedef ksplit_geom<T, BS_R, BS_C, MM_> geo;
     constexpr int MM = geo::MM, S = geo::S, RBS = geo::RBS, P = geo::P, BLK = geo::BLK;
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(BS_R == 16 ? 1024 : 512) void bsr_mfma_ksplit(const
         for (int w = 0; w < used; ++w)
             s += *reinterpret_cast<const f32x4*>(lds + (size_t)w * geo::REGION + ((size_t)i * LD + 4 * q) * 4);
         if (i_base + i < m)
-            store4<O>(Y + (size_t)(i_base + i) * (size_t)n + (size_t)(STR > 1 ? r * STR + (int)blockIdx.y : r) * BS_R + 4 * q, s.x, s.y, s.z, s.w);
+            finish_store4<T, O>(ep, Y, i_base + i, (STR > 1 ? r * STR + (int)blockIdx.y : r) * BS_R + 4 * q, n, s.x, s.y, s.z, s.w);
     }
 }
 
@@ -291,13 +291,15 @@ bsr_status launch_ksplit_tile(const spmm_args& a, const tune_opts& tune)
         if (grid > 0) { table = item_table; items = W->n_cu; blocks = grid; }
     }
     const size_t lds = (size_t)nw * geo::REGION;
-    static const hipError_t attr =
-        hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_ksplit<T, O, BS_R, BS_C, MM, STR>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    if (attr != hipSuccess) return BSR_ERR_HIP;
-    hipLaunchKernelGGL((bsr_mfma_ksplit<T, O, BS_R, BS_C, MM, STR>), dim3((unsigned)blocks, STR), dim3(64 * nw), lds, a.stream,
-                       (const T*)a.X, (const T*)W->data, W->indices, table, (O*)a.Y, m, k, n, R, per, items);
-    return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    return with_epilogue(a, [&](auto ep) -> bsr_status {
+        static const hipError_t attr =
+            hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_ksplit<T, O, BS_R, BS_C, MM, STR, decltype(ep)>),
+                                hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        if (attr != hipSuccess) return BSR_ERR_HIP;
+        hipLaunchKernelGGL((bsr_mfma_ksplit<T, O, BS_R, BS_C, MM, STR, decltype(ep)>), dim3((unsigned)blocks, STR), dim3(64 * nw), lds,
+                           a.stream, (const T*)a.X, (const T*)W->data, W->indices, table, (O*)a.Y, m, k, n, R, per, items, ep);
+        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    });
 }
 
 // Blocks of 32 and 64 rows in strips of 16, a workgroup each, while there are few items: a block's whole height is

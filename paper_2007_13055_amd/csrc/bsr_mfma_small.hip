@@ -12,7 +12,7 @@
 // between products as with every other kernel.
 #include <algorithm>
 
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 
@@ -71,12 +71,12 @@ struct small_geom {
     static constexpr int REGION = ((STAGE > PART ? STAGE : PART) + 15) & ~15;
 };
 
-template <typename T, typename O, int BS_R, int BS_C>
+template <typename T, typename O, int BS_R, int BS_C, typename E>
 __global__ __launch_bounds__(512) void bsr_mfma_small(const T* __restrict__ X, const T* __restrict__ data, int w_bytes,
                                                       const int32_t* __restrict__ sb_desc,
                                                       const i32x4* __restrict__ sb_entries,
                                                       const int32_t* __restrict__ sb_cols, O* __restrict__ Y,
-                                                      int m, int k, int n, int sb_rows, int per)
+                                                      int m, int k, int n, int sb_rows, int per, E ep)
 {
     typedef small_geom<T> geo;
     constexpr int S = geo::S, RBS = geo::RBS, P = geo::P, LD = geo::LD;
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(512) void bsr_mfma_small(const T* __restrict__ X, c
         for (int w = 0; w < used; ++w)
             s += *reinterpret_cast<const f32x4*>(lds + (size_t)w * geo::REGION + ((size_t)i * LD + 4 * c4) * 4);
         if (i_base + i < m)
-            store4<O>(Y + (size_t)(i_base + i) * (size_t)n + (size_t)tr * 16 + 4 * c4, s.x, s.y, s.z, s.w);
+            finish_store4<T, O>(ep, Y, i_base + i, tr * 16 + 4 * c4, n, s.x, s.y, s.z, s.w);
     }
 }
 
@@ -191,10 +191,12 @@ bsr_status launch_small_shape(const spmm_args& a, const tune_opts& tune)
     nw = nw < 1 ? 1 : (nw > nw_cap ? nw_cap : nw);
     if (tune.nw >= 1 && tune.nw <= 8) nw = tune.nw;
     const size_t lds = (size_t)nw * geo::REGION;
-    hipLaunchKernelGGL((bsr_mfma_small<T, O, BS_R, BS_C>), dim3((unsigned)blocks), dim3(64 * nw), lds, a.stream,
-                       (const T*)a.X, (const T*)W->data, (int)(W->nnzb * W->bs_r * W->bs_c * geo::S), W->sb_desc,
-                       reinterpret_cast<const i32x4*>(W->sb_entries), W->sb_cols, (O*)a.Y, m, k, n, W->sb_rows, per);
-    return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    return with_epilogue(a, [&](auto ep) -> bsr_status {
+        hipLaunchKernelGGL((bsr_mfma_small<T, O, BS_R, BS_C, decltype(ep)>), dim3((unsigned)blocks), dim3(64 * nw), lds, a.stream,
+                           (const T*)a.X, (const T*)W->data, (int)(W->nnzb * W->bs_r * W->bs_c * geo::S), W->sb_desc,
+                           reinterpret_cast<const i32x4*>(W->sb_entries), W->sb_cols, (O*)a.Y, m, k, n, W->sb_rows, per, ep);
+        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    });
 }
 
 template <typename T, typename O>

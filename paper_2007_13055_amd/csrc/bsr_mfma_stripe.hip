@@ -24,7 +24,7 @@
 // LDS layout of the stripe: one PANEL per block-column (TM rows x 32 bytes, panels PS bytes apart),
 // so the 16-row tiles of a lane's operand are at compile-time offsets from one address; the two
 // 16-byte halves of a row are swapped in rows with bit 2 set.
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 
@@ -38,12 +38,12 @@ constexpr int kStageBatch = 8;       // 16-byte loads in flight per thread while
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-template <typename T, typename O, int TM>
+template <typename T, typename O, int TM, typename E>
 __global__ __launch_bounds__(768) void bsr_mfma_stripe16(const T* __restrict__ X, const T* __restrict__ data,
                                                          unsigned w_bytes, const int32_t* __restrict__ pair_ptr,
                                                          const i32x4* __restrict__ pairs, O* __restrict__ Y,
                                                          int m, int k, int n, int R, int n_tiles, int n_groups,
-                                                         int rows_per_group, unsigned cpr_magic)
+                                                         int rows_per_group, unsigned cpr_magic, E ep)
 {
     constexpr int SUB = TM / 16;                      // 16-row MFMA tiles along m
     constexpr int PS = TM * 32 + 32;                  // bytes from one panel to the next (+32: panels shift by 8 banks)
@@ -198,6 +198,30 @@ __global__ __launch_bounds__(768) void bsr_mfma_stripe16(const T* __restrict__ X
     // lanes write one row's 64 outputs as 16-byte pieces.
     constexpr int OB = kRowsPerWave * 16 * (int)sizeof(O);   // bytes of one output row of the wavefront's tile
     constexpr int OS = OB + 16, OC = OB / 16;                // padded LDS stride, 16-byte pieces per row
+    if constexpr (E::on) {
+        // The same with the sums in fp32 (rounded once, behind the epilogue), 16 rows at a time.
+        constexpr int FS = kRowsPerWave * 16 * 4 + 16, EPP = 16 / (int)sizeof(O);
+        unsigned char* fl = lds + (size_t)(C + 1) * PS + (size_t)wave * (16 * FS);
+        const int frow = lane / OC, c0 = (lane - frow * OC) * EPP, cols = (r_end - r_first) * 16;
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            wave_lds_fence();                         // the other lanes have read the rows before
+#pragma unroll
+            for (int j = 0; j < kRowsPerWave; ++j)
+                *reinterpret_cast<f32x4*>(fl + (size_t)li * FS + (j * 16 + 4 * h) * 4) = acc[j][s];
+            wave_lds_fence();
+#pragma unroll
+            for (int pass = 0; pass < 16 * OC / 64; ++pass) {
+                const int row = pass * (64 / OC) + frow, i = i_base + s * 16 + row;
+                float v[EPP];
+                load_run<float>(v, reinterpret_cast<const float*>(fl + (size_t)row * FS) + c0);
+                if (i >= m || c0 >= cols) continue;
+                finish<T, O>(ep, v, i, r_first * 16 + c0, n);
+                store_run<O>(Y + (size_t)i * (size_t)n + r_first * 16 + c0, v);
+            }
+        }
+        return;
+    }
     constexpr int SPP = sizeof(O) == 2 ? (SUB >= 2 ? 2 : 1) : 1;   // 16-row tiles per pass (scratch <= 4.6 KB)
     constexpr int RPI = 64 / OC;                             // rows one store instruction covers
     unsigned char* scratch = lds + (size_t)(C + 1) * PS + (size_t)wave * (SPP * 16 * OS);
@@ -250,19 +274,21 @@ bsr_status launch_stripe_types(const spmm_args& a, const tune_opts& tune)
         rows_per_group = (rows_per_group + kRowsPerWave - 1) / kRowsPerWave * kRowsPerWave;
         n_groups = (R + rows_per_group - 1) / rows_per_group;
         const int waves = rows_per_group / kRowsPerWave;
-        const size_t lds = stripe_lds_bytes(k, TM, waves, sizeof(O));
+        const size_t lds = stripe_lds_bytes(k, TM, waves, a.epilogue ? sizeof(float) : sizeof(O));   // what the sums pass through
         if (lds > 160 * 1024) return BSR_ERR_UNSUPPORTED;
         const int64_t blocks = (int64_t)((n_tiles + kXcds - 1) / kXcds) * kXcds * n_groups;
         if (blocks >= ((int64_t)1 << 31)) return BSR_ERR_SHAPE;
-        static const hipError_t attr =
-            hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_stripe16<T, O, TM>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        if (attr != hipSuccess) return BSR_ERR_HIP;
-        hipLaunchKernelGGL((bsr_mfma_stripe16<T, O, TM>), dim3((unsigned)blocks), dim3(64 * waves), lds, a.stream,
-                           (const T*)a.X, (const T*)W->data, (unsigned)(W->nnzb * 512), W->pair_ptr,
-                           reinterpret_cast<const i32x4*>(W->pairs), (O*)a.Y, m, k, n, R, n_tiles,
-                           n_groups, rows_per_group, (unsigned)(0x100000000ull / (unsigned)(k * sizeof(T) / 16)) + 1u);
-        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        return with_epilogue(a, [&](auto ep) -> bsr_status {
+            static const hipError_t attr =
+                hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_stripe16<T, O, TM, decltype(ep)>),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+            if (attr != hipSuccess) return BSR_ERR_HIP;
+            hipLaunchKernelGGL((bsr_mfma_stripe16<T, O, TM, decltype(ep)>), dim3((unsigned)blocks), dim3(64 * waves), lds, a.stream,
+                               (const T*)a.X, (const T*)W->data, (unsigned)(W->nnzb * 512), W->pair_ptr,
+                               reinterpret_cast<const i32x4*>(W->pairs), (O*)a.Y, m, k, n, R, n_tiles,
+                               n_groups, rows_per_group, (unsigned)(0x100000000ull / (unsigned)(k * sizeof(T) / 16)) + 1u, ep);
+            return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        });
     };
     // rows of X per workgroup: the largest stripe that still leaves 32 m-tiles (fewer, taller stripes
     // read W less often; too few leave CUs idle while a stripe is staged)

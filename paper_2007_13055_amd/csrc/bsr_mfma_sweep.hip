@@ -32,7 +32,7 @@
 #include <cmath>
 #include <numeric>
 
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 using namespace bsr_dev::lds_loads;
@@ -57,12 +57,12 @@ __device__ __forceinline__ constexpr unsigned turn(unsigned r) { return (r >> 1)
 __device__ __forceinline__ void window_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // OWN: outputs that come out as NaN are summed again (below).
-template <typename T, typename O, int SUB, bool OWN>
+template <typename T, typename O, int SUB, bool OWN, typename E>
 __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
     const T* __restrict__ X, const T* __restrict__ data, unsigned w_bytes, const i32x4* __restrict__ recs,
     const int32_t* __restrict__ win_ptr, const i32x4* __restrict__ quads, O* __restrict__ Y, int m, int k, int n,
     int n_tiles, int tiles_padded, int n_quads, int n_win, int q_log, int bs_r, int row_bytes,
-    const int32_t* __restrict__ indptr, const int32_t* __restrict__ indices)
+    const int32_t* __restrict__ indptr, const int32_t* __restrict__ indices, E ep)
 {
     constexpr int S = (int)sizeof(T);
     constexpr int CH = 16 / S;                        // columns of a granule
@@ -244,6 +244,7 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
 #pragma unroll
                 for (int e = 0; e < EPT; ++e) v[e] += src[e];
             }
+            finish<T, O>(ep, v, i, col, n);
             O* dst = Y + (size_t)i * (size_t)n + col;
             if constexpr (EPT == 4) {
                 *reinterpret_cast<f32x4*>(dst) = f32x4{v[0], v[1], v[2], v[3]};
@@ -270,13 +271,14 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
                 for (int e = 0; e < EPT; ++e) {
                     const float stored = (float)dst[e];
                     if (stored == stored) continue;
-                    float own = 0.f;
+                    float own[1] = {0.f};
                     for (int b = indptr[(col + e) >> 3]; b < indptr[((col + e) >> 3) + 1]; ++b) {
                         const T* x = X + (size_t)i * (size_t)k + (size_t)indices[b] * bs_c;
                         const T* w = data + ((size_t)b * 8 + ((col + e) & 7)) * bs_c;
-                        for (int c = 0; c < bs_c; ++c) own += (float)x[c] * (float)w[c];
+                        for (int c = 0; c < bs_c; ++c) own[0] += (float)x[c] * (float)w[c];
                     }
-                    dst[e] = from_f32<O>(own);
+                    finish<T, O>(ep, own, i, col + e, n);
+                    dst[e] = from_f32<O>(own[0]);
                 }
             }
     }
@@ -322,16 +324,18 @@ bsr_status launch_sub(const spmm_args& a, int q_log)
     const int64_t blocks = (int64_t)padded * n_groups;
     if (blocks >= ((int64_t)1 << 31)) return BSR_ERR_SHAPE;
     constexpr size_t ring = (size_t)kRing * SUB * kPitch, out = (size_t)kWaves * (SUB >= 2 ? kRowsOut : 16) * kLdOut * sizeof(float);
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_sweep<T, O, SUB, OWN>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)std::max(ring, out));
-    if (attr != hipSuccess) return BSR_ERR_HIP;
-    hipLaunchKernelGGL((bsr_mfma_sweep<T, O, SUB, OWN>), dim3((unsigned)blocks), dim3(64 * (kWaves + kLoaders)), std::max(ring, out), a.stream,
-                       (const T*)a.X, (const T*)W->data, (unsigned)(W->nnzb * W->bs_r * W->bs_c * sizeof(T)),
-                       reinterpret_cast<const i32x4*>(W->sw_base + W->sw.recs_at), W->sw_base + W->sw.win_at,
-                       reinterpret_cast<const i32x4*>(W->sw_base), (O*)a.Y, m, (int)W->k, (int)W->n,
-                       n_tiles, padded, W->sw_quads, W->sw_windows, q_log, W->bs_r, W->bs_c * (int)sizeof(T),
-                       W->indptr, W->indices);
-    return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    return with_epilogue(a, [&](auto ep) -> bsr_status {
+        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_sweep<T, O, SUB, OWN, decltype(ep)>),
+                                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)std::max(ring, out));
+        if (attr != hipSuccess) return BSR_ERR_HIP;
+        hipLaunchKernelGGL((bsr_mfma_sweep<T, O, SUB, OWN, decltype(ep)>), dim3((unsigned)blocks), dim3(64 * (kWaves + kLoaders)), std::max(ring, out),
+                           a.stream, (const T*)a.X, (const T*)W->data, (unsigned)(W->nnzb * W->bs_r * W->bs_c * sizeof(T)),
+                           reinterpret_cast<const i32x4*>(W->sw_base + W->sw.recs_at), W->sw_base + W->sw.win_at,
+                           reinterpret_cast<const i32x4*>(W->sw_base), (O*)a.Y, m, (int)W->k, (int)W->n,
+                           n_tiles, padded, W->sw_quads, W->sw_windows, q_log, W->bs_r, W->bs_c * (int)sizeof(T),
+                           W->indptr, W->indices, ep);
+        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    });
 }
 
 // A result in fp32 keeps as many chains of additions as the kernel of 16x16 tiles gives it: 8 where that starts few

@@ -12,7 +12,7 @@
 // The lanes that share an output element's reduction are inside the matrix core here; what the
 // paper's reduction kernels do with explicit cross-thread sums (Sections 4.4.2-4.4.3) the MFMA
 // does across its k = 4 lane groups.
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 
@@ -79,11 +79,11 @@ __global__ __launch_bounds__(256) void transpose_f32(const float* __restrict__ X
 // cost 2*U load instructions per chunk, each occupying the memory pipeline for 16 cycles whatever
 // it carries: 3.4 of the kernel's 8.9 us.)  Blocks and block-columns are read through buffer
 // resources over the wavefront's share, so pieces past its end read as zero without branches.
-template <int U>
+template <int U, typename E>
 __global__ __launch_bounds__(256) void bsr_thin16_f32(const float* __restrict__ XT, const float* __restrict__ data,
                                                       const int32_t* __restrict__ indices,
                                                       const int32_t* __restrict__ row_desc, float* __restrict__ Y,
-                                                      int m, int n, int R, int mg)
+                                                      int m, int n, int R, int mg, E ep)
 {
     constexpr int SUBS = 4;                           // 16-row MFMA tiles per wavefront: 64 rows
     constexpr int WT = (U * 256 + 1023) / 1024;       // 1 KiB pieces of W per chunk (a block is 64 bytes)
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(256) void bsr_thin16_f32(const float* __restrict__ 
     f32x4 sum;
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] = (red[0][row][c4 + e] + red[1][row][c4 + e]) + (red[2][row][c4 + e] + red[3][row][c4 + e]);
-    if (i0 + row < m) *reinterpret_cast<f32x4*>(Y + (size_t)(i0 + row) * n + (size_t)r * 16 + c4) = sum;
+    if (i0 + row < m) finish_store4<float, float>(ep, Y, i0 + row, r * 16 + c4, n, sum.x, sum.y, sum.z, sum.w);
 }
 
 }  // namespace
@@ -209,9 +209,11 @@ bsr_status launch_thin_with_scratch(const spmm_args& a, const tune_opts& tune, v
         const int64_t per_xcd = (int64_t)((tiles + mg - 1) / mg) * ((R + 8 / mg - 1) / (8 / mg));
         const int64_t blocks = 8 * per_xcd;
         if (blocks >= ((int64_t)1 << 31)) return BSR_ERR_SHAPE;
-        hipLaunchKernelGGL((bsr_thin16_f32<U>), dim3((unsigned)blocks), dim3(256), 0, a.stream,
-                           (const float*)XT, (const float*)W->data, W->indices, W->row_desc, (float*)a.Y, m, n, R, mg);
-        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        return with_epilogue(a, [&](auto ep) -> bsr_status {
+            hipLaunchKernelGGL((bsr_thin16_f32<U, decltype(ep)>), dim3((unsigned)blocks), dim3(256), 0, a.stream,
+                               (const float*)XT, (const float*)W->data, W->indices, W->row_desc, (float*)a.Y, m, n, R, mg, ep);
+            return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        });
     };
     // groups of 4 blocks per chunk: a quarter of the longest block-row in one chunk when that is at
     // most 16 groups (every chunk multiplies all its U groups, so U should not be much larger)

@@ -31,7 +31,7 @@
 // with loads of their own.  One barrier per phase.
 #include <algorithm>
 
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 
@@ -53,12 +53,12 @@ static_assert(kLds <= 160 * 1024 && kWaves == kRowsX, "LDS; a wavefront moves on
 // LDS writes of this wavefront done, then the workgroup's barrier (loads from memory stay in flight across it)
 __device__ __forceinline__ void wg_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-template <int CAP>
+template <int CAP, typename E>
 __global__ __launch_bounds__(kThreads) void bsr_thin16_rows(const float* __restrict__ X, const float* __restrict__ data,
                                                            const int32_t* __restrict__ indices,
                                                            const int32_t* __restrict__ row_desc,
                                                            const int32_t* __restrict__ ph_ptr, float* __restrict__ Y,
-                                                           int m, int k, int n, int R, int nph, int n_rg, int n_set, int pos_stride)
+                                                           int m, int k, int n, int R, int nph, int n_rg, int n_set, int pos_stride, E ep)
 {
     static_assert(CAP % 4 == 0 && CAP <= kMaxCap, "MFMAs are skipped four at a time");
     constexpr int NC = (4 * CAP + 63) / 64;           // loads of 64 block-columns per run
@@ -196,7 +196,11 @@ __global__ __launch_bounds__(kThreads) void bsr_thin16_rows(const float* __restr
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int i = i0 + 4 * kk + j;
-            if (i < m) Y[(size_t)i * n + (size_t)r * 16 + lo] = acc[0][j] + acc[1][j];
+            float v[1] = {acc[0][j] + acc[1][j]};
+            if (i < m) {
+                finish<float, float>(ep, v, i, r * 16 + lo, n);
+                Y[(size_t)i * n + (size_t)r * 16 + lo] = v[0];
+            }
         }
     }
 }
@@ -255,13 +259,15 @@ bsr_status launch_mfma_thinrow(const spmm_args& a, const tune_opts& tune)
         const int n_rg = (m + kRowsX - 1) / kRowsX, n_set = (R + kWaves - 1) / kWaves;
         const int64_t grid = 8 * (int64_t)((n_rg + 3) / 4) * ((n_set + 1) / 2);
         if (grid >= ((int64_t)1 << 31)) return BSR_ERR_SHAPE;
-        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_thin16_rows<CAP>),
-                                                           hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-        if (attr != hipSuccess) return BSR_ERR_HIP;
-        hipLaunchKernelGGL((bsr_thin16_rows<CAP>), dim3((unsigned)grid), dim3(kThreads), kLds, a.stream, (const float*)a.X,
-                           (const float*)W->data, W->indices, W->row_desc, W->thin_pos, (float*)a.Y, m, k, n, R,
-                           W->thin_nph, n_rg, n_set, W->thin_pos_stride);
-        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        return with_epilogue(a, [&](auto ep) -> bsr_status {
+            static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_thin16_rows<CAP, decltype(ep)>),
+                                                               hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+            if (attr != hipSuccess) return BSR_ERR_HIP;
+            hipLaunchKernelGGL((bsr_thin16_rows<CAP, decltype(ep)>), dim3((unsigned)grid), dim3(kThreads), kLds, a.stream, (const float*)a.X,
+                               (const float*)W->data, W->indices, W->row_desc, W->thin_pos, (float*)a.Y, m, k, n, R,
+                               W->thin_nph, n_rg, n_set, W->thin_pos_stride, ep);
+            return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        });
     };
     // MFMAs of a phase whose operands are loaded ahead (4 blocks each): enough for the average run and a
     // quarter more; the few longer runs take their tails with loads of their own

@@ -15,7 +15,7 @@
 // rest (the plan's long_rows) are started first for all m-tiles.
 #include <algorithm>
 
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 
@@ -40,11 +40,11 @@ struct slot_groups {
     int start[kMaxGroups + 1];
 };
 
-template <typename T, typename O, int BS_R, int BS_C, int MT, int D>
+template <typename T, typename O, int BS_R, int BS_C, int MT, int D, typename E>
 __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, const T* __restrict__ data,
                                                      const int32_t* __restrict__ indices,
                                                      const int32_t* __restrict__ row_desc, O* __restrict__ Y,
-                                                     int m, int k, int n, int R, int n_tiles, slot_groups groups)
+                                                     int m, int k, int n, int R, int n_tiles, slot_groups groups, E ep)
 {
     constexpr int MM = 32;                            // MFMA tile edge (bs_r >= 32 only)
     constexpr int NA = BS_R / MM;
@@ -220,6 +220,34 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
     constexpr int OC = OB / 16;                       // 16-byte pieces per output row
     constexpr int RPP = 64 / OC;                      // rows one wavefront stores per pass
     static_assert(OB % 16 == 0 && 64 % OC == 0 && (MT * MM) % RPP == 0, "output tile splits into 16-byte pieces");
+    if constexpr (E::on) {
+        // The same with the sums in fp32 (rounded once, behind the epilogue), 32 rows at a time.
+        constexpr int FS = BS_R * 4 + 16;             // padded LDS stride
+        constexpr int EPP = 16 / (int)sizeof(O);      // outputs of a piece
+        unsigned char* fl = lds + (size_t)wave * MM * FS;
+        const int frow = lane / OC, j = r * BS_R + (lane - frow * OC) * EPP;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            wave_lds_fence();                         // the other lanes have read the rows before
+#pragma unroll
+            for (int u = 0; u < NA; ++u)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f32x4*>(fl + (size_t)li * FS + (u * 32 + 8 * g + 4 * h) * 4) =
+                        f32x4{acc[u][t][4 * g], acc[u][t][4 * g + 1], acc[u][t][4 * g + 2], acc[u][t][4 * g + 3]};
+            wave_lds_fence();
+#pragma unroll
+            for (int pass = 0; pass < MM / RPP; ++pass) {
+                const int row = pass * RPP + frow, i = i_base + (wave * MT + t) * MM + row;
+                float v[EPP];
+                load_run<float>(v, reinterpret_cast<const float*>(fl + (size_t)row * FS) + (j - r * BS_R));
+                if (i >= m) continue;
+                finish<T, O>(ep, v, i, j, n);
+                store_run<O>(Y + (size_t)i * (size_t)n + j, v);
+            }
+        }
+        return;
+    }
     unsigned char* ol = lds + (size_t)wave * (MT * MM) * OS;
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -281,18 +309,20 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
             const int64_t blocks = (int64_t)((n_tiles + kXcds - 1) / kXcds) * kXcds * (R - first);
             if (blocks >= ((int64_t)1 << 31) || blocks * 256 >= ((int64_t)1 << 32)) return BSR_ERR_SHAPE;
             const size_t lds_stage = (size_t)(TM + BS_R) * (BS_C * sizeof(T) + 16);
-            const size_t lds_out = (size_t)TM * (BS_R * sizeof(O) + 16);
-            const size_t lds = lds_stage > lds_out ? lds_stage : lds_out;
-            if (lds > 48 * 1024) {                    // above the default dynamic-LDS limit: raise it once
-                static const hipError_t attr = hipFuncSetAttribute(
-                    reinterpret_cast<const void*>(&bsr_mfma_tile<T, O, BS_R, BS_C, MT, D>),
-                    hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-                if (attr != hipSuccess) return BSR_ERR_HIP;
-            }
-            hipLaunchKernelGGL((bsr_mfma_tile<T, O, BS_R, BS_C, MT, D>), dim3((unsigned)blocks), dim3(256), lds, a.stream,
-                               (const T*)a.X, (const T*)W->data, W->indices, W->row_desc, (O*)a.Y, m, k, n, R, n_tiles,
-                               groups);
-            return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+            return with_epilogue(a, [&](auto ep) -> bsr_status {
+                const size_t lds_out = decltype(ep)::on ? (size_t)4 * 32 * (BS_R * 4 + 16) : (size_t)TM * (BS_R * sizeof(O) + 16);
+                const size_t lds = lds_stage > lds_out ? lds_stage : lds_out;
+                if (lds > 48 * 1024) {                // above the default dynamic-LDS limit: raise it once
+                    static const hipError_t attr = hipFuncSetAttribute(
+                        reinterpret_cast<const void*>(&bsr_mfma_tile<T, O, BS_R, BS_C, MT, D, decltype(ep)>),
+                        hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+                    if (attr != hipSuccess) return BSR_ERR_HIP;
+                }
+                hipLaunchKernelGGL((bsr_mfma_tile<T, O, BS_R, BS_C, MT, D, decltype(ep)>), dim3((unsigned)blocks), dim3(256), lds, a.stream,
+                                   (const T*)a.X, (const T*)W->data, W->indices, W->row_desc, (O*)a.Y, m, k, n, R, n_tiles,
+                                   groups, ep);
+                return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+            });
         };
         const int depth = tune.a > 0 ? tune.a : 2;
         if (tune.mt == 1) {

@@ -27,7 +27,7 @@
 // the chunk's end read zeros for their block (a buffer load past the end) and add them to a clamped address.
 #include <algorithm>
 
-#include "bsr_mfma_common.h"
+#include "bsr_epilogue.h"
 
 using namespace bsr_dev;
 
@@ -44,12 +44,13 @@ static_assert(kLds <= 160 * 1024 && kTile % 16 == 0, "LDS; 16-byte writes clear 
 
 struct chunk_t { int j, e, cnt; };                    // block-column, first pair, pairs (0: none)
 
+template <typename E>
 __global__ __launch_bounds__(kThreads) void bsr_wide16_f32(const float* __restrict__ X, const float* __restrict__ data,
                                                           const int32_t* __restrict__ pairs,
                                                           const int32_t* __restrict__ chunks,
                                                           const int32_t* __restrict__ chunk_ptr, float* __restrict__ Y,
                                                           int m, int k, int n, int nq, int n_rg,
-                                                          unsigned data_bytes)
+                                                          unsigned data_bytes, E ep)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     const int lane = threadIdx.x & 63;
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(kThreads) void bsr_wide16_f32(const float* __restri
                 f32x4 sum = *reinterpret_cast<const f32x4*>(lds + (row * kTS + 4 * c4) * 4);
 #pragma unroll
                 for (int w = 1; w < kWv; ++w) sum += *reinterpret_cast<const f32x4*>(lds + w * kTile + (row * kTS + 4 * c4) * 4);
-                *reinterpret_cast<f32x4*>(Y + (size_t)(i0 + row) * n + c0 + 4 * c4) = sum;
+                finish_store4<float, float>(ep, Y, i0 + row, c0 + 4 * c4, n, sum.x, sum.y, sum.z, sum.w);
             }
         }
     } else {
@@ -189,7 +190,9 @@ __global__ __launch_bounds__(kThreads) void bsr_wide16_f32(const float* __restri
                 float sum = *reinterpret_cast<const float*>(lds + (row * kTS + c) * 4);
 #pragma unroll
                 for (int w = 1; w < kWv; ++w) sum += *reinterpret_cast<const float*>(lds + w * kTile + (row * kTS + c) * 4);
-                Y[(size_t)(i0 + row) * n + c0 + c] = sum;
+                float v[1] = {sum};
+                finish<float, float>(ep, v, i0 + row, c0 + c, n);
+                Y[(size_t)(i0 + row) * n + c0 + c] = v[0];
             }
         }
     }
@@ -298,11 +301,13 @@ bsr_status launch_mfma_wide(const spmm_args& a, const tune_opts&)
     const int n_rg = (m + kRowsX - 1) / kRowsX, nq = W->wide_nq;
     const int64_t grid = 8 * (int64_t)((n_rg + 3) / 4) * ((nq + 1) / 2);
     if (grid >= ((int64_t)1 << 31)) return BSR_ERR_SHAPE;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_wide16_f32),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-    if (attr != hipSuccess) return BSR_ERR_HIP;
-    hipLaunchKernelGGL(bsr_wide16_f32, dim3((unsigned)grid), dim3(kThreads), kLds, a.stream, (const float*)a.X,
-                       (const float*)W->data, W->wide_pairs, W->wide_chunks, W->wide_chunk_ptr, (float*)a.Y, m, k, n,
-                       nq, n_rg, (unsigned)(W->nnzb * 64));
-    return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    return with_epilogue(a, [&](auto ep) -> bsr_status {
+        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_wide16_f32<decltype(ep)>),
+                                                           hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        if (attr != hipSuccess) return BSR_ERR_HIP;
+        hipLaunchKernelGGL(bsr_wide16_f32<decltype(ep)>, dim3((unsigned)grid), dim3(kThreads), kLds, a.stream, (const float*)a.X,
+                           (const float*)W->data, W->wide_pairs, W->wide_chunks, W->wide_chunk_ptr, (float*)a.Y, m, k, n,
+                           nq, n_rg, (unsigned)(W->nnzb * 64), ep);
+        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    });
 }

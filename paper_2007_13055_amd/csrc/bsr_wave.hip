@@ -9,7 +9,7 @@
 // LDS memory.
 #include <type_traits>
 
-#include "bsr_internal.h"
+#include "bsr_epilogue.h"
 
 namespace {
 
@@ -57,11 +57,11 @@ __device__ __forceinline__ float wave_sum(float v)
 //   block-columns, so the block-column of a lane's elements comes from the same 128 bytes as the
 //   row bounds; longer block-rows read block_indices for the rest.
 // Any block shape, any m.  A block-row without stored blocks leaves the partial sums at zero.
-template <typename T, typename O, int TM, int VEC>
+template <typename T, typename O, int TM, int VEC, typename E>
 __global__ __launch_bounds__(256) void bsr_wave_generic(const T* __restrict__ X, const T* __restrict__ data,
                                                         const int32_t* __restrict__ indices,
                                                         const int32_t* __restrict__ row_desc, O* __restrict__ Y,
-                                                        int m, int k, int n, int bs_r, int bs_c, int col_groups)
+                                                        int m, int k, int n, int bs_r, int bs_c, int col_groups, E ep)
 {
     struct alignas(sizeof(T) * VEC) vec_t { T v[VEC]; };
     const int lane = threadIdx.x & 63;
@@ -97,6 +97,20 @@ __global__ __launch_bounds__(256) void bsr_wave_generic(const T* __restrict__ X,
 #pragma unroll
             for (int v = 0; v < VEC; ++v) acc[t] = fmaf(to_f32(x[t].v[v]), to_f32(w.v[v]), acc[t]);
     }
+    if constexpr (E::on) {                           // lane t finishes row t: the rows' loads and activations side by side
+        float mine[1] = {0.f};
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {
+            const float s = wave_sum(acc[t]);
+            mine[0] = lane == t ? s : mine[0];
+        }
+        const int i = i0 + lane;
+        if (lane < TM && i < m) {
+            bsr_dev::finish<T, O>(ep, mine, i, j, n);
+            Y[(size_t)i * n + j] = from_f32<O>(mine[0]);
+        }
+        return;
+    }
 #pragma unroll
     for (int t = 0; t < TM; ++t) {
         const float s = wave_sum(acc[t]);
@@ -115,10 +129,12 @@ bsr_status launch_generic(const spmm_args& a, const tune_opts& tune)
         const int64_t row_groups = (m + TM - 1) / TM;
         const int64_t blocks = row_groups * col_groups;
         if (blocks >= ((int64_t)1 << 31) || blocks * 256 >= ((int64_t)1 << 32)) return BSR_ERR_SHAPE;
-        hipLaunchKernelGGL((bsr_wave_generic<T, O, TM, VEC>), dim3((unsigned)blocks), dim3(256), 0, a.stream,
-                           (const T*)a.X, (const T*)W->data, W->indices, W->row_desc, (O*)a.Y, m, k, n,
-                           (int)W->bs_r, (int)W->bs_c, col_groups);
-        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        return with_epilogue(a, [&](auto ep) -> bsr_status {
+            hipLaunchKernelGGL((bsr_wave_generic<T, O, TM, VEC, decltype(ep)>), dim3((unsigned)blocks), dim3(256), 0, a.stream,
+                               (const T*)a.X, (const T*)W->data, W->indices, W->row_desc, (O*)a.Y, m, k, n,
+                               (int)W->bs_r, (int)W->bs_c, col_groups, ep);
+            return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        });
     };
     // 16-byte pieces when a block row is made of them (k is a multiple of bs_c and X, W are 16-byte
     // aligned, so every piece is aligned), single elements otherwise
