@@ -28,6 +28,7 @@ struct epilogue_args {
     int64_t residual_ld;
     int32_t act;
     int32_t bias_f32;
+    int32_t once;                                     // residual and Z0 are read past the caches
 };
 struct no_epilogue {
     static constexpr bool on = false;
@@ -40,8 +41,12 @@ bsr_status with_epilogue(const spmm_args& a, F launch)
     if (!a.epilogue) return launch(no_epilogue{});
     const bsr_epilogue& e = *a.epilogue;
     const int32_t act = e.act;
+    // Results beyond a quarter of the 256 MB cache behind the L2s: what is read once for each would push X and W out of it
+    // (residual of 8192 x 8192 fp16: 159 us, read past the caches 140).  Smaller ones it often still holds from the kernel
+    // that wrote them (4096 x 4096 bf16: 31 us, past the caches 38).
+    const bool once = (int64_t)a.m * a.W->n * (a.y_dtype == BSR_F32 ? 4 : 2) > ((int64_t)64 << 20);
     return launch(epilogue_args{e.bias_dev, e.residual_dev, act == BSR_ACT_NONE ? nullptr : e.through_dev, e.z_dev,
-                                e.residual_ld ? e.residual_ld : a.W->n, act, e.bias_dtype == BSR_F32});
+                                e.residual_ld ? e.residual_ld : a.W->n, act, e.bias_dtype == BSR_F32, once});
 }
 
 namespace bsr_dev {
@@ -49,13 +54,16 @@ namespace bsr_dev {
 constexpr float kLog2e = 1.44269504f;
 
 __device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
-// 0 where `share` is, whatever x is (0 * inf is no part of a limit)
-__device__ __forceinline__ float share_of(float share, float x) { return share == 0.f ? 0.f : share * x; }
+// share * x; 0 where share is, at infinite x too (0 * inf is no part of a limit).  A NaN x has made `share` one.
+constexpr float kMost = 3.40282347e+38f;
+__device__ __forceinline__ float share_of(float share, float x) { return share * __builtin_amdgcn_fmed3f(x, -kMost, __builtin_inff()); }
 
-// exp(-a^2 / 2) and Q(a) of a = |x|
-__device__ __forceinline__ void normal_tail(float a, float& e, float& q)
+__device__ __forceinline__ float finite(float x) { return __builtin_amdgcn_fmed3f(x, -kMost, kMost); }
+
+// exp(-x^2 / 2) and Q(|x|)
+__device__ __forceinline__ void normal_tail(float x, float& e, float& q)
 {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.24f, a, 1.f));
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.24f, fabsf(x), 1.f)), y = x * 0.849321800f;   // sqrt(log2(e) / 2)
     float s = -0.0529904738f;
     s = fmaf(s, t, 0.152789459f);
     s = fmaf(s, t, -0.0656933263f);
@@ -64,21 +72,26 @@ __device__ __forceinline__ void normal_tail(float a, float& e, float& q)
     s = fmaf(s, t, 0.0928374827f);
     s = fmaf(s, t, 0.0955223069f);
     s = fmaf(s, t, 0.0957537889f);
-    e = __builtin_amdgcn_exp2f(a * a * (-0.5f * kLog2e));
+    e = __builtin_amdgcn_exp2f(-y * y);
     q = e * (t * s);
 }
 
 constexpr float kGeluA = 1.59576912f, kGeluB = 0.044715f;          // 2 sqrt(2 / pi)
+__device__ __forceinline__ float gelu_share(float x, float xx)      // s(2 u)
+{
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * fmaf(-kLog2e * kGeluA * kGeluB, xx, -kLog2e * kGeluA)));
+}
 
 template <int ACT> __device__ __forceinline__ float act_value(float x)
 {
     if constexpr (ACT == BSR_ACT_RELU) return x < 0.f ? 0.f : x;
     if constexpr (ACT == BSR_ACT_GELU) {
         float e, q;
-        normal_tail(fabsf(x), e, q);
-        return (x < 0.f ? 0.f : x) - share_of(q, fabsf(x));
+        normal_tail(x, e, q);
+        // med3 for the minimum and the maximum, which cost an instruction more each (of 17); a NaN x has made q one
+        return fmaf(-q, __builtin_amdgcn_fmed3f(fabsf(x), -kMost, kMost), __builtin_amdgcn_fmed3f(x, 0.f, __builtin_inff()));
     }
-    if constexpr (ACT == BSR_ACT_GELU_TANH) return share_of(logistic(kGeluA * x * fmaf(kGeluB, x * x, 1.f)), x);
+    if constexpr (ACT == BSR_ACT_GELU_TANH) return share_of(gelu_share(x, x * x), x);
     if constexpr (ACT == BSR_ACT_SILU) return share_of(logistic(x), x);
     return x;
 }
@@ -88,16 +101,16 @@ template <int ACT> __device__ __forceinline__ float act_slope(float x)
     if constexpr (ACT == BSR_ACT_RELU) return x > 0.f ? 1.f : x != x ? x : 0.f;
     if constexpr (ACT == BSR_ACT_GELU) {
         float e, q;
-        normal_tail(fabsf(x), e, q);
-        return (x < 0.f ? q : 1.f - q) + share_of(e, x * 0.398942280f);   // Phi(x) + x phi(x)
+        normal_tail(x, e, q);
+        return fmaf(e * 0.398942280f, finite(x), x < 0.f ? q : 1.f - q);   // x phi(x) + Phi(x)
     }
     if constexpr (ACT == BSR_ACT_GELU_TANH) {
-        const float xx = x * x, s = logistic(kGeluA * x * fmaf(kGeluB, xx, 1.f));
-        return s + share_of(s * (1.f - s), kGeluA * x * fmaf(3.f * kGeluB, xx, 1.f));
+        const float xx = x * x, s = gelu_share(x, xx);
+        return fmaf(s * (1.f - s), finite(x * fmaf(3.f * kGeluA * kGeluB, xx, kGeluA)), s);
     }
     if constexpr (ACT == BSR_ACT_SILU) {
         const float s = logistic(x);
-        return s + share_of(s * (1.f - s), x);
+        return fmaf(s * (1.f - s), finite(x), s);
     }
     return 1.f;
 }
@@ -111,58 +124,83 @@ template <typename F> __device__ __forceinline__ void with_act(int act, F f)
     else if (act == BSR_ACT_SILU) f(std::integral_constant<int, BSR_ACT_SILU>{});
 }
 
-// N consecutive elements (1, 4 or 8), at an address that is a multiple of their size up to 16 bytes.
-template <typename T, int N> __device__ __forceinline__ void load_run(float (&v)[N], const T* __restrict__ p)
-{
-    if constexpr (N == 1) {
-        v[0] = (float)*p;
-    } else {
-        constexpr int K = (int)(16 / sizeof(T)) < N ? (int)(16 / sizeof(T)) : N;
-        typedef T vec_t __attribute__((ext_vector_type(K)));
+// N consecutive elements (1, 4 or 8) as loaded, at an address that is a multiple of their size up to 16 bytes.
+template <typename T, int N> struct run_of {
+    static constexpr int K = (int)(16 / sizeof(T)) < N ? (int)(16 / sizeof(T)) : N;   // of a load
+    typedef T vec_t __attribute__((ext_vector_type(K)));
+    vec_t part[N / K];
+    __device__ __forceinline__ void load(const T* __restrict__ p, bool once = false)   // uniform
+    {
 #pragma unroll
-        for (int i = 0; i < N; i += K) {
-            const vec_t t = *reinterpret_cast<const vec_t*>(p + i);
-#pragma unroll
-            for (int e = 0; e < K; ++e) v[i + e] = (float)t[e];
+        for (int i = 0; i < N / K; ++i) {
+            const vec_t* at = reinterpret_cast<const vec_t*>(p + i * K);
+            // (the comments in the code keep the compiler from making one ordinary load of the two)
+            if (once) {
+                asm volatile("; read once");
+                part[i] = __builtin_nontemporal_load(at);
+                asm volatile("; read once");
+            } else {
+                part[i] = *at;
+            }
         }
     }
-}
-template <typename O, int N> __device__ __forceinline__ void store_run(O* __restrict__ p, const float (&v)[N])
+    __device__ __forceinline__ float operator[](int e) const { return (float)part[e / K][e % K]; }
+};
+template <typename T, int N> __device__ __forceinline__ void load_run(float (&v)[N], const T* __restrict__ p)
 {
-    if constexpr (N == 1) {
-        *p = from_f32<O>(v[0]);
-    } else {
-        constexpr int K = (int)(16 / sizeof(O)) < N ? (int)(16 / sizeof(O)) : N;
-        typedef O vec_t __attribute__((ext_vector_type(K)));
+    run_of<T, N> r;
+    r.load(p);
 #pragma unroll
-        for (int i = 0; i < N; i += K) {
-            vec_t t;
+    for (int e = 0; e < N; ++e) v[e] = r[e];
+}
+template <bool NT = false, typename O, int N> __device__ __forceinline__ void store_run(O* __restrict__ p, const float (&v)[N])
+{
+    constexpr int K = run_of<O, N>::K;
 #pragma unroll
-            for (int e = 0; e < K; ++e) t[e] = from_f32<O>(v[i + e]);
-            *reinterpret_cast<vec_t*>(p + i) = t;
-        }
+    for (int i = 0; i < N; i += K) {
+        typename run_of<O, N>::vec_t t;
+#pragma unroll
+        for (int e = 0; e < K; ++e) t[e] = from_f32<O>(v[i + e]);
+        auto* at = reinterpret_cast<typename run_of<O, N>::vec_t*>(p + i);
+        if constexpr (NT) __builtin_nontemporal_store(t, at);
+        else *at = t;
     }
 }
 
-// Sums of columns j .. j + N - 1 of row i, as they are to be stored.  T: W's type, O: Y's.
-template <typename T, typename O, int N>
-__device__ __forceinline__ void finish(const epilogue_args& ep, float (&v)[N], int i, int j, int n)
-{
-    const size_t at = (size_t)i * (size_t)n + (size_t)j;
-    if (ep.bias) {
-        float b[N];
+// What the sums of columns j .. j + N - 1 meet, T: W's type, O: Y's: the bias, and row i's part of what is read once per
+// result.  Apart from finish(), so that a kernel can have the reads under way before it has its sums.
+template <typename T, int N> struct bias_run {
+    float b[N];
+    __device__ __forceinline__ void fetch(const epilogue_args& ep, int j)
+    {
+#pragma unroll
+        for (int e = 0; e < N; ++e) b[e] = 0.f;
+        if (!ep.bias) return;
         if (std::is_same<T, float>::value || ep.bias_f32) load_run<float>(b, static_cast<const float*>(ep.bias) + j);
         else load_run<T>(b, static_cast<const T*>(ep.bias) + j);
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] += b[e];
     }
-    if (ep.z) store_run<O>(static_cast<O*>(ep.z) + at, v);
+};
+template <typename O, int N> struct result_reads {
+    run_of<O, N> z0, r;
+    __device__ __forceinline__ void fetch(const epilogue_args& ep, int i, int j, int n)
+    {
+        if (ep.through) z0.load(static_cast<const O*>(ep.through) + (size_t)i * (size_t)n + (size_t)j, ep.once);
+        if (ep.residual) r.load(static_cast<const O*>(ep.residual) + (size_t)i * (size_t)ep.residual_ld + (size_t)j, ep.once);
+    }
+};
+
+// Sums of columns j .. j + N - 1 of row i, as they are to be stored.
+template <typename T, typename O, int N>
+__device__ __forceinline__ void finish(const epilogue_args& ep, const bias_run<T, N>& bias, const result_reads<O, N>& reads, float (&v)[N], int i,
+                                       int j, int n)
+{
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] += bias.b[e];
+    if (ep.z) store_run<true>(static_cast<O*>(ep.z) + (size_t)i * (size_t)n + (size_t)j, v);
     if (ep.through) {
-        float z0[N];
-        load_run<O>(z0, static_cast<const O*>(ep.through) + at);
         with_act(ep.act, [&](auto act) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[e] *= act_slope<decltype(act)::value>(z0[e]);
+            for (int e = 0; e < N; ++e) v[e] *= act_slope<decltype(act)::value>(reads.z0[e]);
         });
     } else {
         with_act(ep.act, [&](auto act) {
@@ -171,13 +209,19 @@ __device__ __forceinline__ void finish(const epilogue_args& ep, float (&v)[N], i
         });
     }
     if (ep.residual) {
-        float r[N];
-        load_run<O>(r, static_cast<const O*>(ep.residual) + (size_t)i * (size_t)ep.residual_ld + (size_t)j);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] += r[e];
+        for (int e = 0; e < N; ++e) v[e] += reads.r[e];
     }
 }
-template <typename T, typename O, int N> __device__ __forceinline__ void finish(const no_epilogue&, float (&)[N], int, int, int) {}
+template <typename T, typename O, int N>
+__device__ __forceinline__ void finish(const epilogue_args& ep, float (&v)[N], int i, int j, int n)
+{
+    bias_run<T, N> bias;
+    result_reads<O, N> reads;
+    bias.fetch(ep, j);
+    reads.fetch(ep, i, j, n);
+    finish<T, O>(ep, bias, reads, v, i, j, n);
+}
 
 // As store4: 4 consecutive columns of row i.
 template <typename T, typename O, typename E>
@@ -187,7 +231,7 @@ __device__ __forceinline__ void finish_store4(const E& ep, O* __restrict__ Y, in
     if constexpr (E::on) {
         float v[4] = {v0, v1, v2, v3};
         finish<T, O>(ep, v, i, j, n);
-        store_run<O>(dst, v);
+        store_run(dst, v);
     } else {
         store4<O>(dst, v0, v1, v2, v3);
     }

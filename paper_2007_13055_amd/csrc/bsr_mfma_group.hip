@@ -375,17 +375,36 @@ __global__ __launch_bounds__(768) void bsr_mfma_group(const T* __restrict__ X, c
             for (int rt = 0; rt < 4; ++rt)
                 *reinterpret_cast<f32x4*>(ob + (16 * rt + fr) * kStageStride + (16 * ct + 4 * fq) * 4) = acc[ct][rt];
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    barrier();
     const int i0 = sub * kSub;
     constexpr int EPP = 16 / (int)sizeof(O);          // elements of Y per 16-byte piece
     constexpr int PPR = 64 / EPP;                     // pieces per output row of a block-row
     constexpr int RPP = 512 / PPR;                    // rows per pass of the first 512 threads
+    // what an epilogue reads is on its way a block-row ahead
+    [[maybe_unused]] bias_run<T, EPP> bias, bias_next;
+    [[maybe_unused]] result_reads<O, EPP> reads[E::on ? 64 / RPP : 1], reads_next[E::on ? 64 / RPP : 1];
+    [[maybe_unused]] auto fetch = [&](int j) {
+        if constexpr (E::on) {
+            if (j >= kG || gd[j] < 0) return;         // uniform
+            bias_next.fetch(ep, gd[j] * 64 + tid % PPR * EPP);
+#pragma unroll
+            for (int pass = 0; pass < 64 / RPP; ++pass)
+                reads_next[pass].fetch(ep, min(i0 + pass * RPP + tid % 512 / PPR, m - 1), gd[j] * 64 + tid % PPR * EPP, n);
+        }
+    };
+    fetch(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    barrier();
     if (tid >= 512) return;
     for (int j = 0; j < kG;) {                        // uniform: the wavefronts of a block-row follow each other
         const int r = gd[j];
         int shares = 1;
         while (j + shares < kG && gd[j + shares] == r) ++shares;
+        if constexpr (E::on) {
+            bias = bias_next;
+#pragma unroll
+            for (int pass = 0; pass < 64 / RPP; ++pass) reads[pass] = reads_next[pass];
+            fetch(j + shares);
+        }
         if (r >= 0) {
             unsigned char* yb = reinterpret_cast<unsigned char*>(Y + (size_t)r * 64);
 #pragma unroll
@@ -406,7 +425,7 @@ __global__ __launch_bounds__(768) void bsr_mfma_group(const T* __restrict__ X, c
                     }
                 }
                 if constexpr (E::on)
-                    if (i0 + row < m) finish<T, O>(ep, v, i0 + row, r * 64 + pc * EPP, n);
+                    if (i0 + row < m) finish<T, O>(ep, bias, reads[pass], v, i0 + row, r * 64 + pc * EPP, n);
                 u32x4 out;
                 if constexpr (std::is_same<O, float>::value) {
                     out = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});

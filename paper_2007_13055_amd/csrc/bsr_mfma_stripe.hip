@@ -217,7 +217,7 @@ __global__ __launch_bounds__(768) void bsr_mfma_stripe16(const T* __restrict__ X
                 load_run<float>(v, reinterpret_cast<const float*>(fl + (size_t)row * FS) + c0);
                 if (i >= m || c0 >= cols) continue;
                 finish<T, O>(ep, v, i, r_first * 16 + c0, n);
-                store_run<O>(Y + (size_t)i * (size_t)n + r_first * 16 + c0, v);
+                store_run(Y + (size_t)i * (size_t)n + r_first * 16 + c0, v);
             }
         }
         return;

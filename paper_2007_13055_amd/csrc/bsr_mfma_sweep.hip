@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
 #pragma unroll
                 for (int e = 0; e < EPT; ++e) v[e] += src[e];
             }
-            finish<T, O>(ep, v, i, col, n);
+            if constexpr (E::on) finish<T, O>(ep, v, i, col, n);
             O* dst = Y + (size_t)i * (size_t)n + col;
             if constexpr (EPT == 4) {
                 *reinterpret_cast<f32x4*>(dst) = f32x4{v[0], v[1], v[2], v[3]};
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
                         const T* w = data + ((size_t)b * 8 + ((col + e) & 7)) * bs_c;
                         for (int c = 0; c < bs_c; ++c) own[0] += (float)x[c] * (float)w[c];
                     }
-                    finish<T, O>(ep, own, i, col + e, n);
+                    if constexpr (E::on) finish<T, O>(ep, own, i, col + e, n);
                     dst[e] = from_f32<O>(own[0]);
                 }
             }

@@ -198,7 +198,7 @@ __global__ __launch_bounds__(kThreads) void bsr_thin16_rows(const float* __restr
             const int i = i0 + 4 * kk + j;
             float v[1] = {acc[0][j] + acc[1][j]};
             if (i < m) {
-                finish<float, float>(ep, v, i, r * 16 + lo, n);
+                if constexpr (E::on) finish<float, float>(ep, v, i, r * 16 + lo, n);
                 Y[(size_t)i * n + (size_t)r * 16 + lo] = v[0];
             }
         }

@@ -92,6 +92,23 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
     const int r = desc[0];
     const int p0 = desc[1], p1 = p0 + desc[2];
 
+    // What an epilogue reads: on its way while the blocks are multiplied.  A lane finishes pieces of 16 bytes of Y, always of
+    // the same columns.
+    constexpr int OC = BS_R * (int)sizeof(O) / 16;    // 16-byte pieces per output row of the tile
+    constexpr int RPP = 64 / OC;                      // rows one wavefront stores per pass
+    constexpr int EPP = 16 / (int)sizeof(O);          // outputs of a piece
+    [[maybe_unused]] bias_run<T, EPP> bias;
+    [[maybe_unused]] result_reads<O, EPP> reads[E::on ? MT : 1][E::on ? MM / RPP : 1];
+    if constexpr (E::on) {
+        const int j = r * BS_R + lane % OC * EPP;
+        bias.fetch(ep, j);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int pass = 0; pass < MM / RPP; ++pass)
+                reads[t][pass].fetch(ep, min(i_base + (wave * MT + t) * MM + pass * RPP + lane / OC, m - 1), j, n);
+    }
+
     typedef f32x16 acc_t;
     acc_t acc[NA][MT];
 #pragma unroll
@@ -217,33 +234,33 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
     // outputs as 16-byte pieces, i.e. full 128-byte lines for a 64-wide fp16 tile.
     constexpr int OB = BS_R * (int)sizeof(O);         // bytes of one output row of the tile
     constexpr int OS = OB + 16;                       // padded LDS stride
-    constexpr int OC = OB / 16;                       // 16-byte pieces per output row
-    constexpr int RPP = 64 / OC;                      // rows one wavefront stores per pass
     static_assert(OB % 16 == 0 && 64 % OC == 0 && (MT * MM) % RPP == 0, "output tile splits into 16-byte pieces");
     if constexpr (E::on) {
-        // The same with the sums in fp32 (rounded once, behind the epilogue), 32 rows at a time.
+        // The same with the sums in fp32 (rounded once, behind the epilogue), 16 rows at a time: no more LDS than the
+        // staging takes, so as many workgroups share a CU as without an epilogue.
         constexpr int FS = BS_R * 4 + 16;             // padded LDS stride
-        constexpr int EPP = 16 / (int)sizeof(O);      // outputs of a piece
-        unsigned char* fl = lds + (size_t)wave * MM * FS;
+        unsigned char* fl = lds + (size_t)wave * 16 * FS;
         const int frow = lane / OC, j = r * BS_R + (lane - frow * OC) * EPP;
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
+        for (int q = 0; q < 2 * MT; ++q) {
+            const int t = q / 2;
             wave_lds_fence();                         // the other lanes have read the rows before
+            if (li / 16 == q % 2)
 #pragma unroll
-            for (int u = 0; u < NA; ++u)
+                for (int u = 0; u < NA; ++u)
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<f32x4*>(fl + (size_t)li * FS + (u * 32 + 8 * g + 4 * h) * 4) =
-                        f32x4{acc[u][t][4 * g], acc[u][t][4 * g + 1], acc[u][t][4 * g + 2], acc[u][t][4 * g + 3]};
+                    for (int g = 0; g < 4; ++g)
+                        *reinterpret_cast<f32x4*>(fl + (size_t)(li % 16) * FS + (u * 32 + 8 * g + 4 * h) * 4) =
+                            f32x4{acc[u][t][4 * g], acc[u][t][4 * g + 1], acc[u][t][4 * g + 2], acc[u][t][4 * g + 3]};
             wave_lds_fence();
 #pragma unroll
-            for (int pass = 0; pass < MM / RPP; ++pass) {
-                const int row = pass * RPP + frow, i = i_base + (wave * MT + t) * MM + row;
+            for (int pass = 0; pass < 16 / RPP; ++pass) {
+                const int row = pass * RPP + frow, i = i_base + (wave * MT + t) * MM + q % 2 * 16 + row;
                 float v[EPP];
                 load_run<float>(v, reinterpret_cast<const float*>(fl + (size_t)row * FS) + (j - r * BS_R));
                 if (i >= m) continue;
-                finish<T, O>(ep, v, i, j, n);
-                store_run<O>(Y + (size_t)i * (size_t)n + j, v);
+                finish<T, O>(ep, bias, reads[t][q % 2 * (16 / RPP) + pass], v, i, j, n);
+                store_run<true>(Y + (size_t)i * (size_t)n + j, v);
             }
         }
         return;
@@ -310,7 +327,7 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
             if (blocks >= ((int64_t)1 << 31) || blocks * 256 >= ((int64_t)1 << 32)) return BSR_ERR_SHAPE;
             const size_t lds_stage = (size_t)(TM + BS_R) * (BS_C * sizeof(T) + 16);
             return with_epilogue(a, [&](auto ep) -> bsr_status {
-                const size_t lds_out = decltype(ep)::on ? (size_t)4 * 32 * (BS_R * 4 + 16) : (size_t)TM * (BS_R * sizeof(O) + 16);
+                const size_t lds_out = decltype(ep)::on ? (size_t)4 * 16 * (BS_R * 4 + 16) : (size_t)TM * (BS_R * sizeof(O) + 16);
                 const size_t lds = lds_stage > lds_out ? lds_stage : lds_out;
                 if (lds > 48 * 1024) {                // above the default dynamic-LDS limit: raise it once
                     static const hipError_t attr = hipFuncSetAttribute(

@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void bsr_wide16_f32(const float* __restri
 #pragma unroll
                 for (int w = 1; w < kWv; ++w) sum += *reinterpret_cast<const float*>(lds + w * kTile + (row * kTS + c) * 4);
                 float v[1] = {sum};
-                finish<float, float>(ep, v, i0 + row, c0 + c, n);
+                if constexpr (E::on) finish<float, float>(ep, v, i0 + row, c0 + c, n);
                 Y[(size_t)(i0 + row) * n + c0 + c] = v[0];
             }
         }
