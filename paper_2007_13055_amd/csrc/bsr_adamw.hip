@@ -4,7 +4,7 @@
 //     m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
 //     p = p (1 - lr decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
 //
-// Work split: the tensors are cut into chunks of 4096 elements, a workgroup each, listed in a table that bsr_adamw_create()
+// Work split: the tensors are cut into chunks of 4096 elements (1024 where there are few), a workgroup each, listed in a table that bsr_adamw_create()
 // uploads once; a launch takes all the chunks of one kind (type, gradient's type, master copy or not), so a model of one kind
 // is one launch however many tensors it has.  A wavefront takes 256 elements at a time, four neighbouring ones a lane.
 //
@@ -36,9 +36,10 @@ using namespace bsr_dev;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 4096;                          // elements of a workgroup
-constexpr int kShared = 256;                          // elements that share scales: one pass of a wavefront
-constexpr int kPasses = kChunk / (4 * kThreads);
+constexpr int kPass = 4 * kThreads;                   // elements that a workgroup takes at a time
+constexpr int kPasses = 4;                            // of a chunk, one where there are few chunks
+constexpr int kChunk = kPasses * kPass;
+constexpr int kShared = 256;                          // elements that share scales: a wavefront's at a time
 constexpr float kTop8 = 448.f;                        // largest e4m3 number
 
 // A tensor as the kernels see it.
@@ -62,7 +63,7 @@ static_assert(sizeof(tensor_desc) == 96, "uploaded as words");
 struct step_args {
     float lr, beta1, beta2, one1, one2, eps;          // one1 = 1 - beta1
     float rate, root;                                 // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t); where step_dev is null
-    float log1, log2;                                 // natural logarithms of the betas
+    float log1, log2, log2_beta2;                     // natural logarithms of the betas, log2 of beta2
     float grad_scale;
     uint32_t key;                                     // of the seed and the step
     uint32_t seed;
@@ -82,64 +83,48 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x)
 }
 __host__ __device__ __forceinline__ uint32_t step_key(uint32_t seed, uint64_t step) { return mix(seed + 0x9E3779B1u * (uint32_t)step); }
 
-template <int CTRL> __device__ __forceinline__ float dpp(float v)
+template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false); }
+// Largest v of the wavefront (the steps of a sum over 64 lanes).  On the bits of numbers that are not negative, whose order
+// theirs is: a maximum of floats costs another instruction for each operand, to quieten a NaN.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+    v = max(v, dpp<0xB1>(v));
+    v = max(v, dpp<0x4E>(v));
+    v = max(v, dpp<0x141>(v));
+    v = max(v, dpp<0x140>(v));
+    v = max(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x401F));
+    return max((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 32));
 }
-// Largest v of the wavefront, in every lane (the steps of a sum over 64 lanes).
-__device__ __forceinline__ float wave_max(float v)
-{
-    v = fmaxf(v, dpp<0xB1>(v));
-    v = fmaxf(v, dpp<0x4E>(v));
-    v = fmaxf(v, dpp<0x141>(v));
-    v = fmaxf(v, dpp<0x140>(v));
-    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(__builtin_bit_cast(int, v), 0x401F)));
-    const float lo = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 0));
-    const float hi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 32));
-    return fmaxf(lo, hi);
-}
+__device__ __forceinline__ uint32_t bits_of(float v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ float float_of(uint32_t v) { return __builtin_bit_cast(float, v); }
 
-// Four elements at p, `n` of them there (at least one).
-template <typename T> __device__ __forceinline__ void load4(float (&v)[4], const T* __restrict__ p, int n)
-{
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    if (n >= 4) {
-        const t4 t = *reinterpret_cast<const t4*>(p);
+// Four neighbouring elements as loaded.  FULL: all of them are there, else the first n (any n; the others as zeros).
+template <typename T> struct run4 {
+    typedef T vec_t __attribute__((ext_vector_type(4)));
+    vec_t v;
+    template <bool FULL> __device__ __forceinline__ void load(const T* p, int n)
+    {
+        if (FULL || n >= 4) {
+            v = *reinterpret_cast<const vec_t*>(p);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (float)t[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = e < n ? (float)p[e] : 0.f;
+            for (int e = 0; e < 4; ++e) v[e] = e < n ? p[e] : (T)0;
+        }
     }
-}
-template <typename T> __device__ __forceinline__ void put4(T* __restrict__ p, const T (&v)[4], int n)
-{
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    if (n >= 4) {
-        *reinterpret_cast<t4*>(p) = t4{v[0], v[1], v[2], v[3]};
-    } else {
+    template <bool FULL> __device__ __forceinline__ void store(T* p, int n) const
+    {
+        if (FULL || n >= 4) {
+            *reinterpret_cast<vec_t*>(p) = v;
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < n) p[e] = v[e];
+            for (int e = 0; e < 4; ++e)
+                if (e < n) p[e] = v[e];
+        }
     }
-}
-// Four codes, packed
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* __restrict__ p, int n)
-{
-    if (n >= 4) return *reinterpret_cast<const uint32_t*>(p);
-    uint32_t w = 0;
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-        if (e < n) w |= (uint32_t)p[e] << (8 * e);
-    return w;
-}
-__device__ __forceinline__ void put_codes(uint8_t* __restrict__ p, uint32_t w, int n)
-{
-    if (n >= 4) { *reinterpret_cast<uint32_t*>(p) = w; return; }
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-        if (e < n) p[e] = (uint8_t)(w >> (8 * e));
-}
+};
+typedef run4<uint8_t> codes4;
+__device__ __forceinline__ uint32_t word_of(const codes4& c) { return __builtin_bit_cast(uint32_t, c.v); }
+__device__ __forceinline__ codes4 codes_of(uint32_t w) { codes4 c; c.v = __builtin_bit_cast(codes4::vec_t, w); return c; }
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
@@ -152,17 +137,16 @@ __device__ __forceinline__ void decode_second(float (&v)[4], uint32_t codes, flo
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const uint32_t c = (codes >> (8 * e)) & 255u;
-        v[e] = c ? __builtin_amdgcn_exp2f(fmaf((float)c - 1.f, spacing, start)) : 0.f;
+        const float c = (float)((codes >> (8 * e)) & 255u);
+        v[e] = c > 0.f ? __builtin_amdgcn_exp2f(fmaf(c, spacing, start - spacing)) : 0.f;
     }
 }
 
 // fp32 to 16 bits, away from zero with the probability that keeps the mean; `random`: 16 random bits.
 __device__ __forceinline__ bf16_t round_at_random(bf16_t, float x, uint32_t random)
 {
-    uint32_t u = __builtin_bit_cast(uint32_t, x);
-    if ((u & 0x7F800000u) != 0x7F800000u) u += random & 0xFFFFu;      // infinities and NaN as they are
-    else if (u & 0x007FFFFFu) u |= 0x00400000u;
+    // an infinity's low bits are zeros and stay below the place; of a NaN the arithmetic has set the highest bit, which stays
+    const uint32_t u = bits_of(x) + (x == x ? random & 0xFFFFu : 0u);
     return __builtin_bit_cast(bf16_t, (uint16_t)(u >> 16));
 }
 __device__ __forceinline__ f16_t round_at_random(f16_t, float x, uint32_t random)
@@ -175,126 +159,181 @@ __device__ __forceinline__ f16_t round_at_random(f16_t, float x, uint32_t random
     return (f16_t)copysignf(ldexpf(whole, exponent - 10), x);
 }
 
-// T: the parameter's type, GT: the gradient's, BITS: of the moments.
+// What a wavefront reads for 256 elements.  T: the parameter's type, GT: the gradient's, BITS: of the moments.
+template <typename T, typename GT, int BITS, bool MASTER> struct pass_reads {
+    typedef std::conditional_t<MASTER, float, T> P;   // what the parameter is read from
+    typedef std::conditional_t<BITS == 32, float, uint8_t> S;
+    run4<P> p;
+    run4<GT> g;
+    run4<S> m, v;
+    float scale[3];
+
+    template <bool FULL> __device__ __forceinline__ void fetch(const tensor_desc& d, int64_t first, int at, int n)
+    {
+        p.template load<FULL>(static_cast<const P*>(MASTER ? (const void*)d.master : d.param) + first + at, n);
+        g.template load<FULL>(static_cast<const GT*>(d.grad) + first + at, n);
+        m.template load<FULL>(static_cast<const S*>(d.m) + first + at, n);
+        v.template load<FULL>(static_cast<const S*>(d.v) + first + at, n);
+        if constexpr (BITS == 8)
+#pragma unroll
+            for (int e = 0; e < 3; ++e) scale[e] = d.scales[3 * ((first + at) / kShared) + e];
+    }
+};
+
+struct step_now {                                     // a step's settings as a chunk uses them
+    float beta1, beta2, log2_beta2, eps, rate, root, keep;
+    float one1, one2;                                 // (1 - beta1) scale, (1 - beta2) scale^2 for gradients times scale
+    uint32_t base;
+};
+
+template <typename T, typename GT, int BITS, bool MASTER, bool FULL>
+__device__ __forceinline__ void step_pass(const tensor_desc& d, const step_now& h, const pass_reads<T, GT, BITS, MASTER>& in, int64_t first, int at, int n,
+                                          T* turned)
+{
+    float p[4], m[4], v[4];
+    run4<T> stored;
+    uint32_t random[4];
+    // m and v times their betas: with 8 bits as part of the scales (the step takes all the VALU's time that memory leaves)
+    if constexpr (BITS == 8) {
+        decode_first(m, word_of(in.m), in.scale[0] * h.beta1);
+        decode_second(v, word_of(in.v), in.scale[1] + h.log2_beta2, in.scale[2]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { m[e] = in.m.v[e] * h.beta1; v[e] = in.v.v[e] * h.beta2; }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float g = (float)in.g.v[e];
+        m[e] = fmaf(h.one1, g, m[e]);
+        v[e] = fmaf(h.one2 * g, g, v[e]);
+        const float down = fmaf(__builtin_amdgcn_sqrtf(v[e]), h.root, h.eps);
+        p[e] = fmaf(-h.rate * m[e], __builtin_amdgcn_rcpf(down), (float)in.p.v[e] * h.keep);
+        // fp32 numbers, of which the stored ones are roundings: left to itself the compiler rounds the exact sum to fp16
+        asm("" : "+v"(p[e]));
+        random[e] = mix(h.base + (uint32_t)(at + e));
+        if constexpr (MASTER || std::is_same<T, float>::value) stored.v[e] = from_f32<T>(p[e]);
+        else stored.v[e] = round_at_random(T{}, p[e], mix(random[e] + 0x3C6EF373u));
+    }
+    if (FULL || n > 0) {
+        stored.template store<FULL>(static_cast<T*>(d.param) + first + at, n);
+        if constexpr (MASTER) {
+            run4<float> w;
+            w.v = run4<float>::vec_t{p[0], p[1], p[2], p[3]};
+            w.template store<FULL>(d.master + first + at, n);
+        }
+    }
+    if (d.transposed) *reinterpret_cast<typename run4<T>::vec_t*>(turned + at) = stored.v;   // uniform
+    if constexpr (BITS == 32) {
+        if (FULL || n > 0) {
+            run4<float> w;
+            w.v = run4<float>::vec_t{m[0], m[1], m[2], m[3]};
+            w.template store<FULL>(static_cast<float*>(d.m) + first + at, n);
+            w.v = run4<float>::vec_t{v[0], v[1], v[2], v[3]};
+            w.template store<FULL>(static_cast<float*>(d.v) + first + at, n);
+        }
+    } else {
+        constexpr float kLeast = 0x1p-120f, kMost = 0x1.fffffep+127f;
+        float top = 0.f;
+        uint32_t top_v = 0, low_v = 0;                // low_v: the largest complement
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool mine = FULL || e < n;
+            top = mine ? fmaxf(top, fabsf(m[e])) : top;
+            top_v = max(top_v, mine ? bits_of(v[e]) : 0u);
+            low_v = max(low_v, mine && v[e] >= kLeast ? ~bits_of(v[e]) : 0u);
+        }
+        const float top_m = float_of(wave_max(bits_of(top))), most = float_of(wave_max(top_v)), least = float_of(~wave_max(low_v));
+        float scale[3] = {0.f, 0.f, 0x1p-12f};
+        float inverse = 0.f;
+        if (top_m >= 0x1p-100f) {                     // uniform
+            scale[0] = top_m * (1.f / kTop8);
+            inverse = kTop8 * __builtin_amdgcn_rcpf(top_m);
+        }
+        int packed = __builtin_amdgcn_cvt_pk_fp8_f32(m[0] * inverse, m[1] * inverse, 0, false);
+        packed = __builtin_amdgcn_cvt_pk_fp8_f32(m[2] * inverse, m[3] * inverse, packed, true);
+        if (!(most <= kMost)) {                       // a gradient that is not finite: so are the values of the whole group
+            scale[1] = most;
+        } else if (most >= kLeast) {                  // uniform
+            scale[1] = __builtin_amdgcn_logf(fmaxf(least, most * 0x1p-40f));         // log2
+            scale[2] = fmaxf((__builtin_amdgcn_logf(most) - scale[1]) * (1.f / 254.f), 0x1p-12f);
+        }
+        const float per = __builtin_amdgcn_rcpf(scale[2]), offset = -scale[1] * per;
+        const float step = 0x1p24f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(scale[2]) - 1.f);
+        uint32_t codes = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float below = __builtin_amdgcn_fmed3f(floorf(fmaf(__builtin_amdgcn_logf(v[e]), per, offset)), 0.f, 253.f);
+            // where v lies from one code to the next, times 2^24
+            const float up = fmaf(v[e] * step, __builtin_amdgcn_exp2f(-fmaf(below, scale[2], scale[1])), -step);
+            const uint32_t code = (uint32_t)below + 1u + ((float)(random[e] >> 8) < up ? 1u : 0u);
+            codes |= (v[e] >= kLeast ? code : 0u) << (8 * e);
+        }
+        if (FULL || n > 0) {
+            codes_of((uint32_t)packed).template store<FULL>(static_cast<uint8_t*>(d.m) + first + at, n);
+            codes_of(codes).template store<FULL>(static_cast<uint8_t*>(d.v) + first + at, n);
+        }
+        const int lane = threadIdx.x & 63;
+        if (lane < 3) d.scales[3 * ((first + at) / kShared) + lane] = lane == 0 ? scale[0] : lane == 1 ? scale[1] : scale[2];
+    }
+}
+
+// `passes`: of a chunk, 1024 elements each.
 template <typename T, typename GT, int BITS, bool MASTER>
-__global__ __launch_bounds__(kThreads) void bsr_adamw_chunks(const tensor_desc* __restrict__ tensors, const int2* __restrict__ chunks, step_args h)
+__global__ __launch_bounds__(kThreads) void bsr_adamw_chunks(const tensor_desc* __restrict__ tensors, const int2* __restrict__ chunks, int passes,
+                                                             step_args a)
 {
     __shared__ __attribute__((aligned(16))) T turned[kChunk];
     const int2 where = chunks[blockIdx.x];            // {tensor, chunk of it}
     const tensor_desc& d = tensors[where.x];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t first = (int64_t)where.y * kChunk;
-    const int there = (int)min(d.count - first, (int64_t)kChunk);   // elements of this chunk
+    const int64_t first = (int64_t)where.y * (passes * kPass);
+    const int there = (int)min(d.count - first, (int64_t)(passes * kPass));   // elements of this chunk
+    const int at = wave * kShared + lane * 4;         // of this lane in the first pass
 
-    float grad_scale = h.grad_scale, lr = h.lr, rate = h.rate, root = h.root;
-    uint32_t key = h.key;
-    if (h.grad_scale_dev) {
-        grad_scale = *h.grad_scale_dev;
-        if (grad_scale == 0.f) return;                // the step is skipped: whole grid
+    // A whole chunk's reads are all on their way before the first is used.
+    typedef pass_reads<T, GT, BITS, MASTER> reads_t;
+    reads_t in[kPasses];
+    const bool whole = there == kChunk;
+    if (whole)
+#pragma unroll
+        for (int q = 0; q < kPasses; ++q) in[q].template fetch<true>(d, first, at + q * kPass, 4);
+
+    step_now h{a.beta1, a.beta2, a.log2_beta2, a.eps, a.rate, a.root, 0.f, 0.f, 0.f, 0u};
+    float lr = a.lr, grad_scale = a.grad_scale;
+    uint32_t key = a.key;
+    if (a.grad_scale_dev) {
+        grad_scale = *a.grad_scale_dev;
+        if (grad_scale == 0.f) return;                // the step is skipped: the whole grid leaves
     }
-    if (h.lr_dev) lr = *h.lr_dev;
-    if (h.step_dev) {
-        const int64_t t = *h.step_dev;
-        root = __builtin_amdgcn_rsqf(-expm1f((float)t * h.log2));
-        rate = -1.f / expm1f((float)t * h.log1);
-        key = step_key(h.seed, (uint64_t)t);
+    h.one1 = a.one1 * grad_scale;
+    h.one2 = a.one2 * grad_scale * grad_scale;
+    if (a.lr_dev) lr = *a.lr_dev;
+    if (a.step_dev) {
+        const int64_t t = *a.step_dev;
+        h.root = __builtin_amdgcn_rsqf(-expm1f((float)t * a.log2));
+        h.rate = -1.f / expm1f((float)t * a.log1);
+        key = step_key(a.seed, (uint64_t)t);
     }
-    rate *= lr;
-    const float keep = 1.f - lr * d.decay;
-    const uint32_t base = mix(d.number + key) + (uint32_t)first;
+    h.rate *= lr;
+    h.keep = 1.f - lr * d.decay;
+    h.base = mix(d.number + key) + (uint32_t)first;
 
-    T* const param = static_cast<T*>(d.param) + first;
-    float* const master = MASTER ? d.master + first : nullptr;
-    const GT* const grad = static_cast<const GT*>(d.grad) + first;
-
+    if (whole) {
 #pragma unroll
-    for (int q = 0; q < kPasses; ++q) {
-        const int at = (q * 4 + wave) * kShared + lane * 4, n = there - at;   // n <= 0: nothing for this lane
-        if ((q * 4 + wave) * kShared >= there) break; // uniform
-        float p[4], g[4], m[4], v[4], scale[3] = {0.f, 0.f, 0.f};
-        const int64_t block = (first + (q * 4 + wave) * kShared) / kShared;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = g[e] = m[e] = v[e] = 0.f;
-        if (n > 0) {
-            load4(g, grad + at, n);
-            if constexpr (MASTER) load4(p, master + at, n);
-            else load4(p, param + at, n);
-            if constexpr (BITS == 32) {
-                load4(m, static_cast<const float*>(d.m) + first + at, n);
-                load4(v, static_cast<const float*>(d.v) + first + at, n);
+        for (int q = 0; q < kPasses; ++q) step_pass<T, GT, BITS, MASTER, true>(d, h, in[q], first, at + q * kPass, 4, turned);
+    } else {
+        for (int q = 0; q < passes; ++q) {
+            const int left = there - (q * kPass + wave * kShared);
+            if (left <= 0) break;                     // uniform
+            const int here = at + q * kPass;
+            if (left >= kShared) {
+                in[0].template fetch<true>(d, first, here, 4);
+                step_pass<T, GT, BITS, MASTER, true>(d, h, in[0], first, here, 4, turned);
+            } else {
+                in[0].template fetch<false>(d, first, here, there - here);
+                step_pass<T, GT, BITS, MASTER, false>(d, h, in[0], first, here, there - here, turned);
             }
-        }
-        if constexpr (BITS == 8) {
-#pragma unroll
-            for (int e = 0; e < 3; ++e) scale[e] = d.scales[3 * block + e];
-            if (n > 0) {
-                decode_first(m, load_codes(static_cast<const uint8_t*>(d.m) + first + at, n), scale[0]);
-                decode_second(v, load_codes(static_cast<const uint8_t*>(d.v) + first + at, n), scale[1], scale[2]);
-            }
-        }
-        T stored[4];
-        uint32_t bits[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float ge = g[e] * grad_scale;
-            m[e] = fmaf(h.one1, ge, h.beta1 * m[e]);
-            v[e] = fmaf(h.one2 * ge, ge, h.beta2 * v[e]);
-            const float down = fmaf(__builtin_amdgcn_sqrtf(v[e]), root, h.eps);
-            p[e] = fmaf(-rate * m[e], __builtin_amdgcn_rcpf(down), p[e] * keep);
-            // fp32 numbers, of which the stored ones are roundings: left to itself the compiler rounds the exact sum to fp16
-            asm("" : "+v"(p[e]));
-            bits[e] = mix(base + (uint32_t)(at + e));
-            if constexpr (MASTER || std::is_same<T, float>::value) stored[e] = from_f32<T>(p[e]);
-            else stored[e] = round_at_random(T{}, p[e], mix(bits[e] + 0x3C6EF373u));
-        }
-        if (n > 0) {
-            put4(param + at, stored, n);
-            if constexpr (MASTER) put4(master + at, p, n);
-            if constexpr (BITS == 32) {
-                put4(static_cast<float*>(d.m) + first + at, m, n);
-                put4(static_cast<float*>(d.v) + first + at, v, n);
-            }
-        }
-        if (d.transposed) {                           // uniform
-            typedef T t4 __attribute__((ext_vector_type(4)));
-            *reinterpret_cast<t4*>(turned + at) = t4{stored[0], stored[1], stored[2], stored[3]};
-        }
-        if constexpr (BITS == 8) {
-            constexpr float kLeast = 0x1p-120f;
-            float top_m = 0.f, top_v = 0.f, low_v = std::numeric_limits<float>::infinity();
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) {
-                    top_m = fmaxf(top_m, fabsf(m[e]));
-                    top_v = fmaxf(top_v, v[e]);
-                    if (v[e] >= kLeast) low_v = fminf(low_v, v[e]);
-                }
-            top_m = wave_max(top_m);
-            top_v = wave_max(top_v);
-            low_v = -wave_max(-low_v);
-            scale[0] = top_m >= 0x1p-100f ? top_m * (1.f / kTop8) : 0.f;
-            const float inverse = top_m >= 0x1p-100f ? kTop8 / top_m : 0.f;
-            int packed = __builtin_amdgcn_cvt_pk_fp8_f32(m[0] * inverse, m[1] * inverse, 0, false);
-            packed = __builtin_amdgcn_cvt_pk_fp8_f32(m[2] * inverse, m[3] * inverse, packed, true);
-            const bool some = top_v >= kLeast;
-            scale[1] = some ? __builtin_amdgcn_logf(fmaxf(low_v, top_v * 0x1p-40f)) : 0.f;      // log2
-            scale[2] = some ? fmaxf((__builtin_amdgcn_logf(top_v) - scale[1]) * (1.f / 254.f), 0x1p-12f) : 0x1p-12f;
-            const float per = 1.f / scale[2], step = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(scale[2]) - 1.f);
-            uint32_t codes = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float place = floorf((__builtin_amdgcn_logf(v[e]) - scale[1]) * per);
-                const float below = fminf(fmaxf(place, 0.f), 253.f);
-                const float up = fmaf(v[e], __builtin_amdgcn_exp2f(-fmaf(below, scale[2], scale[1])), -1.f) * step;
-                const uint32_t code = (uint32_t)below + 1u + ((float)(bits[e] >> 8) * 0x1p-24f < up ? 1u : 0u);
-                codes |= (v[e] >= kLeast ? code : 0u) << (8 * e);
-            }
-            if (n > 0) {
-                put_codes(static_cast<uint8_t*>(d.m) + first + at, (uint32_t)packed, n);
-                put_codes(static_cast<uint8_t*>(d.v) + first + at, codes, n);
-            }
-            if (lane < 3) d.scales[3 * block + lane] = lane == 0 ? scale[0] : lane == 1 ? scale[1] : scale[2];
         }
     }
     if (!d.transposed) return;                        // uniform
@@ -326,36 +365,56 @@ struct output_ptrs { void* m[kOutputs]; void* v[kOutputs]; };
 
 // The moments as values of type O.
 template <typename O, int BITS>
-__global__ __launch_bounds__(kThreads) void bsr_adamw_values(const tensor_desc* __restrict__ tensors, const int2* __restrict__ chunks, int first_tensor,
-                                                             output_ptrs outs)
+__global__ __launch_bounds__(kThreads) void bsr_adamw_values(const tensor_desc* __restrict__ tensors, const int2* __restrict__ chunks, int passes,
+                                                             int first_tensor, output_ptrs outs)
 {
+    typedef std::conditional_t<BITS == 32, float, uint8_t> S;
     const int2 where = chunks[blockIdx.x];
     const tensor_desc& d = tensors[where.x];
     O* const m_out = static_cast<O*>(outs.m[where.x - first_tensor]);
     O* const v_out = static_cast<O*>(outs.v[where.x - first_tensor]);
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t first = (int64_t)where.y * kChunk;
-    const int there = (int)min(d.count - first, (int64_t)kChunk);
+    const int64_t first = (int64_t)where.y * (passes * kPass);
+    const int there = (int)min(d.count - first, (int64_t)(passes * kPass));
+    struct reads_t {
+        run4<S> m, v;
+        float scale[3];
+    };
+    auto fetch = [&](auto full, reads_t& in, int at, int n) {
+        in.m.template load<decltype(full)::value>(static_cast<const S*>(d.m) + first + at, n);
+        in.v.template load<decltype(full)::value>(static_cast<const S*>(d.v) + first + at, n);
+        if constexpr (BITS == 8)
 #pragma unroll
-    for (int q = 0; q < kPasses; ++q) {
-        const int at = (q * 4 + wave) * kShared + lane * 4, n = there - at;
-        if (n <= 0) break;
-        const int64_t block = (first + (q * 4 + wave) * kShared) / kShared;
+            for (int e = 0; e < 3; ++e) in.scale[e] = d.scales[3 * ((first + at) / kShared) + e];
+    };
+    auto put = [&](auto full, const reads_t& in, int at, int n) {
         float m[4], v[4];
         if constexpr (BITS == 32) {
-            load4(m, static_cast<const float*>(d.m) + first + at, n);
-            load4(v, static_cast<const float*>(d.v) + first + at, n);
-        } else {
-            const float* s = d.scales + 3 * block;
-            decode_first(m, load_codes(static_cast<const uint8_t*>(d.m) + first + at, n), s[0]);
-            decode_second(v, load_codes(static_cast<const uint8_t*>(d.v) + first + at, n), s[1], s[2]);
-        }
-        O a[4], b[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { a[e] = from_f32<O>(m[e]); b[e] = from_f32<O>(v[e]); }
-        if (m_out) put4(m_out + first + at, a, n);
-        if (v_out) put4(v_out + first + at, b, n);
+            for (int e = 0; e < 4; ++e) { m[e] = in.m.v[e]; v[e] = in.v.v[e]; }
+        } else {
+            decode_first(m, word_of(in.m), in.scale[0]);
+            decode_second(v, word_of(in.v), in.scale[1], in.scale[2]);
+        }
+        run4<O> a, b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { a.v[e] = from_f32<O>(m[e]); b.v[e] = from_f32<O>(v[e]); }
+        if (m_out) a.template store<decltype(full)::value>(m_out + first + at, n);
+        if (v_out) b.template store<decltype(full)::value>(v_out + first + at, n);
+    };
+    // 256 elements a wavefront, whose scales are the same address for all lanes
+    const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kShared + ((int)threadIdx.x & 63) * 4;
+    if (there == kChunk) {
+        reads_t in[kPasses];
+#pragma unroll
+        for (int q = 0; q < kPasses; ++q) fetch(std::true_type{}, in[q], mine + q * kPass, 4);
+#pragma unroll
+        for (int q = 0; q < kPasses; ++q) put(std::true_type{}, in[q], mine + q * kPass, 4);
+        return;
+    }
+    for (int at = mine; at < there; at += kPass) {
+        reads_t in;
+        fetch(std::false_type{}, in, at, there - at);
+        put(std::false_type{}, in, at, there - at);
     }
 }
 
@@ -365,6 +424,18 @@ size_t words_of(size_t bytes) { return (bytes + 255) / 256 * 64; }
 int log2_of(int64_t v) { int l = 0; while (((int64_t)1 << l) < v) ++l; return l; }
 // Whether the step's own kernel writes the transposes of such blocks: they are whole in a chunk.
 bool turns(const bsr_adamw_tensor& t) { return kChunk % ((int64_t)t.bs_r * t.bs_c) == 0; }
+int64_t chunks_of(int64_t count, int passes) { return (count + passes * kPass - 1) / (passes * kPass); }
+// Passes of a chunk of this list: one where there would be fewer than four workgroups a CU else and every transposed block
+// fits (an fp32 layer of 0.95 M elements, 30 MB: 10.8 us a call with four, 7.5 with one).
+int passes_of(int64_t n, const bsr_adamw_tensor* tensors)
+{
+    int64_t chunks = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        chunks += chunks_of(tensors[i].count, kPasses);
+        if (tensors[i].t_param_dev && turns(tensors[i]) && kPass % ((int64_t)tensors[i].bs_r * tensors[i].bs_c) != 0) return kPasses;
+    }
+    return chunks < 1024 ? 1 : kPasses;
+}
 // Whether bsr_transpose_values() takes them: sides of whole 16-byte pieces, or blocks that fit its LDS.
 bool transposable(const bsr_adamw_tensor& t)
 {
@@ -376,7 +447,7 @@ bool transposable(const bsr_adamw_tensor& t)
 }  // namespace
 
 struct bsr_adamw {
-    int bits = 32, device = 0;
+    int bits = 32, passes = kPasses, device = 0;
     std::vector<bsr_adamw_tensor> tensors;            // the caller's, in the order of the table (by kind)
     std::vector<int64_t> number;                      // their places in the caller's list
     std::vector<int32_t> first_chunk;                 // of each, and the end
@@ -411,7 +482,7 @@ bsr_status check_sizes(int64_t n, const bsr_adamw_tensor* tensors, int32_t state
                 t.count / ((int64_t)t.bs_r * t.bs_c) >= ((int64_t)1 << 31)) return BSR_ERR_SHAPE;
             if (!turns(t) && !transposable(t)) return BSR_ERR_UNSUPPORTED;
         }
-        chunks += (t.count + kChunk - 1) / kChunk;
+        chunks += chunks_of(t.count, kPasses);
         if (chunks >= ((int64_t)1 << 24)) return BSR_ERR_SHAPE;   // a launch has below 2^32 threads
     }
     return BSR_OK;
@@ -420,9 +491,10 @@ bsr_status check_sizes(int64_t n, const bsr_adamw_tensor* tensors, int32_t state
 size_t workspace_words(int64_t n, const bsr_adamw_tensor* tensors)
 {
     size_t words = words_of((size_t)n * sizeof(tensor_desc)), chunks = 0;
+    const int passes = passes_of(n, tensors);
     for (int64_t i = 0; i < n; ++i) {
         const bsr_adamw_tensor& t = tensors[i];
-        chunks += (size_t)((t.count + kChunk - 1) / kChunk);
+        chunks += (size_t)chunks_of(t.count, passes);
         if (t.t_param_dev) words += words_of((size_t)(t.count / ((int64_t)t.bs_r * t.bs_c)) * 4);
     }
     return std::max<size_t>(words + words_of(chunks * sizeof(int2)), 64);
@@ -480,6 +552,7 @@ bsr_status create_adamw(bsr_adamw** out, int64_t n, const bsr_adamw_tensor* tens
     if (!apart(n, tensors, state_bits, {workspace_dev, words * 4})) return BSR_ERR_OVERLAP;
     std::unique_ptr<bsr_adamw> opt(new bsr_adamw);
     opt->bits = state_bits;
+    opt->passes = passes_of(n, tensors);
     std::vector<int64_t> order((size_t)n);
     for (int64_t i = 0; i < n; ++i) order[(size_t)i] = i;
     std::stable_sort(order.begin(), order.end(), [&](int64_t a, int64_t b) { return kind_of(tensors[a]) < kind_of(tensors[b]); });
@@ -487,12 +560,12 @@ bsr_status create_adamw(bsr_adamw** out, int64_t n, const bsr_adamw_tensor* tens
     int32_t* const dev = static_cast<int32_t*>(workspace_dev);
     const size_t chunks_at = words_of((size_t)n * sizeof(tensor_desc));
     size_t chunk = 0, total = 0;
-    for (int64_t i = 0; i < n; ++i) total += (size_t)((tensors[i].count + kChunk - 1) / kChunk);
+    for (int64_t i = 0; i < n; ++i) total += (size_t)chunks_of(tensors[i].count, opt->passes);
     size_t at = chunks_at + words_of(total * sizeof(int2));
     for (int64_t s = 0; s < n; ++s) {
         const bsr_adamw_tensor& t = tensors[order[(size_t)s]];
         opt->first_chunk.push_back((int32_t)chunk);
-        const int32_t mine = (int32_t)((t.count + kChunk - 1) / kChunk);
+        const int32_t mine = (int32_t)chunks_of(t.count, opt->passes);
         for (int32_t c = 0; c < mine; ++c, ++chunk) {
             opt->host[chunks_at + 2 * chunk] = (int32_t)s;
             opt->host[chunks_at + 2 * chunk + 1] = c;
@@ -547,7 +620,7 @@ template <typename T, typename GT, bool MASTER>
 bsr_status launch_kind(const bsr_adamw* opt, const bsr_adamw::launch_t& l, const step_args& h, hipStream_t stream)
 {
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)l.count), dim3(kThreads), 0, stream, opt->descs, opt->chunks + l.first, h);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)l.count), dim3(kThreads), 0, stream, opt->descs, opt->chunks + l.first, opt->passes, h);
         return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
     };
     return opt->bits == 8 ? go(bsr_adamw_chunks<T, GT, 8, MASTER>) : go(bsr_adamw_chunks<T, GT, 32, MASTER>);
@@ -627,6 +700,7 @@ bsr_status bsr_adamw_step(const bsr_adamw* opt, const bsr_adamw_hyper* hyper, vo
     h.eps = (float)y.eps;
     h.log1 = (float)std::log(y.beta1);
     h.log2 = (float)std::log(y.beta2);
+    h.log2_beta2 = (float)std::log2(y.beta2);
     if (!y.step_dev) {
         h.rate = (float)(1.0 / (1.0 - std::pow(y.beta1, (double)y.step)));
         h.root = (float)(1.0 / std::sqrt(1.0 - std::pow(y.beta2, (double)y.step)));
@@ -673,7 +747,7 @@ bsr_status bsr_adamw_moments(const bsr_adamw* opt, bsr_dtype dtype, void* const*
             outs.v[i - s] = exp_avg_sq_out[opt->number[i]];
         }
         auto go = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), 0, stream, opt->descs, opt->chunks + first, (int)s, outs);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), 0, stream, opt->descs, opt->chunks + first, opt->passes, (int)s, outs);
             return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
         };
         const bool eight = opt->bits == 8;
