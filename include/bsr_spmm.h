@@ -202,7 +202,7 @@ bsr_status bsr_spmm_epilogue(const bsr_matrix* W, int64_t m, const void* X_dev, 
  *   DB_dev         DEVICE, n floats, or NULL (not both NULL); m == 0: zeros
  *   workspace_dev  DEVICE, bsr_epilogue_backward_workspace_size() bytes (0: none, it may be NULL), overwritten; read only
  *                  where DB_dev is given.  Calls that may run at the same time, replayed graphs among them, need one each.
- * Asynchronous on hip_stream.  Errors: NULL, SHAPE (m or n negative, m >= 2^30, n >= 2^31 - 512, or m*n >= 2^40), DTYPE,
+ * Asynchronous on hip_stream.  Errors: NULL, SHAPE (m or n negative, m >= 2^30, n >= 2^28, or m*n >= 2^40), DTYPE,
  * ALIGN (a pointer not 16-byte aligned), WORKSPACE, OVERLAP, HIP.
  */
 bsr_status bsr_epilogue_backward_workspace_size(int64_t m, int64_t n, size_t* bytes);
@@ -403,7 +403,7 @@ typedef struct {
 typedef struct {
     double lr, beta1, beta2, eps;       /* 0 <= beta < 1, lr and eps >= 0 */
     int64_t step;                       /* t >= 1 */
-    float grad_scale;                   /* 1: gradients as they are; 0: the step is skipped */
+    float grad_scale;                   /* 1: gradients as they are; 0: the step is skipped (else 2^-40 to 2^40 in size) */
     uint32_t seed;
     const float* lr_dev;
     const int64_t* step_dev;

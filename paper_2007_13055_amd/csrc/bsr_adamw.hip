@@ -266,7 +266,7 @@ __device__ __forceinline__ void step_pass(const tensor_desc& d, const step_now& 
             // where v lies from one code to the next, times 2^24
             const float up = fmaf(v[e] * step, __builtin_amdgcn_exp2f(-fmaf(below, scale[2], scale[1])), -step);
             const uint32_t code = (uint32_t)below + 1u + ((float)(random[e] >> 8) < up ? 1u : 0u);
-            codes |= (v[e] >= kLeast ? code : 0u) << (8 * e);
+            codes |= (v[e] < kLeast ? 0u : code) << (8 * e);   // (a NaN has a code, of which its scales make one again)
         }
         if (FULL || n > 0) {
             codes_of((uint32_t)packed).template store<FULL>(static_cast<uint8_t*>(d.m) + first + at, n);
@@ -634,6 +634,20 @@ bsr_status launch_type(const bsr_adamw* opt, const bsr_adamw::launch_t& l, const
     return f32_grad ? launch_kind<T, float, false>(opt, l, h, stream) : launch_kind<T, T, false>(opt, l, h, stream);
 }
 
+// The tables are there for what `stream` is given next.  What is recorded into a graph cannot wait for an upload outside of
+// it, so a capture right behind bsr_adamw_create() waits here, on the host.
+void ready_for(const bsr_adamw* opt, hipStream_t stream)
+{
+    if (opt->uploaded && is_capturing(stream) && !upload_landed(opt->uploaded, opt->landed)) {
+        hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;      // in the default mode the wait would end the capture
+        const bool swapped = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
+        if (hipEventSynchronize(opt->uploaded) == hipSuccess) opt->landed.store(true, std::memory_order_release);
+        if (swapped) (void)hipThreadExchangeStreamCaptureMode(&mode);
+        (void)hipGetLastError();
+    }
+    order_after_upload(stream, opt->uploaded, opt->landed);
+}
+
 bool on_its_device(const bsr_adamw* opt)
 {
     int dev = -1;
@@ -690,7 +704,7 @@ bsr_status bsr_adamw_step(const bsr_adamw* opt, const bsr_adamw_hyper* hyper, vo
     if (reinterpret_cast<uintptr_t>(y.step_dev) & 7u) return BSR_ERR_ALIGN;
     if (!on_its_device(opt)) return BSR_ERR_DEVICE;
     hipStream_t stream = (hipStream_t)hip_stream;
-    order_after_upload(stream, opt->uploaded, opt->landed);
+    ready_for(opt, stream);
     step_args h{};
     h.lr = (float)y.lr;
     h.beta1 = (float)y.beta1;
@@ -736,7 +750,7 @@ bsr_status bsr_adamw_moments(const bsr_adamw* opt, bsr_dtype dtype, void* const*
         if (!aligned16(exp_avg_out[i]) || !aligned16(exp_avg_sq_out[i])) return BSR_ERR_ALIGN;
     if (!on_its_device(opt)) return BSR_ERR_DEVICE;
     hipStream_t stream = (hipStream_t)hip_stream;
-    order_after_upload(stream, opt->uploaded, opt->landed);
+    ready_for(opt, stream);
     for (size_t s = 0; s < n; s += kOutputs) {
         const size_t end = std::min(n, s + kOutputs);
         const int32_t first = opt->first_chunk[s], count = opt->first_chunk[end] - first;

@@ -180,7 +180,7 @@ bsr_status launch_types(const backward_shape& s, int64_t m, int64_t n, bsr_act a
     return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
 }
 
-bool sizes_fit(int64_t m, int64_t n) { return m >= 0 && n >= 0 && m < ((int64_t)1 << 30) && n < ((int64_t)1 << 31) - 512; }
+bool sizes_fit(int64_t m, int64_t n) { return m >= 0 && n >= 0 && m < ((int64_t)1 << 30) && n < ((int64_t)1 << 28); }
 
 }  // namespace
 

@@ -301,16 +301,17 @@ int act_code(PyObject* name)
     return -1;
 }
 
-// Whether the kernels of this call may touch the tensor: they run on the current device's current stream.
-bool here(const at::Tensor& t, const char* what)
+// Whether the kernels of this call may touch the tensor: they run on the current device's current stream, X's or G's, which
+// is checked against the current device first (`device`: its number, else -1).
+bool here(const at::Tensor& t, const char* what, int device = -1)
 {
-    if (t.is_cuda() && t.get_device() == c10::hip::current_device()) return true;
+    if (t.is_cuda() && t.get_device() == (device < 0 ? (int)c10::hip::current_device() : device)) return true;
     PyErr_Format(PyExc_ValueError, "%s must be on the current GPU", what);
     return false;
 }
 
-// An optional contiguous (rows, cols) tensor of type `code` on the current GPU; false with an error set.
-bool matrix_of(PyObject* obj, const char* what, int64_t rows, int64_t cols, int code, const at::Tensor** out)
+// An optional contiguous (rows, cols) tensor of type `code` on `device`; false with an error set.
+bool matrix_of(PyObject* obj, const char* what, int64_t rows, int64_t cols, int code, int device, const at::Tensor** out)
 {
     *out = nullptr;
     if (obj == Py_None) return true;
@@ -321,7 +322,7 @@ bool matrix_of(PyObject* obj, const char* what, int64_t rows, int64_t cols, int 
         return false;
     }
     *out = t;
-    return here(*t, what);
+    return here(*t, what, device);
 }
 
 // spmm_epilogue(W, core, X, Y or None, y_dtype or None, bias or None, act or None, residual or None, through or None,
@@ -338,6 +339,7 @@ PyObject* spmm_epilogue(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     if (x_code < 0) return nullptr;
     if (x_code != c->dtype || !X->is_contiguous()) return value_error("X must be contiguous and of W's dtype");
     if (!here(*X, "X")) return nullptr;
+    const int device = (int)X->get_device();
     const int64_t m = X->size(0);
     const int y_code = name_code(a[4], c->dtype);
     if (y_code < 0) return nullptr;
@@ -351,7 +353,7 @@ PyObject* spmm_epilogue(PyObject*, PyObject* const* a, Py_ssize_t nargs)
         if (code < 0) return nullptr;
         if (bias->dim() != 1 || bias->size(0) != c->n || !bias->is_contiguous() || (code != c->dtype && code != BSR_F32))
             return value_error("bias must be a contiguous (n,) tensor of W's dtype or fp32");
-        if (!here(*bias, "bias")) return nullptr;
+        if (!here(*bias, "bias", device)) return nullptr;
         ep.bias_dev = bias->data_ptr();
         ep.bias_dtype = (bsr_dtype)code;
     }
@@ -360,12 +362,12 @@ PyObject* spmm_epilogue(PyObject*, PyObject* const* a, Py_ssize_t nargs)
         if (!dims2(*residual, m, c->n) || residual->scalar_type() != kTypes[y_code] ||
             (c->n > 1 && residual->stride(1) != 1) || (m > 1 && residual->stride(0) < c->n))
             return value_error("residual must be an (m, n) tensor of the result's type, its rows contiguous");
-        if (!here(*residual, "residual")) return nullptr;
+        if (!here(*residual, "residual", device)) return nullptr;
         ep.residual_dev = residual->data_ptr();
         ep.residual_ld = m > 1 ? residual->stride(0) : 0;
     }
-    if (!matrix_of(a[8], "through", m, c->n, y_code, &through) || !matrix_of(a[9], "Z", m, c->n, y_code, &Z) ||
-        !matrix_of(a[3], "Y", m, c->n, y_code, &Y)) return nullptr;
+    if (!matrix_of(a[8], "through", m, c->n, y_code, device, &through) || !matrix_of(a[9], "Z", m, c->n, y_code, device, &Z) ||
+        !matrix_of(a[3], "Y", m, c->n, y_code, device, &Y)) return nullptr;
     if (through) ep.through_dev = through->data_ptr();
     const int keep_z = PyObject_IsTrue(a[10]);
     if (keep_z < 0 || !ensure_scratch(a[0], c, m)) return nullptr;
@@ -413,20 +415,21 @@ PyObject* epilogue_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     if (g_code < 0) return nullptr;
     if (G->dim() != 2 || !G->is_contiguous()) return value_error("G must be a contiguous (m, n) tensor");
     if (!here(*G, "G")) return nullptr;
+    const int device = (int)G->get_device();
     const int64_t m = G->size(0), n = G->size(1);
     const int act = act_code(a[2]);
     if (act < 0) return nullptr;
-    if (!matrix_of(a[1], "Z", m, n, g_code, &Z)) return nullptr;
+    if (!matrix_of(a[1], "Z", m, n, g_code, device, &Z)) return nullptr;
     if (!Z && act != BSR_ACT_NONE) return value_error("Z must be given unless act is none");
     const int dz_code = name_code(a[4], g_code);
     if (dz_code < 0) return nullptr;
     if (dz_code != g_code && g_code != BSR_F32) return value_error("dz_dtype must be G's type unless that is fp32");
-    if (!matrix_of(a[3], "DZ", m, n, dz_code, &DZ)) return nullptr;
+    if (!matrix_of(a[3], "DZ", m, n, dz_code, device, &DZ)) return nullptr;
     if (a[5] != Py_None) {
         if (!tensor_of(a[5], "DB", &DB)) return nullptr;
         if (DB->dim() != 1 || DB->size(0) != n || !DB->is_contiguous() || DB->scalar_type() != at::kFloat)
             return value_error("DB must be a contiguous (n,) fp32 tensor");
-        if (!here(*DB, "DB")) return nullptr;
+        if (!here(*DB, "DB", device)) return nullptr;
     }
     const int need_dz = PyObject_IsTrue(a[6]), need_db = PyObject_IsTrue(a[7]);
     if (need_dz < 0 || need_db < 0) return nullptr;

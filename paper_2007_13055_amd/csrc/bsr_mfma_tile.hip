@@ -92,23 +92,6 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
     const int r = desc[0];
     const int p0 = desc[1], p1 = p0 + desc[2];
 
-    // What an epilogue reads: on its way while the blocks are multiplied.  A lane finishes pieces of 16 bytes of Y, always of
-    // the same columns.
-    constexpr int OC = BS_R * (int)sizeof(O) / 16;    // 16-byte pieces per output row of the tile
-    constexpr int RPP = 64 / OC;                      // rows one wavefront stores per pass
-    constexpr int EPP = 16 / (int)sizeof(O);          // outputs of a piece
-    [[maybe_unused]] bias_run<T, EPP> bias;
-    [[maybe_unused]] result_reads<O, EPP> reads[E::on ? MT : 1][E::on ? MM / RPP : 1];
-    if constexpr (E::on) {
-        const int j = r * BS_R + lane % OC * EPP;
-        bias.fetch(ep, j);
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int pass = 0; pass < MM / RPP; ++pass)
-                reads[t][pass].fetch(ep, min(i_base + (wave * MT + t) * MM + pass * RPP + lane / OC, m - 1), j, n);
-    }
-
     typedef f32x16 acc_t;
     acc_t acc[NA][MT];
 #pragma unroll
@@ -234,16 +217,32 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
     // outputs as 16-byte pieces, i.e. full 128-byte lines for a 64-wide fp16 tile.
     constexpr int OB = BS_R * (int)sizeof(O);         // bytes of one output row of the tile
     constexpr int OS = OB + 16;                       // padded LDS stride
+    constexpr int OC = OB / 16;                       // 16-byte pieces per output row
+    constexpr int RPP = 64 / OC;                      // rows one wavefront stores per pass
     static_assert(OB % 16 == 0 && 64 % OC == 0 && (MT * MM) % RPP == 0, "output tile splits into 16-byte pieces");
     if constexpr (E::on) {
         // The same with the sums in fp32 (rounded once, behind the epilogue), 16 rows at a time: no more LDS than the
         // staging takes, so as many workgroups share a CU as without an epilogue.
         constexpr int FS = BS_R * 4 + 16;             // padded LDS stride
+        constexpr int EPP = 16 / (int)sizeof(O);      // outputs of a piece
         unsigned char* fl = lds + (size_t)wave * 16 * FS;
+        // A lane finishes pieces of the same columns; what it reads for them is on its way 16 rows ahead.  (From before the
+        // blocks are multiplied: fewer wavefronts for want of registers, 3200 x (1024, 8192) bf16 32x32 with all parts 46.0
+        // us in place of 42.3; for all rows, 8192^3 f16 64x64 154 in place of 150.)
         const int frow = lane / OC, j = r * BS_R + (lane - frow * OC) * EPP;
+        bias_run<T, EPP> bias;
+        result_reads<O, EPP> reads[2][16 / RPP];
+        auto fetch_reads = [&](int q) {
+#pragma unroll
+            for (int pass = 0; pass < 16 / RPP; ++pass)
+                reads[q % 2][pass].fetch(ep, min(i_base + wave * MT * MM + q * 16 + pass * RPP + frow, m - 1), j, n);
+        };
+        bias.fetch(ep, j);
+        fetch_reads(0);
 #pragma unroll
         for (int q = 0; q < 2 * MT; ++q) {
             const int t = q / 2;
+            if (q + 1 < 2 * MT) fetch_reads(q + 1);
             wave_lds_fence();                         // the other lanes have read the rows before
             if (li / 16 == q % 2)
 #pragma unroll
@@ -259,7 +258,7 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
                 float v[EPP];
                 load_run<float>(v, reinterpret_cast<const float*>(fl + (size_t)row * FS) + (j - r * BS_R));
                 if (i >= m) continue;
-                finish<T, O>(ep, bias, reads[t][q % 2 * (16 / RPP) + pass], v, i, j, n);
+                finish<T, O>(ep, bias, reads[q % 2][pass], v, i, j, n);
                 store_run<true>(Y + (size_t)i * (size_t)n + j, v);
             }
         }
@@ -326,7 +325,7 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
             const int64_t blocks = (int64_t)((n_tiles + kXcds - 1) / kXcds) * kXcds * (R - first);
             if (blocks >= ((int64_t)1 << 31) || blocks * 256 >= ((int64_t)1 << 32)) return BSR_ERR_SHAPE;
             const size_t lds_stage = (size_t)(TM + BS_R) * (BS_C * sizeof(T) + 16);
-            return with_epilogue(a, [&](auto ep) -> bsr_status {
+            auto launch = [&](auto ep) -> bsr_status {
                 const size_t lds_out = decltype(ep)::on ? (size_t)4 * 16 * (BS_R * 4 + 16) : (size_t)TM * (BS_R * sizeof(O) + 16);
                 const size_t lds = lds_stage > lds_out ? lds_stage : lds_out;
                 if (lds > 48 * 1024) {                // above the default dynamic-LDS limit: raise it once
@@ -339,9 +338,13 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
                                    (const T*)a.X, (const T*)W->data, W->indices, W->row_desc, (O*)a.Y, m, k, n, R, n_tiles,
                                    groups, ep);
                 return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
-            });
+            };
+            if constexpr (D > 2) return launch(no_epilogue{});
+            else return with_epilogue(a, launch);
         };
-        const int depth = tune.a > 0 ? tune.a : 2;
+        // (three and four blocks in flight are candidates of bsr_tune() alone: with an epilogue two take their place, for
+        // the same sums -- each further one is 18 more kernels of this file, which takes longest to compile)
+        const int depth = std::min(tune.a > 0 ? tune.a : 2, a.epilogue ? 2 : 4);
         if (tune.mt == 1) {
             if (depth == 1) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
             if (depth == 2) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});

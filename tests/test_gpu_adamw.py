@@ -366,3 +366,68 @@ def test_training_steps_of_two_layers(dtype, bits):
             assert np.all(np.abs(new - want) <= 2.0 ** -22 * np.abs(before[i][0]) + 2.0 ** -19 * step + 2.0 ** -22 * H["lr"] * 12), (t, i)
         for p, W, WT, perm, _ in layers:
             assert torch.equal(WT.block_data, W.block_data[torch.from_numpy(perm).long().cuda()].transpose(1, 2).contiguous())
+
+
+def test_captured_right_behind_the_handle():
+    """No eager step before: the tables' upload is waited for during the capture."""
+    import torch
+    import paper_2007_13055_amd as lib
+    params, grads = _tensors([300000, 5, 9000], "bf16", "bf16", 12)
+    want, _ = _tensors([300000, 5, 9000], "bf16", "bf16", 12)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2000000)                                        # the upload comes behind it
+        opt = lib.bsr_adamw_create(params, grads, master=True)
+    with torch.cuda.graph(graph):
+        lib.bsr_adamw_step(opt, 1, **H)
+    graph.replay()
+    torch.cuda.synchronize()
+    one = lib.bsr_adamw_create(want, grads, master=True)
+    lib.bsr_adamw_step(one, 1, **H)
+    for a, b in zip(opt.params + opt.exp_avg + opt.master, one.params + one.exp_avg + one.master):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_that_are_not_finite(bits):
+    """They reach their own element and, held in 8 bits, the moments of its 256; nothing else."""
+    import torch
+    import paper_2007_13055_amd as lib
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        params, grads = _tensors([1000], "f32", "f32", 13)
+        clean, _ = _tensors([1000], "f32", "f32", 13)
+        spoilt = grads[0].clone()
+        spoilt[300] = bad
+        opt = lib.bsr_adamw_create(params, [spoilt], state_bits=bits)
+        one = lib.bsr_adamw_create(clean, grads, state_bits=bits)
+        for o in (opt, one):
+            lib.bsr_adamw_step(o, 1, **H)
+        assert not bool(params[0][300].isfinite())
+        rest = torch.arange(1000, device="cuda") != 300
+        assert torch.equal(params[0][rest], clean[0][rest])
+        m, v = lib.bsr_adamw_moments(opt)[0]
+        m1, v1 = lib.bsr_adamw_moments(one)[0]
+        group = (torch.arange(1000, device="cuda") // 256 == 1) if bits == 8 else ~rest
+        assert torch.equal(m[~group], m1[~group]) and torch.equal(v[~group], v1[~group])
+        assert not bool(v[group].isfinite().any()) and not bool(m[300].isfinite())
+
+
+def test_all_of_a_groups_gradients_are_zero():
+    """Groups without a positive value, and ones with a single one: zeros stay zeros, and the one keeps its value."""
+    import torch
+    import paper_2007_13055_amd as lib
+    g = torch.zeros(1024, device="cuda")
+    g[300], g[600], g[601] = 2.0, 1e-12, 3e4
+    p = torch.ones(1024, device="cuda")
+    opt = lib.bsr_adamw_create([p], [g], state_bits=8, weight_decay=0.0)
+    for t in (1, 2, 3):
+        lib.bsr_adamw_step(opt, t, **H)
+    m, v = lib.bsr_adamw_moments(opt)[0]
+    assert bool((v[g == 0] == 0).all()) and bool((m[g == 0] == 0).all()) and bool((p[g == 0] == 1).all())
+    want = 1 - 0.95 ** 3
+    assert abs(float(v[300]) / (want * 4) - 1) < 3 * 2.0 ** -11           # spacing 2^-12 in log2, up or down a few times
+    # 3e4 squared is the largest of its group; 1e-12 squared is below 2^-40 of it and is held as that, so its update shrinks
+    assert abs(float(v[601]) / (want * 9e8) - 1) < 0.4 and float(v[600]) > 0 and abs(float(p[600]) - 1) < 1e-3
+    assert abs(float(p[601]) - (1 - 3 * H["lr"])) < 1e-4
