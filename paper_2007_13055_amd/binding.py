@@ -1,7 +1,8 @@
 """Binding for libbsr_spmm.so: same names as the C entry points, marshalling only.
 
-The products (bsr_spmm, bsr_spmm_ex, bsr_spmm_static, bsr_spmm_epilogue, bsr_epilogue_backward, bsr_sddmm) go through the native module _binding, whose calls cost
-about what the launch itself does; everything called once per matrix goes through ctypes."""
+What is called once a product or a step (bsr_spmm, bsr_spmm_ex, bsr_spmm_static, bsr_spmm_epilogue, bsr_epilogue_backward,
+bsr_sddmm, bsr_adamw_step, bsr_adamw_moments) goes through the native module _binding, whose calls cost about what the launch
+itself does; everything called once per matrix goes through ctypes."""
 from __future__ import annotations
 
 import ctypes
@@ -124,7 +125,7 @@ def _native_module():
     _binding.bind(*(ctypes.cast(f, ctypes.c_void_p).value
                     for f in (lib.bsr_spmm_ex, lib.bsr_spmm_static, lib.bsr_sddmm_ws, lib.bsr_scratch_size,
                               lib.bsr_sddmm_workspace_size, lib.bsr_spmm_epilogue, lib.bsr_epilogue_backward,
-                              lib.bsr_epilogue_backward_workspace_size)), BsrError)
+                              lib.bsr_epilogue_backward_workspace_size, lib.bsr_adamw_step, lib.bsr_adamw_moments)), BsrError)
     _native = _binding
     return _native
 
@@ -388,9 +389,11 @@ class BsrAdamW:
         self.state_bits, self.params, self.grads, self.master = state_bits, params, grads, master
         self.exp_avg, self.exp_avg_sq, self.scales = exp_avg, exp_avg_sq, scales
         self.handle, self.device, self._keep = None, None, []
+        self._address, self._index, self._counts = 0, 0, tuple(int(p.numel()) for p in params)   # what the calls read
 
     def close(self):
         if self.handle:
+            self._address = 0
             load_library().bsr_adamw_destroy(self.handle)
             self.handle = None
 
@@ -421,6 +424,7 @@ def bsr_adamw_create(params, grads, *, weight_decay=0.0, state_bits=32, moments=
     date, perm from bsr_transpose_pattern."""
     import torch
     lib = load_library()
+    _native_module()
     params, grads = list(params), list(grads)
     n = len(params)
     if len(grads) != n or (moments is not None and len(moments) != n) or (transposed is not None and len(transposed) != n) or \
@@ -483,14 +487,8 @@ def bsr_adamw_create(params, grads, *, weight_decay=0.0, state_bits=32, moments=
                               torch.cuda.current_stream().cuda_stream)
     if st != 0:
         raise BsrError(st, "bsr_adamw_create")
-    opt.handle = handle
+    opt.handle, opt._address, opt._index = handle, handle.value, device.index
     return opt
-
-
-def _device_scalar(t, what, dtype, device):
-    if t.dtype != dtype or t.numel() != 1 or t.device != device:
-        raise ValueError(f"{what} on the GPU must be one {dtype} on {device}")
-    return t.data_ptr()
 
 
 def bsr_adamw_step(opt: BsrAdamW, step, *, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, grad_scale=1.0, seed=0):
@@ -498,44 +496,15 @@ def bsr_adamw_step(opt: BsrAdamW, step, *, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
 
     step counts from 1.  step, lr and grad_scale may be GPU tensors of one int64, fp32 and fp32, which a step captured into a
     graph reads at every replay; a grad_scale of 0 skips the step.  seed: of the random roundings."""
-    import torch
-    h = AdamWHyper(beta1=betas[0], beta2=betas[1], eps=eps, seed=int(seed) & 0xFFFFFFFF)
-    if isinstance(step, torch.Tensor):
-        h.step_dev = _device_scalar(step, "step", torch.int64, opt.device)
-    else:
-        h.step = int(step)
-    if isinstance(lr, torch.Tensor):
-        h.lr_dev = _device_scalar(lr, "lr", torch.float32, opt.device)
-    else:
-        h.lr = lr
-    if isinstance(grad_scale, torch.Tensor):
-        h.grad_scale_dev = _device_scalar(grad_scale, "grad_scale", torch.float32, opt.device)
-    else:
-        h.grad_scale = grad_scale
-    st = load_library().bsr_adamw_step(opt.handle, ctypes.byref(h), torch.cuda.current_stream().cuda_stream)
-    if st != 0:
-        raise BsrError(st, "bsr_adamw_step")
+    _native.adamw_step(opt._address, opt._index, step, lr, betas[0], betas[1], eps, grad_scale, seed)
 
 
 def bsr_adamw_moments(opt: BsrAdamW, dtype="f32", out=None):
     """[(m, v), ...]: the moments as values of `dtype` ("f32" | "f16" | "bf16"), whatever they are held in; out: such a list to
-    fill (of one type, each entry of it a tensor, a pair's tensors of a parameter's number of elements)."""
-    import torch
+    fill (of one type, each entry a pair of tensors of a parameter's number of elements)."""
     if out is None:
+        import torch
         new = lambda p: torch.empty(p.numel(), dtype=_torch_dtype(dtype), device=opt.device)  # noqa: E731
         out = [(new(p), new(p)) for p in opt.params]
-    else:
-        out = [tuple(pair) for pair in out]
-        if len(out) != len(opt.params) or any(len(pair) != 2 for pair in out):
-            raise ValueError("out: a pair of tensors a parameter")
-        if out:
-            dtype = _dtype_name(out[0][0])
-        for i, (pair, p) in enumerate(zip(out, opt.params)):
-            for t in pair:
-                _adamw_buffer(t, f"out[{i}]", (_torch_dtype(dtype),), p.numel(), opt.device)
-    n = len(out)
-    ms, vs = ((ctypes.c_void_p * max(n, 1))(*(pair[k].data_ptr() for pair in out)) for k in (0, 1))
-    st = load_library().bsr_adamw_moments(opt.handle, _DTYPE_CODE[dtype], ms, vs, torch.cuda.current_stream().cuda_stream)
-    if st != 0:
-        raise BsrError(st, "bsr_adamw_moments")
+    _native.adamw_moments(opt._address, opt._index, opt._counts, out if isinstance(out, list) else list(out))
     return out

@@ -13,6 +13,8 @@
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 
+#include <vector>
+
 #include "bsr_spmm.h"
 
 namespace {
@@ -25,6 +27,8 @@ bsr_status (*g_scratch_size)(const bsr_matrix*, int64_t, size_t*) = nullptr;
 bsr_status (*g_spmm_epilogue)(const bsr_matrix*, int64_t, const void*, void*, bsr_dtype, const bsr_epilogue*, void*) = nullptr;
 bsr_status (*g_backward)(int64_t, int64_t, bsr_act, bsr_dtype, const void*, const void*, bsr_dtype, void*, float*, void*, size_t, void*) = nullptr;
 bsr_status (*g_backward_workspace)(int64_t, int64_t, size_t*) = nullptr;
+bsr_status (*g_adamw_step)(const bsr_adamw*, const bsr_adamw_hyper*, void*) = nullptr;
+bsr_status (*g_adamw_moments)(const bsr_adamw*, bsr_dtype, void* const*, void* const*, void*) = nullptr;
 PyObject* g_error = nullptr;                          // BsrError(status, where)
 
 // What the calls need to know of a matrix; owned by the Python object that owns the handle.
@@ -476,13 +480,114 @@ PyObject* epilogue_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
+// A setting of a step: a number, or one element of `type` on `device`, whose address is taken.  False with an error set.
+template <typename N, typename P>
+bool setting(PyObject* obj, const char* what, at::ScalarType type, int device, N (*number)(PyObject*), N* value, const P** at_device)
+{
+    if (!THPVariable_Check(obj)) {
+        *value = number(obj);
+        return !PyErr_Occurred();
+    }
+    const at::Tensor& t = THPVariable_Unpack(obj);
+    if (t.scalar_type() != type || t.numel() != 1 || !t.is_cuda() || t.get_device() != device) {
+        PyErr_Format(PyExc_ValueError, "%s on the GPU must be one %s of the handle's device", what, type == at::kLong ? "int64" : "fp32");
+        return false;
+    }
+    *at_device = static_cast<const P*>(t.data_ptr());
+    return true;
+}
+long long integer(PyObject* o)                        // whatever int() takes
+{
+    PyObject* i = PyNumber_Long(o);
+    if (!i) return -1;
+    const long long v = PyLong_AsLongLong(i);
+    Py_DECREF(i);
+    return v;
+}
+double real(PyObject* o) { return PyFloat_AsDouble(o); }
+
+const bsr_adamw* adamw_of(PyObject* address)          // 0: closed, which the entry points refuse
+{
+    return reinterpret_cast<const bsr_adamw*>(PyLong_AsUnsignedLongLong(address));
+}
+
+// adamw_step(handle's address, device, step, lr, beta1, beta2, eps, grad_scale, seed)
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 9) return value_error("adamw_step takes 9 arguments");
+    const bsr_adamw* opt = adamw_of(a[0]);
+    const int device = (int)PyLong_AsLong(a[1]);
+    if (PyErr_Occurred()) return nullptr;
+    bsr_adamw_hyper h{};
+    long long step = 1;
+    double grad_scale = 1.0;
+    if (!setting(a[2], "step", at::kLong, device, integer, &step, &h.step_dev) || !setting(a[3], "lr", at::kFloat, device, real, &h.lr, &h.lr_dev) ||
+        !setting(a[7], "grad_scale", at::kFloat, device, real, &grad_scale, &h.grad_scale_dev)) return nullptr;
+    h.step = step;
+    h.grad_scale = (float)grad_scale;
+    h.beta1 = real(a[4]);
+    h.beta2 = real(a[5]);
+    h.eps = real(a[6]);
+    h.seed = (uint32_t)PyLong_AsUnsignedLongLongMask(a[8]);
+    if (PyErr_Occurred()) return nullptr;
+    bsr_status st;
+    {
+        pybind11::gil_scoped_release no_gil;
+        st = g_adamw_step(opt, &h, stream());
+    }
+    if (st != BSR_OK) return failed(st, "bsr_adamw_step");
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// adamw_moments(handle's address, device, tuple of the tensors' elements, list of pairs of tensors)
+PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t nargs)
+{
+    HANDLE_TH_ERRORS
+    if (nargs != 4 || !PyTuple_Check(a[2]) || !PyList_Check(a[3])) return value_error("adamw_moments takes an address, a device, a tuple and a list");
+    const bsr_adamw* opt = adamw_of(a[0]);
+    const int device = (int)PyLong_AsLong(a[1]);
+    if (PyErr_Occurred()) return nullptr;
+    const Py_ssize_t n = PyTuple_GET_SIZE(a[2]);
+    if (PyList_GET_SIZE(a[3]) != n) return value_error("out: a pair of tensors a parameter");
+    std::vector<void*> out[2];
+    int code = -1;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject* pair = PyList_GET_ITEM(a[3], i);
+        if (!PyTuple_Check(pair) || PyTuple_GET_SIZE(pair) != 2) return value_error("out: a pair of tensors a parameter");
+        const long long count = PyLong_AsLongLong(PyTuple_GET_ITEM(a[2], i));
+        for (int k = 0; k < 2; ++k) {
+            const at::Tensor* t = nullptr;
+            PyObject* obj = PyTuple_GET_ITEM(pair, k);
+            if (!tensor_of(obj, "out", &t)) return nullptr;
+            if (code < 0 && (code = type_code(*t, obj)) < 0) return nullptr;
+            if (t->scalar_type() != kTypes[code] || t->numel() != count || !t->is_contiguous() || !t->is_cuda() || t->get_device() != device) {
+                PyErr_Format(PyExc_ValueError, "out[%lld]: contiguous tensors of one type, %lld elements each, on the handle's device", (long long)i, count);
+                return nullptr;
+            }
+            out[k].push_back(t->data_ptr());
+        }
+    }
+    out[0].push_back(nullptr);                        // an address for an empty list
+    out[1].push_back(nullptr);
+    bsr_status st;
+    {
+        pybind11::gil_scoped_release no_gil;
+        st = g_adamw_moments(opt, code < 0 ? BSR_F32 : (bsr_dtype)code, out[0].data(), out[1].data(), stream());
+    }
+    if (st != BSR_OK) return failed(st, "bsr_adamw_moments");
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(address of bsr_spmm_ex, bsr_spmm_static, bsr_sddmm_ws, bsr_scratch_size, bsr_sddmm_workspace_size,
-//      bsr_spmm_epilogue, bsr_epilogue_backward, bsr_epilogue_backward_workspace_size, BsrError)
+//      bsr_spmm_epilogue, bsr_epilogue_backward, bsr_epilogue_backward_workspace_size, bsr_adamw_step, bsr_adamw_moments, BsrError)
 PyObject* bind(PyObject*, PyObject* args)
 {
-    unsigned long long f[8];
+    unsigned long long f[10];
     PyObject* error = nullptr;
-    if (!PyArg_ParseTuple(args, "KKKKKKKKO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &error)) return nullptr;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9], &error)) return nullptr;
     g_spmm = reinterpret_cast<decltype(g_spmm)>(f[0]);
     g_spmm_static = reinterpret_cast<decltype(g_spmm_static)>(f[1]);
     g_sddmm = reinterpret_cast<decltype(g_sddmm)>(f[2]);
@@ -491,6 +596,8 @@ PyObject* bind(PyObject*, PyObject* args)
     g_spmm_epilogue = reinterpret_cast<decltype(g_spmm_epilogue)>(f[5]);
     g_backward = reinterpret_cast<decltype(g_backward)>(f[6]);
     g_backward_workspace = reinterpret_cast<decltype(g_backward_workspace)>(f[7]);
+    g_adamw_step = reinterpret_cast<decltype(g_adamw_step)>(f[8]);
+    g_adamw_moments = reinterpret_cast<decltype(g_adamw_moments)>(f[9]);
     Py_INCREF(error);
     Py_XDECREF(g_error);
     g_error = error;
@@ -506,6 +613,9 @@ PyMethodDef methods[] = {
      "spmm_epilogue(W, core, X, Y, y_dtype, bias, act, residual, through, Z, keep_z) -> Y or (Y, Z)"},
     {"epilogue_backward", reinterpret_cast<PyCFunction>(epilogue_backward), METH_FASTCALL,
      "epilogue_backward(G, Z, act, DZ, dz_dtype, DB, need_dz, need_db) -> (DZ, DB)"},
+    {"adamw_step", reinterpret_cast<PyCFunction>(adamw_step), METH_FASTCALL,
+     "adamw_step(handle, device, step, lr, beta1, beta2, eps, grad_scale, seed)"},
+    {"adamw_moments", reinterpret_cast<PyCFunction>(adamw_moments), METH_FASTCALL, "adamw_moments(handle, device, counts, out)"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Native host path of the binding.", -1, methods};
