@@ -24,7 +24,7 @@
  *     device work is queued on it and the call returns without waiting.
  *
  * Debug mode.  A handle created while the environment variable BSR_SPMM_DEBUG is set to anything but "0"
- * re-checks, on the device and before every product (bsr_spmm, bsr_spmm_ex, bsr_spmm_static, bsr_sddmm,
+ * re-checks, on the device and before every product (bsr_spmm, bsr_spmm_ex, bsr_spmm_static, bsr_spmm_epilogue, bsr_sddmm,
  * bsr_sddmm_ws), the arrays every kernel address derives from: index_pointer and block_indices as they are in device
  * memory at that moment (BSR_ERR_INDPTR, BSR_ERR_INDEX) and the plan in the workspace
  * (BSR_ERR_WORKSPACE when it no longer holds what bsr_create() wrote, or the first product that wanted more of
@@ -380,7 +380,7 @@ bsr_status bsr_spmm_static(const bsr_matrix* W, int64_t m, const void* X_dev, vo
  * element's in the tensor: the same call on the same values gives the same bits.  The update itself sees m and v before
  * their rounding.
  * Not finite gradients: they reach p, and with 8-bit states the moments of their whole group; a loop that scales its loss
- * looks for them and sets grad_scale_dev to 0, for which nothing is written.
+ * looks for them and sets grad_scale_dev to 0, for which parameters and moments stay as they are.
  */
 typedef struct bsr_adamw bsr_adamw;     /* opaque handle: the list of tensors (device pointers not owned) */
 typedef struct {
@@ -419,7 +419,8 @@ typedef struct {
  * bsr_adamw_step            one step, asynchronous on hip_stream (steps on other streams wait for the upload on the device);
  *                           steps of one handle must not overlap in time.  A captured step may be replayed
  * bsr_adamw_moments         m and v as values of `dtype`: exp_avg_out[i], exp_avg_sq_out[i] (HOST arrays of DEVICE pointers,
- *                           count elements each, or NULL: not wanted) for tensor i of the list
+ *                           count elements each, or NULL: not wanted) for tensor i of the list; apart from one another and
+ *                           from the list's buffers
  * bsr_adamw_destroy         frees the handle's host memory (after waiting for the upload); NULL is accepted
  * Errors: NULL; SHAPE (sizes, blocks that do not make up a tensor, settings out of range, 2^36 elements in all); DTYPE
  * (state_bits too); ALIGN (16 bytes, scales and scalars their own size); INDEX (t_perm_host is no permutation);

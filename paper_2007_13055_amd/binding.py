@@ -501,7 +501,7 @@ def bsr_adamw_step(opt: BsrAdamW, step, *, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
 
 def bsr_adamw_moments(opt: BsrAdamW, dtype="f32", out=None):
     """[(m, v), ...]: the moments as values of `dtype` ("f32" | "f16" | "bf16"), whatever they are held in; out: such a list to
-    fill (of one type, each entry a pair of tensors of a parameter's number of elements)."""
+    fill (of one type, each entry a pair of tensors of a parameter's number of elements, apart from one another and from opt's own)."""
     if out is None:
         import torch
         new = lambda p: torch.empty(p.numel(), dtype=_torch_dtype(dtype), device=opt.device)  # noqa: E731

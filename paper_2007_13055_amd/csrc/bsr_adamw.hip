@@ -21,7 +21,9 @@
 // The stored values of W^T: the chunk's new values pass through LDS and leave in the order of W^T's blocks, 16 bytes a
 // thread, where a block's size divides the chunk; for other blocks bsr_transpose_values() is launched behind.
 //
-// What bounds it: memory, 28 bytes an element with a master copy and fp32 moments of bf16 parameters.
+// What bounds it: memory, 28 bytes an element with a master copy and fp32 moments of bf16 parameters, 30 with W^T: 40 million
+// elements in 231 us, a large copy's rate.  8-bit moments without a master copy move 10, 12 with W^T, and are bound by the vector units
+// (hash, logarithms, exponentials): 112 us, 93 at that rate.  0.95 million elements: 6.0 us, of which the launch is a third.
 #include <algorithm>
 #include <cmath>
 #include <limits>
@@ -444,6 +446,24 @@ bool transposable(const bsr_adamw_tensor& t)
     return block <= 32 * 1024 && (size_t)t.bs_r * (size_t)(t.bs_c + 1) * size_of(t.dtype) <= 64 * 1024;
 }
 
+struct used_range { uintptr_t from, to; bool written; };
+void add_range(std::vector<used_range>& all, const void* p, size_t bytes, bool written)
+{
+    if (p && bytes) all.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written});
+}
+bool by_start(const used_range& a, const used_range& b) { return a.from < b.from; }
+// Whether all that is written is apart from everything else of these, which are in order.
+bool apart(const std::vector<used_range>& all)
+{
+    uintptr_t end = 0, written_end = 0;               // of what begins before
+    for (const used_range& x : all) {
+        if (x.from < (x.written ? end : written_end)) return false;
+        end = std::max(end, x.to);
+        if (x.written) written_end = std::max(written_end, x.to);
+    }
+    return true;
+}
+
 }  // namespace
 
 struct bsr_adamw {
@@ -455,6 +475,7 @@ struct bsr_adamw {
     std::vector<launch_t> launches;
     struct behind_t { size_t tensor; const int32_t* perm; };   // transposes that are launches of their own
     std::vector<behind_t> behind;
+    std::vector<used_range> ranges;                   // all buffers of the list
     const tensor_desc* descs = nullptr;               // device
     const int2* chunks = nullptr;
     std::vector<int32_t> host;                        // kept for the asynchronous upload
@@ -500,14 +521,11 @@ size_t workspace_words(int64_t n, const bsr_adamw_tensor* tensors)
     return std::max<size_t>(words + words_of(chunks * sizeof(int2)), 64);
 }
 
-// Whether everything that a step writes is apart from everything else of the list.
-bool apart(int64_t n, const bsr_adamw_tensor* tensors, int32_t bits, const byte_range& workspace)
+// The buffers of a list, in order.
+std::vector<used_range> ranges_of(int64_t n, const bsr_adamw_tensor* tensors, int32_t bits, const byte_range& workspace)
 {
-    struct item { uintptr_t from, to; bool written; };
-    std::vector<item> all;
-    auto add = [&](const void* p, size_t bytes, bool written) {
-        if (p && bytes) all.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written});
-    };
+    std::vector<used_range> all;
+    auto add = [&](const void* p, size_t bytes, bool written) { add_range(all, p, bytes, written); };
     add(workspace.p, workspace.bytes, true);
     for (int64_t i = 0; i < n; ++i) {
         const bsr_adamw_tensor& t = tensors[i];
@@ -520,14 +538,8 @@ bool apart(int64_t n, const bsr_adamw_tensor* tensors, int32_t bits, const byte_
         if (bits == 8) add(t.scales_dev, (c + kShared - 1) / kShared * 12, true);
         add(t.grad_dev, c * size_of(t.grad_dtype), false);
     }
-    std::sort(all.begin(), all.end(), [](const item& a, const item& b) { return a.from < b.from; });
-    uintptr_t end = 0, written_end = 0;               // of what begins before
-    for (const item& x : all) {
-        if (x.from < (x.written ? end : written_end)) return false;
-        end = std::max(end, x.to);
-        if (x.written) written_end = std::max(written_end, x.to);
-    }
-    return true;
+    std::sort(all.begin(), all.end(), by_start);
+    return all;
 }
 
 bsr_status create_adamw(bsr_adamw** out, int64_t n, const bsr_adamw_tensor* tensors, int32_t state_bits, void* workspace_dev,
@@ -549,8 +561,9 @@ bsr_status create_adamw(bsr_adamw** out, int64_t n, const bsr_adamw_tensor* tens
             if (!aligned16(p)) return BSR_ERR_ALIGN;
         if (reinterpret_cast<uintptr_t>(t.scales_dev) & 3u) return BSR_ERR_ALIGN;
     }
-    if (!apart(n, tensors, state_bits, {workspace_dev, words * 4})) return BSR_ERR_OVERLAP;
     std::unique_ptr<bsr_adamw> opt(new bsr_adamw);
+    opt->ranges = ranges_of(n, tensors, state_bits, {workspace_dev, words * 4});
+    if (!apart(opt->ranges)) return BSR_ERR_OVERLAP;
     opt->bits = state_bits;
     opt->passes = passes_of(n, tensors);
     std::vector<int64_t> order((size_t)n);
@@ -748,6 +761,18 @@ bsr_status bsr_adamw_moments(const bsr_adamw* opt, bsr_dtype dtype, void* const*
     const size_t n = opt->tensors.size();
     for (size_t i = 0; i < n; ++i)
         if (!aligned16(exp_avg_out[i]) || !aligned16(exp_avg_sq_out[i])) return BSR_ERR_ALIGN;
+    try {
+        std::vector<used_range> outs, all;
+        for (size_t i = 0; i < n; ++i)
+            for (const void* p : {(const void*)exp_avg_out[opt->number[i]], (const void*)exp_avg_sq_out[opt->number[i]]})
+                add_range(outs, p, (size_t)opt->tensors[i].count * size_of(dtype), true);
+        std::sort(outs.begin(), outs.end(), by_start);
+        all.resize(outs.size() + opt->ranges.size());
+        std::merge(outs.begin(), outs.end(), opt->ranges.begin(), opt->ranges.end(), all.begin(), by_start);
+        if (!apart(all)) return BSR_ERR_OVERLAP;
+    } catch (const std::bad_alloc&) {
+        return BSR_ERR_HIP;
+    }
     if (!on_its_device(opt)) return BSR_ERR_DEVICE;
     hipStream_t stream = (hipStream_t)hip_stream;
     ready_for(opt, stream);

@@ -555,11 +555,11 @@ PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     int code = -1;
     for (Py_ssize_t i = 0; i < n; ++i) {
         PyObject* pair = PyList_GET_ITEM(a[3], i);
-        if (!PyTuple_Check(pair) || PyTuple_GET_SIZE(pair) != 2) return value_error("out: a pair of tensors a parameter");
+        if (!(PyTuple_Check(pair) || PyList_Check(pair)) || PySequence_Fast_GET_SIZE(pair) != 2) return value_error("out: a pair of tensors a parameter");
         const long long count = PyLong_AsLongLong(PyTuple_GET_ITEM(a[2], i));
         for (int k = 0; k < 2; ++k) {
             const at::Tensor* t = nullptr;
-            PyObject* obj = PyTuple_GET_ITEM(pair, k);
+            PyObject* obj = PySequence_Fast_GET_ITEM(pair, k);
             if (!tensor_of(obj, "out", &t)) return nullptr;
             if (code < 0 && (code = type_code(*t, obj)) < 0) return nullptr;
             if (t->scalar_type() != kTypes[code] || t->numel() != count || !t->is_contiguous() || !t->is_cuda() || t->get_device() != device) {
