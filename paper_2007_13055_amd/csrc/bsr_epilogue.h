@@ -41,10 +41,10 @@ bsr_status with_epilogue(const spmm_args& a, F launch)
     if (!a.epilogue) return launch(no_epilogue{});
     const bsr_epilogue& e = *a.epilogue;
     const int32_t act = e.act;
-    // Results beyond a quarter of the 256 MB cache behind the L2s: what is read once for each would push X and W out of it
-    // (residual of 8192 x 8192 fp16: 159 us, read past the caches 140).  Smaller ones it often still holds from the kernel
-    // that wrote them (4096 x 4096 bf16: 31 us, past the caches 38).
-    const bool once = (int64_t)a.m * a.W->n * (a.y_dtype == BSR_F32 ? 4 : 2) > ((int64_t)64 << 20);
+    // Where neither is in the 256 MB cache behind the L2s, both ways take as long (within 3 % from 34 to 134 MB).  A residual that
+    // the kernel that wrote it left there is read faster through the caches (two 105 MB ones in turn: 89 us, past them 99;
+    // 34 MB: 30 and 36), unless it pushes the result and itself out: two of 134 MB, 154 us, past the caches 136.
+    const bool once = (int64_t)a.m * a.W->n * (a.y_dtype == BSR_F32 ? 4 : 2) > ((int64_t)112 << 20);
     return launch(epilogue_args{e.bias_dev, e.residual_dev, act == BSR_ACT_NONE ? nullptr : e.through_dev, e.z_dev,
                                 e.residual_ld ? e.residual_ld : a.W->n, act, e.bias_dtype == BSR_F32, once});
 }
