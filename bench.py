@@ -2,7 +2,7 @@
 """Benchmark of bsr_spmm on one MI355X.
 
     python bench.py [--gpus 1] [--steps K] [--warmup W] [--workload NAME] [--no-all-configs] [--no-cpu]
-                    [--no-cold] [--no-peaks] [--paper-grid] [--sibling]
+                    [--no-cold] [--no-peaks] [--paper-grid] [--sibling] [--layer]
 
 A step is one whole product Y = X * W^T (one bsr_spmm call) on the headline workload -- by default the
 "large skewed" configuration (fp16, m = k = n = 8192, 64x64 blocks, density 0.05, power-law block-rows), the
@@ -259,6 +259,35 @@ def _sibling(p, steps, chunk):
             "sampled_us_per_product": sd * 1e6, "sampled_tflops": p.flops / sd / 1e12}
 
 
+def _layer(p, steps, chunk):
+    """One training step of a layer with workload p's W, part by part: Y = gelu(X W^T + b) + R with the sums kept
+    (bsr_spmm_epilogue), dZ and the bias's gradient (bsr_epilogue_backward), the gradient of the input taken on through an
+    activation in front (the epilogue on the handle of W^T), of the stored blocks (bsr_sddmm), and an AdamW step that brings
+    W^T's values up to date (fp32 moments; fp32 master copies of 16-bit types); and the step with 8-bit moments."""
+    import torch
+    import paper_2007_13055_amd as lib
+    tdt = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[p.in_dtype]
+    W, X, _ = _upload(p)
+    WT = lib.bsr_create_transposed(p.n, p.k, p.block_data, p.block_indices, p.index_pointer, dtype=p.in_dtype)
+    perm = lib.bsr_transpose_pattern(p.n, p.k, p.bs_r, p.bs_c, p.index_pointer, p.block_indices)[2]
+    new = lambda *s: torch.randn(s, device="cuda").to(tdt)
+    R, G, H, bias = new(p.m, p.n), new(p.m, p.n), new(p.m, p.k), new(p.n)
+    Y, Z, DZ, DB = torch.empty_like(R), torch.empty_like(R), torch.empty_like(R), torch.empty(p.n, device="cuda")
+    DH, DW = torch.empty_like(H), torch.empty_like(W.block_data)
+    opt = {bits: lib.bsr_adamw_create([W.block_data, bias], [DW, DB], weight_decay=[0.1, 0.0], state_bits=bits,
+                                      master=True if tdt is not torch.float32 and bits == 32 else None, transposed=[(WT, perm), None])
+           for bits in (32, 8)}
+    parts = {
+        "forward_us": lambda: lib.bsr_spmm_epilogue(W, X, Y, bias=bias, act="gelu", residual=R, Z=Z),
+        "activation_gradient_us": lambda: lib.bsr_epilogue_backward(G, Z, "gelu", DZ, DB=DB),
+        "input_gradient_us": lambda: lib.bsr_spmm_epilogue(WT, DZ, DH, act="gelu", through=H),
+        "blocks_gradient_us": lambda: lib.bsr_sddmm(W, DZ, X, DW),
+        "adamw_us": lambda: lib.bsr_adamw_step(opt[32], 1, lr=1e-4),
+        "adamw_8_bit_us": lambda: lib.bsr_adamw_step(opt[8], 1, lr=1e-4),
+    }
+    return {name: _time_steps(fn, steps, 20, chunk)[1] / steps * 1e6 for name, fn in parts.items()}
+
+
 def _cold(p, steps):
     """The product with operands that are NOT resident in the 256 MB last-level cache: the calls rotate
     through enough distinct (W, X, Y) sets that 1 GiB of other data passes between two uses of the same
@@ -358,6 +387,8 @@ def main():
     ap.add_argument("--no-peaks", action="store_true", help="skip the copy and MFMA-loop measurements of this chip")
     ap.add_argument("--sibling", action="store_true",
                     help="also time the sibling products (Z = G * W through the handle of W^T, and the sampled product)")
+    ap.add_argument("--layer", action="store_true",
+                    help="also time a training step of a layer: epilogue, gradients, AdamW")
     ap.add_argument("--paper-grid", action="store_true",
                     help="also time the 36 cells of the paper's own shape grid (m = 1, 8) and add them as 'paper_grid'")
     ap.add_argument("--workload", default="skewed", choices=list(CONFIG_ID),
@@ -442,6 +473,9 @@ def main():
         out["per_config"] = table
     if a.paper_grid:
         out["paper_grid"] = _paper_grid(1000, 100)
+    if a.layer:
+        import workloads as wl
+        out["layer"] = _layer(wl.config(headline), a.steps, chunk)
     if a.sibling:
         import workloads as wl
         out["sibling"] = _sibling(wl.config(headline), a.steps, chunk)
