@@ -113,6 +113,27 @@ def test_16_bit_results_are_rounded_once(shape, monkeypatch):
         assert np.all(np.abs(_f64(Y) - want) <= bound + u * (np.abs(want) + bound) + tiny), (shape, act)
 
 
+@pytest.mark.parametrize("shape", KERNELS, ids=lambda s: "x".join(map(str, s)))
+def test_parts_do_not_change_each_other(shape, monkeypatch):
+    """Y is the same whether or not Z is kept, and a residual of zeros and a bias of zeros change nothing."""
+    import torch
+    import paper_2007_13055_amd as lib
+    m, k, n, bs_r, bs_c, dtype, tune = shape
+    if tune:
+        monkeypatch.setenv("BSR_SPMM_TUNE", tune)
+    p = _problem(m, k, n, bs_r, bs_c, dtype, seed=6)
+    W, X = _handle(p), to_device(p.X, dtype)
+    T = torch_dtype(dtype)
+    bias = torch.randn(n, generator=torch.Generator(device="cuda").manual_seed(7), device="cuda").to(T)
+    none = torch.zeros((m, n), dtype=T, device="cuda")
+    for act in ACTS:
+        Y = lib.bsr_spmm_epilogue(W, X, bias=bias, act=act)
+        assert torch.equal(lib.bsr_spmm_epilogue(W, X, bias=bias, act=act, keep_z=True)[0], Y), act
+        assert torch.equal(lib.bsr_spmm_epilogue(W, X, bias=bias, act=act, residual=none), Y), act   # (-0 + 0 equals -0)
+        assert torch.equal(lib.bsr_spmm_epilogue(W, X, bias=torch.zeros_like(bias), act=act), lib.bsr_spmm_epilogue(W, X, act=act)), act
+    assert torch.equal(lib.bsr_spmm_epilogue(W, X), lib.bsr_spmm(W, X))
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_row_groups_and_the_tiles_behind_them(dtype):
     """64x64 blocks, a few block-rows with most of them, from 1024 rows on: two kernels write one result."""
