@@ -219,6 +219,12 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
     constexpr int EPT = 16 / (int)sizeof(O);          // outputs a thread stores
     constexpr int TPR = 64 / EPT;
     float* tiles = reinterpret_cast<float*>(lds);
+    // Pieces quad by quad; with an epilogue row by row, so that a thread keeps its columns and their bias (4096 x (1024, 4096)
+    // bf16 16x16 20 %: bias, gelu_tanh and residual 31.1 us, the other way 33.6; bias alone 26.1 and 27.5): the threads are a
+    // multiple of a row's pieces.
+    auto quad_of = [&](int t) { return E::on ? t / TPR % Q : t / (RP * TPR); };
+    auto row_of = [&](int t) { return E::on ? t / TPR / Q : t / TPR % RP; };
+    [[maybe_unused]] bias_run<T, EPT> bias;
 #pragma unroll
     for (int p = 0; p < 16 * SUB / RP; ++p) {
         __syncthreads();
@@ -231,8 +237,10 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
                     *reinterpret_cast<f32x4*>(mine + (ss * 16 + li) * kLdOut + j * 16 + 4 * h) = acc[j][p * (RP / 16) + ss];
         }
         __syncthreads();
+        if constexpr (E::on)
+            if (p == 0) bias.fetch(ep, min(column[quad_of(tid)] + tid % TPR * EPT, n - EPT));
         for (int t = tid; t < Q * RP * TPR; t += 64 * (kWaves + kLoaders)) {
-            const int qi = t / (RP * TPR), row = t / TPR % RP, c = t % TPR * EPT;
+            const int qi = quad_of(t), row = row_of(t), c = t % TPR * EPT;
             const int i = i_base + p * RP + row, col = column[qi] + c;
             if (col >= n || i >= m) continue;
             const float* src = tiles + ((size_t)(qi * KS) * RP + row) * kLdOut + c;
@@ -244,7 +252,11 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
 #pragma unroll
                 for (int e = 0; e < EPT; ++e) v[e] += src[e];
             }
-            if constexpr (E::on) finish<T, O>(ep, v, i, col, n);
+            if constexpr (E::on) {
+                result_reads<O, EPT> reads;
+                reads.fetch(ep, i, col, n);
+                finish<T, O>(ep, bias, reads, v, i, col, n);
+            }
             O* dst = Y + (size_t)i * (size_t)n + col;
             if constexpr (EPT == 4) {
                 *reinterpret_cast<f32x4*>(dst) = f32x4{v[0], v[1], v[2], v[3]};
@@ -265,7 +277,7 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
         const int bs_c = row_bytes / S;
         for (int p = 0; p < 16 * SUB / RP; ++p)
             for (int t = tid; t < Q * RP * TPR; t += 64 * (kWaves + kLoaders)) {
-                const int i = i_base + p * RP + t / TPR % RP, col = column[t / (RP * TPR)] + t % TPR * EPT;
+                const int i = i_base + p * RP + row_of(t), col = column[quad_of(t)] + t % TPR * EPT;
                 if (col >= n || i >= m) continue;
                 O* dst = Y + (size_t)i * (size_t)n + col;
                 for (int e = 0; e < EPT; ++e) {
