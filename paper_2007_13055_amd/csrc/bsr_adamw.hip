@@ -23,7 +23,7 @@
 //
 // What bounds it: memory, 28 bytes an element with a master copy and fp32 moments of bf16 parameters, 30 with W^T: 40 million
 // elements in 231 us, a large copy's rate.  8-bit moments without a master copy move 10, 12 with W^T, and are bound by the vector units
-// (hash, logarithms, exponentials): 112 us, 93 at that rate.  0.95 million elements: 6.0 us, of which the launch is a third.
+// (hash, logarithms, exponentials): 120 us, 93 at that rate.  0.95 million elements: 6.0 us, of which the launch is a third.
 #include <algorithm>
 #include <cmath>
 #include <limits>
@@ -65,7 +65,7 @@ static_assert(sizeof(tensor_desc) == 96, "uploaded as words");
 struct step_args {
     float lr, beta1, beta2, one1, one2, eps;          // one1 = 1 - beta1
     float rate, root;                                 // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t); where step_dev is null
-    float log1, log2, log2_beta2;                     // natural logarithms of the betas, log2 of beta2
+    float log1, log2;                                 // natural logarithms of the betas
     float grad_scale;
     uint32_t key;                                     // of the seed and the step
     uint32_t seed;
@@ -135,12 +135,18 @@ __device__ __forceinline__ void decode_first(float (&m)[4], uint32_t codes, floa
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
     m[0] = a.x * scale; m[1] = a.y * scale; m[2] = b.x * scale; m[3] = b.y * scale;
 }
+// (the argument's product and sum rounded each, as where a code is chosen)
+__device__ __forceinline__ float second_of(float at, float start, float spacing)
+{
+#pragma clang fp contract(off)
+    return __builtin_amdgcn_exp2f(at * spacing + start);
+}
 __device__ __forceinline__ void decode_second(float (&v)[4], uint32_t codes, float start, float spacing)
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const float c = (float)((codes >> (8 * e)) & 255u);
-        v[e] = c > 0.f ? __builtin_amdgcn_exp2f(fmaf(c, spacing, start - spacing)) : 0.f;
+        v[e] = c > 0.f ? second_of(c - 1.f, start, spacing) : 0.f;
     }
 }
 
@@ -182,8 +188,18 @@ template <typename T, typename GT, int BITS, bool MASTER> struct pass_reads {
     }
 };
 
+// a x + b y, each operation rounded: moments that are held in 8 bits.  Their codes are up to a twelfth of m and a twentieth of
+// v apart, so a last bit that is rounded another way can move the next update by that much.  With the sums, the arguments of
+// exponentials and the quotients rounded as the formulas are written, plain fp32 arithmetic finds the same codes (of 45
+// million one differed).  With fmas and reciprocals 2 of 100 000 v and 2 of a million m did, for 10 of 120 us.
+__device__ __forceinline__ float weighted(float a, float x, float b, float y)
+{
+#pragma clang fp contract(off)
+    return a * x + b * y;
+}
+
 struct step_now {                                     // a step's settings as a chunk uses them
-    float beta1, beta2, log2_beta2, eps, rate, root, keep;
+    float beta1, beta2, eps, rate, root, keep;
     float one1, one2;                                 // (1 - beta1) scale, (1 - beta2) scale^2 for gradients times scale
     uint32_t base;
 };
@@ -195,19 +211,18 @@ __device__ __forceinline__ void step_pass(const tensor_desc& d, const step_now& 
     float p[4], m[4], v[4];
     run4<T> stored;
     uint32_t random[4];
-    // m and v times their betas: with 8 bits as part of the scales (the step takes all the VALU's time that memory leaves)
     if constexpr (BITS == 8) {
-        decode_first(m, word_of(in.m), in.scale[0] * h.beta1);
-        decode_second(v, word_of(in.v), in.scale[1] + h.log2_beta2, in.scale[2]);
+        decode_first(m, word_of(in.m), in.scale[0]);
+        decode_second(v, word_of(in.v), in.scale[1], in.scale[2]);
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { m[e] = in.m.v[e] * h.beta1; v[e] = in.v.v[e] * h.beta2; }
+        for (int e = 0; e < 4; ++e) { m[e] = in.m.v[e]; v[e] = in.v.v[e]; }
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const float g = (float)in.g.v[e];
-        m[e] = fmaf(h.one1, g, m[e]);
-        v[e] = fmaf(h.one2 * g, g, v[e]);
+        m[e] = BITS == 8 ? weighted(h.beta1, m[e], h.one1, g) : fmaf(h.one1, g, m[e] * h.beta1);
+        v[e] = BITS == 8 ? weighted(h.beta2, v[e], h.one2 * g, g) : fmaf(h.one2 * g, g, v[e] * h.beta2);
         const float down = fmaf(__builtin_amdgcn_sqrtf(v[e]), h.root, h.eps);
         p[e] = fmaf(-h.rate * m[e], __builtin_amdgcn_rcpf(down), (float)in.p.v[e] * h.keep);
         // fp32 numbers, of which the stored ones are roundings: left to itself the compiler rounds the exact sum to fp16
@@ -249,10 +264,15 @@ __device__ __forceinline__ void step_pass(const tensor_desc& d, const step_now& 
         float inverse = 0.f;
         if (top_m >= 0x1p-100f) {                     // uniform
             scale[0] = top_m * (1.f / kTop8);
-            inverse = kTop8 * __builtin_amdgcn_rcpf(top_m);
+            inverse = __builtin_amdgcn_rcpf(scale[0]);
+            inverse = fmaf(fmaf(-scale[0], inverse, 1.f), inverse, inverse);
         }
-        int packed = __builtin_amdgcn_cvt_pk_fp8_f32(m[0] * inverse, m[1] * inverse, 0, false);
-        packed = __builtin_amdgcn_cvt_pk_fp8_f32(m[2] * inverse, m[3] * inverse, packed, true);
+        auto quotient = [&](float x) {                // x / scale
+            const float q = x * inverse;
+            return fmaf(fmaf(-q, scale[0], x), inverse, q);
+        };
+        int packed = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(m[0]), quotient(m[1]), 0, false);
+        packed = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(m[2]), quotient(m[3]), packed, true);
         if (!(most <= kMost)) {                       // a gradient that is not finite: so are the values of the whole group
             scale[1] = most;
         } else if (most >= kLeast) {                  // uniform
@@ -264,10 +284,11 @@ __device__ __forceinline__ void step_pass(const tensor_desc& d, const step_now& 
         uint32_t codes = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float below = __builtin_amdgcn_fmed3f(floorf(fmaf(__builtin_amdgcn_logf(v[e]), per, offset)), 0.f, 253.f);
-            // where v lies from one code to the next, times 2^24
-            const float up = fmaf(v[e] * step, __builtin_amdgcn_exp2f(-fmaf(below, scale[2], scale[1])), -step);
-            const uint32_t code = (uint32_t)below + 1u + ((float)(random[e] >> 8) < up ? 1u : 0u);
+            const float at_code = __builtin_amdgcn_fmed3f(floorf(fmaf(__builtin_amdgcn_logf(v[e]), per, offset)), 0.f, 253.f);
+            // where v lies from one code to the next, times 2^24; the quotient v / below
+            const float below = second_of(at_code, scale[1], scale[2]), r = __builtin_amdgcn_rcpf(below), q = v[e] * r;
+            const float up = (fmaf(fmaf(-q, below, v[e]), r, q) - 1.f) * step;
+            const uint32_t code = (uint32_t)at_code + 1u + ((float)(random[e] >> 8) < up ? 1u : 0u);
             codes |= (v[e] < kLeast ? 0u : code) << (8 * e);   // (a NaN has a code, of which its scales make one again)
         }
         if (FULL || n > 0) {
@@ -301,7 +322,7 @@ __global__ __launch_bounds__(kThreads) void bsr_adamw_chunks(const tensor_desc* 
 #pragma unroll
         for (int q = 0; q < kPasses; ++q) in[q].template fetch<true>(d, first, at + q * kPass, 4);
 
-    step_now h{a.beta1, a.beta2, a.log2_beta2, a.eps, a.rate, a.root, 0.f, 0.f, 0.f, 0u};
+    step_now h{a.beta1, a.beta2, a.eps, a.rate, a.root, 0.f, 0.f, 0.f, 0u};
     float lr = a.lr, grad_scale = a.grad_scale;
     uint32_t key = a.key;
     if (a.grad_scale_dev) {
@@ -727,7 +748,6 @@ bsr_status bsr_adamw_step(const bsr_adamw* opt, const bsr_adamw_hyper* hyper, vo
     h.eps = (float)y.eps;
     h.log1 = (float)std::log(y.beta1);
     h.log2 = (float)std::log(y.beta2);
-    h.log2_beta2 = (float)std::log2(y.beta2);
     if (!y.step_dev) {
         h.rate = (float)(1.0 / (1.0 - std::pow(y.beta1, (double)y.step)));
         h.root = (float)(1.0 / std::sqrt(1.0 - std::pow(y.beta2, (double)y.step)));

@@ -431,3 +431,35 @@ def test_all_of_a_groups_gradients_are_zero():
     # 3e4 squared is the largest of its group; 1e-12 squared is below 2^-40 of it and is held as that, so its update shrinks
     assert abs(float(v[601]) / (want * 9e8) - 1) < 0.4 and float(v[600]) > 0 and abs(float(p[600]) - 1) < 1e-3
     assert abs(float(p[601]) - (1 - 3 * H["lr"])) < 1e-4
+
+
+@pytest.mark.parametrize("dtype,grad,master", [("f32", "f32", False), ("bf16", "bf16", True)])
+def test_8_bit_codes_are_those_of_plain_arithmetic(dtype, grad, master):
+    """First moments code by code as fp32 arithmetic that rounds each operation gives them; second moments within a code of
+    their value."""
+    import torch
+    import paper_2007_13055_amd as lib
+    count = 256 * 4000
+    params, grads = _tensors([count], dtype, grad, 21)
+    opt = lib.bsr_adamw_create(params, grads, state_bits=8, master=True if master else None)
+    f32 = torch.float32
+    b1, c1, b2, c2 = (torch.tensor(v, dtype=torch.float64, device="cuda").to(f32) for v in (0.9, 1 - 0.9, 0.95, 1 - 0.95))
+    for t in (1, 2, 3):
+        codes, scales = opt.exp_avg[0].clone(), opt.scales[0].clone()
+        v_codes = opt.exp_avg_sq[0].clone().view(-1, 256).float()
+        lib.bsr_adamw_step(opt, t, seed=3, **H)
+        g = grads[0].float().view(-1, 256)
+        m = codes.view(torch.float8_e4m3fn).float().view(-1, 256) * scales[:, :1]
+        m = torch.add(torch.mul(m, b1), torch.mul(g, c1))
+        scale = m.abs().amax(1, keepdim=True) * torch.tensor(1 / 448, dtype=torch.float64, device="cuda").to(f32)
+        assert torch.equal(opt.scales[0][:, :1], scale), t
+        want = (m / scale).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+        assert torch.equal(opt.exp_avg[0].view(-1, 256), want), t
+        # v before its rounding, in 64 bits: the code lies within one step of it
+        v = torch.where(v_codes > 0, torch.exp2(scales[:, 1:2].double() + (v_codes.double() - 1) * scales[:, 2:].double()), 0.0)
+        v = 0.95 * v + 0.05 * g.double() ** 2
+        now = opt.scales[0].double()
+        at = ((torch.log2(v) - now[:, 1:2]) / now[:, 2:] + 1).clamp_min(1)    # (below 2^-40 of the largest: the first code)
+        # fp32: an argument of some 30 rounded to 2^-19, a step of the codes is at least 2^-6 of it in log2 v here
+        off = (opt.exp_avg_sq[0].view(-1, 256).double() - at)[v > 2.0 ** -100]
+        assert float(off.abs().max()) < 1 + 2.0 ** -10, t
