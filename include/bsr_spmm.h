@@ -162,7 +162,8 @@ bsr_status bsr_spmm(const bsr_matrix* W, int64_t m, const void* X_dev, void* Y_d
  * the activation in front of the layer whose W^T is multiplied: Y = (G W) * act'(Z0).  All of it is fp32 arithmetic on the
  * accumulated sum; what is stored is rounded once, to nearest-even, and act(z) sees the z before that rounding.
  *   act             BSR_ACT_*: none; max(z, 0); z Phi(z), Phi the normal distribution's integral (relative error below
- *                   1e-6); z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2; z / (1 + exp(-z))
+ *                   1.5e-6 + 2^-23 z^2 down to z = -12.9, where Phi is below fp32's normal numbers, and below 1.5e-6 for
+ *                   positive z); z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2; z / (1 + exp(-z))
  *   bias_dev        DEVICE, n elements of bias_dtype (W's dtype or BSR_F32), or NULL
  *   residual_dev    DEVICE, m rows of n elements of y_dtype, `residual_ld` elements apart (0: n, contiguous), or NULL
  *   through_dev     DEVICE, Z0, m*n elements of y_dtype, or NULL; not read where act is BSR_ACT_NONE (slope 1)

@@ -11,8 +11,12 @@
 //   silu       x s(x),   s(x) = 1 / (1 + exp(-x))
 //   gelu_tanh  x s(2 u), u = sqrt(2 / pi) (x + 0.044715 x^3): tanh(u) = 2 s(2 u) - 1
 //   gelu       x Phi(x) = max(x, 0) - |x| Q(|x|),  Q(a) = erfc(a / sqrt 2) / 2 = exp(-a^2 / 2) P(a):  P(a) = t S(t) with
-//              t = 1 / (1 + 0.24 a), S of degree 7, fitted to least relative error (4.3e-7 over a in [0, 40]; in fp32 8e-7).
-//              Written so, a negative x keeps its relative accuracy, which 1 + erf(x / sqrt 2) loses by cancellation.
+//              t = 1 / (1 + 0.24 a), S of degree 7, fitted to least relative error with P(0) = 1/2 held, so that the slope has
+//              no jump at 0 (4.4e-7 over a in [0, 40], with the coefficients as fp32 holds them).  Written so, a negative x
+//              keeps its relative accuracy, which 1 + erf(x / sqrt 2) loses by cancellation.  In fp32 the relative error of
+//              Q is below 1.5e-6 + 2^-23 a^2 while Q is a normal number (a < 12.9): besides the fit, t's two roundings (P
+//              follows t with a power of up to 3.3), the exponential's ulp and three products', 1e-6; and the three
+//              roundings, half an ulp each, of the exponential's argument, of which a^2 / 2 becomes a relative error.
 // A NaN stays one; at infinite z the limits are taken (0 or z, slopes 0 or 1) in place of the NaN of 0 * inf.
 #pragma once
 
@@ -63,16 +67,16 @@ __device__ __forceinline__ float finite(float x) { return __builtin_amdgcn_fmed3
 // exp(-x^2 / 2) and Q(|x|)
 __device__ __forceinline__ void normal_tail(float x, float& e, float& q)
 {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.24f, fabsf(x), 1.f)), y = x * 0.849321800f;   // sqrt(log2(e) / 2)
-    float s = -0.0529904738f;
-    s = fmaf(s, t, 0.152789459f);
-    s = fmaf(s, t, -0.0656933263f);
-    s = fmaf(s, t, 0.118379995f);
-    s = fmaf(s, t, 0.0634018406f);
-    s = fmaf(s, t, 0.0928374827f);
-    s = fmaf(s, t, 0.0955223069f);
-    s = fmaf(s, t, 0.0957537889f);
-    e = __builtin_amdgcn_exp2f(-y * y);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.24f, fabsf(x), 1.f));
+    float s = -0.0530403703f;
+    s = fmaf(s, t, 0.152946189f);
+    s = fmaf(s, t, -0.0658932477f);
+    s = fmaf(s, t, 0.11851076f);
+    s = fmaf(s, t, 0.0633547232f);
+    s = fmaf(s, t, 0.0928467363f);
+    s = fmaf(s, t, 0.0955213904f);
+    s = fmaf(s, t, 0.0957538188f);
+    e = __builtin_amdgcn_exp2f(x * x * -0.72134752f);                 // log2(e) / 2
     q = e * (t * s);
 }
 
