@@ -414,8 +414,8 @@ typedef struct {
 /*
  * bsr_adamw_workspace_size  bytes of DEVICE workspace for the tables of a list (> 0, a multiple of 256)
  * bsr_adamw_create          checks the list (`tensors`, HOST) and uploads its tables to workspace_dev on hip_stream; the
- *                           device buffers and the workspace stay the caller's, must outlive the handle and keep their
- *                           places; everything a step writes must be apart from every other buffer of the list.  Not for a
+ *                           device buffers and the workspace stay the caller's, must outlive the handle, the steps that are
+ *                           still to run (on any stream) and the graphs that hold some, and keep their places; everything a step writes must be apart from every other buffer of the list.  Not for a
  *                           stream that is being captured.  state_bits: 32 or 8, of all its tensors.  *out is NULL on error
  * bsr_adamw_step            one step, asynchronous on hip_stream (steps on other streams wait for the upload on the device);
  *                           steps of one handle must not overlap in time.  A captured step may be replayed

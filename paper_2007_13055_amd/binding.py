@@ -382,6 +382,9 @@ def bsr_query_path(W: BsrMatrix, m: int) -> int:
 class BsrAdamW:
     """Owns the tensors of one list (parameters, gradients, moments, ...; they must outlive the C handle) and the handle.
 
+    Steps may run on any stream of its device, and it may be dropped while they are still to run.  A graph that a step was
+    captured into reads its buffers at every replay: it must outlive the graph.
+
     params, grads, master, exp_avg, exp_avg_sq, scales: lists in the order given to bsr_adamw_create (None where a tensor has
     none)."""
 
@@ -390,6 +393,20 @@ class BsrAdamW:
         self.exp_avg, self.exp_avg_sq, self.scales = exp_avg, exp_avg_sq, scales
         self.handle, self.device, self._keep = None, None, []
         self._address, self._index, self._counts = 0, 0, tuple(int(p.numel()) for p in params)   # what the calls read
+        self._home, self._streams = 0, set()   # the stream its buffers were made on, the others that have been given work
+
+    def _on_stream(self, address):
+        """Work on another stream than the home one, torch's current, is about to be queued: its buffers' memory is not to be
+        used again before that has run, even if nothing else holds them by then."""
+        if address in self._streams:
+            return
+        import torch
+        stream = torch.cuda.current_stream(self.device)
+        for held in (self.params, self.grads, self.master, self.exp_avg, self.exp_avg_sq, self.scales, self._keep):
+            for t in held:
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(stream)
+        self._streams.add(address)
 
     def close(self):
         if self.handle:
@@ -488,6 +505,7 @@ def bsr_adamw_create(params, grads, *, weight_decay=0.0, state_bits=32, moments=
     if st != 0:
         raise BsrError(st, "bsr_adamw_create")
     opt.handle, opt._address, opt._index = handle, handle.value, device.index
+    opt._home = torch.cuda.current_stream().cuda_stream
     return opt
 
 
@@ -496,7 +514,7 @@ def bsr_adamw_step(opt: BsrAdamW, step, *, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
 
     step counts from 1.  step, lr and grad_scale may be GPU tensors of one int64, fp32 and fp32, which a step captured into a
     graph reads at every replay; a grad_scale of 0 skips the step.  seed: of the random roundings."""
-    _native.adamw_step(opt._address, opt._index, step, lr, betas[0], betas[1], eps, grad_scale, seed)
+    _native.adamw_step(opt, opt._address, opt._index, opt._home, step, lr, betas[0], betas[1], eps, grad_scale, seed)
 
 
 def bsr_adamw_moments(opt: BsrAdamW, dtype="f32", out=None):
@@ -506,5 +524,5 @@ def bsr_adamw_moments(opt: BsrAdamW, dtype="f32", out=None):
         import torch
         new = lambda p: torch.empty(p.numel(), dtype=_torch_dtype(dtype), device=opt.device)  # noqa: E731
         out = [(new(p), new(p)) for p in opt.params]
-    _native.adamw_moments(opt._address, opt._index, opt._counts, out if isinstance(out, list) else list(out))
+    _native.adamw_moments(opt, opt._address, opt._index, opt._home, opt._counts, out if isinstance(out, list) else list(out))
     return out

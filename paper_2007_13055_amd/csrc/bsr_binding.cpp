@@ -511,14 +511,32 @@ const bsr_adamw* adamw_of(PyObject* address)          // 0: closed, which the en
     return reinterpret_cast<const bsr_adamw*>(PyLong_AsUnsignedLongLong(address));
 }
 
-// adamw_step(handle's address, device, step, lr, beta1, beta2, eps, grad_scale, seed)
+// A call on another stream than `home`, on which the handle's buffers were made: the owner has the allocator told
+// (BsrAdamW._on_stream), or it would give them away, as soon as the owner is dropped, to what home is given next, while this
+// call is still to read its tables.  False with an error set.
+bool told_of_stream(PyObject* owner, int device, PyObject* home)
+{
+    const unsigned long long made_on = PyLong_AsUnsignedLongLong(home);
+    if (PyErr_Occurred()) return false;
+    if ((int)c10::hip::current_device() != device) return true;   // refused by the entry point
+    const unsigned long long now = reinterpret_cast<uintptr_t>(stream());
+    if (now == made_on) return true;
+    PyObject* done = PyObject_CallMethod(owner, "_on_stream", "K", now);
+    if (!done) return false;
+    Py_DECREF(done);
+    return true;
+}
+
+// adamw_step(owner, handle's address, device, stream it was made on, step, lr, beta1, beta2, eps, grad_scale, seed)
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
-    if (nargs != 9) return value_error("adamw_step takes 9 arguments");
-    const bsr_adamw* opt = adamw_of(a[0]);
-    const int device = (int)PyLong_AsLong(a[1]);
+    if (nargs != 11) return value_error("adamw_step takes 11 arguments");
+    PyObject *owner = a[0], *home = a[3];
+    const bsr_adamw* opt = adamw_of(a[1]);
+    const int device = (int)PyLong_AsLong(a[2]);
     if (PyErr_Occurred()) return nullptr;
+    a += 2;                                           // the settings' places below
     bsr_adamw_hyper h{};
     long long step = 1;
     double grad_scale = 1.0;
@@ -530,7 +548,7 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     h.beta2 = real(a[5]);
     h.eps = real(a[6]);
     h.seed = (uint32_t)PyLong_AsUnsignedLongLongMask(a[8]);
-    if (PyErr_Occurred()) return nullptr;
+    if (PyErr_Occurred() || (opt && !told_of_stream(owner, device, home))) return nullptr;
     bsr_status st;
     {
         pybind11::gil_scoped_release no_gil;
@@ -541,14 +559,17 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
-// adamw_moments(handle's address, device, tuple of the tensors' elements, list of pairs of tensors)
+// adamw_moments(owner, handle's address, device, stream it was made on, tuple of the tensors' elements, list of pairs of tensors)
 PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
-    if (nargs != 4 || !PyTuple_Check(a[2]) || !PyList_Check(a[3])) return value_error("adamw_moments takes an address, a device, a tuple and a list");
-    const bsr_adamw* opt = adamw_of(a[0]);
-    const int device = (int)PyLong_AsLong(a[1]);
+    if (nargs != 6 || !PyTuple_Check(a[4]) || !PyList_Check(a[5]))
+        return value_error("adamw_moments takes an owner, an address, a device, a stream, a tuple and a list");
+    PyObject *owner = a[0], *home = a[3];
+    const bsr_adamw* opt = adamw_of(a[1]);
+    const int device = (int)PyLong_AsLong(a[2]);
     if (PyErr_Occurred()) return nullptr;
+    a += 2;
     const Py_ssize_t n = PyTuple_GET_SIZE(a[2]);
     if (PyList_GET_SIZE(a[3]) != n) return value_error("out: a pair of tensors a parameter");
     std::vector<void*> out[2];
@@ -569,6 +590,7 @@ PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t nargs)
             out[k].push_back(t->data_ptr());
         }
     }
+    if (opt && !told_of_stream(owner, device, home)) return nullptr;
     out[0].push_back(nullptr);                        // an address for an empty list
     out[1].push_back(nullptr);
     bsr_status st;
@@ -614,8 +636,8 @@ PyMethodDef methods[] = {
     {"epilogue_backward", reinterpret_cast<PyCFunction>(epilogue_backward), METH_FASTCALL,
      "epilogue_backward(G, Z, act, DZ, dz_dtype, DB, need_dz, need_db) -> (DZ, DB)"},
     {"adamw_step", reinterpret_cast<PyCFunction>(adamw_step), METH_FASTCALL,
-     "adamw_step(handle, device, step, lr, beta1, beta2, eps, grad_scale, seed)"},
-    {"adamw_moments", reinterpret_cast<PyCFunction>(adamw_moments), METH_FASTCALL, "adamw_moments(handle, device, counts, out)"},
+     "adamw_step(owner, handle, device, stream, step, lr, beta1, beta2, eps, grad_scale, seed)"},
+    {"adamw_moments", reinterpret_cast<PyCFunction>(adamw_moments), METH_FASTCALL, "adamw_moments(owner, handle, device, stream, counts, out)"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Native host path of the binding.", -1, methods};
