@@ -15,8 +15,10 @@
 //              no jump at 0 (4.4e-7 over a in [0, 40], with the coefficients as fp32 holds them).  Written so, a negative x
 //              keeps its relative accuracy, which 1 + erf(x / sqrt 2) loses by cancellation.  In fp32 the relative error of
 //              Q is below 1.5e-6 + 2^-23 a^2 while Q is a normal number (a < 12.9): besides the fit, t's two roundings (P
-//              follows t with a power of up to 3.3), the exponential's ulp and three products', 1e-6; and the three
-//              roundings, half an ulp each, of the exponential's argument, of which a^2 / 2 becomes a relative error.
+//              follows t with a power of up to 3.3), the exponential's ulp and three products', 1e-6; and what the argument
+//              y^2, y = a sqrt(log2(e) / 2), is off by, 2^-24 for the constant and for y, twice each, and for the square, of
+//              which a^2 / 2 becomes a relative error.  (x^2 times a constant has one rounding less, and its products are
+//              ordered otherwise by the compiler: 4096 x (1024, 4096) bf16 16x16 20 % 32.8 us, this way 31.9.)
 // A NaN stays one; at infinite z the limits are taken (0 or z, slopes 0 or 1) in place of the NaN of 0 * inf.
 #pragma once
 
@@ -67,7 +69,7 @@ __device__ __forceinline__ float finite(float x) { return __builtin_amdgcn_fmed3
 // exp(-x^2 / 2) and Q(|x|)
 __device__ __forceinline__ void normal_tail(float x, float& e, float& q)
 {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.24f, fabsf(x), 1.f));
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.24f, fabsf(x), 1.f)), y = x * 0.849321800f;   // sqrt(log2(e) / 2)
     float s = -0.0530403703f;
     s = fmaf(s, t, 0.152946189f);
     s = fmaf(s, t, -0.0658932477f);
@@ -76,7 +78,7 @@ __device__ __forceinline__ void normal_tail(float x, float& e, float& q)
     s = fmaf(s, t, 0.0928467363f);
     s = fmaf(s, t, 0.0955213904f);
     s = fmaf(s, t, 0.0957538188f);
-    e = __builtin_amdgcn_exp2f(x * x * -0.72134752f);                 // log2(e) / 2
+    e = __builtin_amdgcn_exp2f(-y * y);
     q = e * (t * s);
 }
 
