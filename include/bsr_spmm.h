@@ -400,7 +400,8 @@ typedef struct {
 } bsr_adamw_tensor;
 
 /* A step's settings.  The *_dev members (DEVICE scalars, or NULL) take the place of the values beside them when the step runs:
- * a step captured into a graph reads its number, rate and scale at every replay. */
+ * a step captured into a graph reads its number, rate and scale at every replay.  Where the number is below 1 there, or the
+ * scale 0, the step is skipped. */
 typedef struct {
     double lr, beta1, beta2, eps;       /* 0 <= beta < 1, lr and eps >= 0 */
     int64_t step;                       /* t >= 1 */

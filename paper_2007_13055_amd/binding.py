@@ -513,7 +513,7 @@ def bsr_adamw_step(opt: BsrAdamW, step, *, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
     """One step on torch's current stream, updating opt's parameters, master copies, moments and transposes in place.
 
     step counts from 1.  step, lr and grad_scale may be GPU tensors of one int64, fp32 and fp32, which a step captured into a
-    graph reads at every replay; a grad_scale of 0 skips the step.  seed: of the random roundings."""
+    graph reads at every replay; a grad_scale of 0 skips the step, and so does a step below 1 on the GPU.  seed: of the random roundings."""
     _native.adamw_step(opt, opt._address, opt._index, opt._home, step, lr, betas[0], betas[1], eps, grad_scale, seed)
 
 

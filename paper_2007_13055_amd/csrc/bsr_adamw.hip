@@ -334,6 +334,7 @@ __global__ __launch_bounds__(kThreads) void bsr_adamw_chunks(const tensor_desc* 
     if (a.lr_dev) lr = *a.lr_dev;
     if (a.step_dev) {
         const int64_t t = *a.step_dev;
+        if (t < 1) return;                            // no such step (its corrections divide by 0): skipped, as for a scale of 0
         h.root = __builtin_amdgcn_rsqf(-expm1f((float)t * a.log2));
         h.rate = -1.f / expm1f((float)t * a.log1);
         key = step_key(a.seed, (uint64_t)t);
