@@ -361,7 +361,9 @@ bsr_status bsr_spmm_static(const bsr_matrix* W, int64_t m, const void* X_dev, vo
  * of W^T with them.  With g the gradient times grad_scale, t the step's number (from 1):
  *     m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
  *     p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32 whatever the types.
+ * in fp32 whatever the types.  Where eps does not keep the quotient finite (it may be 0): with fp32 states sqrt(v) is at least
+ * 2^-63, the root of the smallest normal number, so that 0 / 0 is 0; with 8-bit states and eps below 2^-40 an element
+ * whose v is below 2^-120, which is held as 0, gets no update.
  *   param_dev      DEVICE, count elements of dtype (block_data of a W, a bias, ...), updated
  *   master_dev     DEVICE, count floats, or NULL: the parameter in fp32 (16-bit types only); it is updated and param_dev is
  *                  its nearest-even rounding.  Without one a 16-bit parameter is rounded up or down at random so that its mean
@@ -374,9 +376,9 @@ bsr_status bsr_spmm_static(const bsr_matrix* W, int64_t m, const void* X_dev, vo
  *                  with t_param_dev (else all 0): the tensor is a W's blocks [stored blocks][bs_r][bs_c], t_param_dev
  *                  (DEVICE) the blocks of its transpose as bsr_transpose_values() orders them, written anew by every step;
  *                  t_perm_host (HOST, read during bsr_adamw_create only) is bsr_transpose_pattern()'s perm
- * 8-bit states, in groups of 256 elements from a tensor's start.  m: an e4m3 number times a scale, rounded to nearest-even.
- * v: 0, or 2^(start + (code - 1) spacing), code 1 .. 255, from the group's smallest positive v (at least 2^-40 of the largest)
- * to its largest, rounded up or down at random so that its mean is kept (a step changes v by less than half the spacing:
+ * 8-bit states, in groups of 256 elements from a tensor's start.  m: an e4m3 number times a scale, rounded to nearest-even; 0
+ * where the group's largest is below 2^-100.  v: 0 for v below 2^-120, else 2^(start + (code - 1) spacing), code 1 .. 255, from
+ * the group's smallest such v (at least 2^-40 of the largest) to its largest, rounded up or down at random so that its mean is kept (a step changes v by less than half the spacing:
  * rounded to nearest it would stop).  The random numbers are a hash of seed, step, the tensor's place in the list and the
  * element's in the tensor: the same call on the same values gives the same bits.  The update itself sees m and v before
  * their rounding.

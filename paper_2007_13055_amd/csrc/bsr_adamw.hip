@@ -10,9 +10,10 @@
 //
 // 8-bit moments.  The 256 elements of a wavefront share three fp32 scales:
 //   m   e4m3 code times scale, scale = (largest |m|) / 448, rounded to nearest-even (a step changes m by a tenth of g - m,
-//       above half a step of the code).
+//       above half a step of the code).  All zeros where the largest is below 2^-100.
 //   v   code c: 0 is zero, 1 .. 255 are low * 2^((c - 1) spacing): evenly spaced in log2 v from the smallest positive v of the
-//       256 (at least 2^-40 of the largest) to the largest, so no positive v becomes 0, which would blow its update up.  A step
+//       256 (at least 2^-40 of the largest, and 2^-120) to the largest, so no larger v becomes 0, which would blow its update
+//       up (and where eps would not hold that back, the elements below get no update).  A step
 //       changes v by 0.1 % of g^2 - v (beta2 = 0.999), while codes are some 1 to 10 % apart: rounded to nearest, v would stop
 //       after its first few dozen steps.  Between two codes the upper one is taken with the probability that keeps the mean.
 // A 16-bit parameter without a master copy is rounded the same way: an update is mostly below half its last place.  The random
@@ -43,6 +44,7 @@ constexpr int kPasses = 4;                            // of a chunk, one where t
 constexpr int kChunk = kPasses * kPass;
 constexpr int kShared = 256;                          // elements that share scales: a wavefront's at a time
 constexpr float kTop8 = 448.f;                        // largest e4m3 number
+constexpr float kLeast = 0x1p-120f;                   // smallest v that 8 bits hold
 
 // A tensor as the kernels see it.
 struct tensor_desc {
@@ -223,8 +225,14 @@ __device__ __forceinline__ void step_pass(const tensor_desc& d, const step_now& 
         const float g = (float)in.g.v[e];
         m[e] = BITS == 8 ? weighted(h.beta1, m[e], h.one1, g) : fmaf(h.one1, g, m[e] * h.beta1);
         v[e] = BITS == 8 ? weighted(h.beta2, v[e], h.one2 * g, g) : fmaf(h.one2 * g, g, v[e] * h.beta2);
-        const float down = fmaf(__builtin_amdgcn_sqrtf(v[e]), h.root, h.eps);
-        p[e] = fmaf(-h.rate * m[e], __builtin_amdgcn_rcpf(down), (float)in.p.v[e] * h.keep);
+        float size = __builtin_amdgcn_sqrtf(v[e]);
+        // the root of a subnormal v would be 0 here; 2^-63, what it is below, keeps m / 0 (and 0 / 0) out where eps does not
+        if constexpr (BITS == 32) size = v[e] < 0x1p-126f ? 0x1p-63f : size;
+        float over = __builtin_amdgcn_rcpf(fmaf(size, h.root, h.eps));
+        // what is held as 0 in 8 bits, m not: below 2^-55 or so, and nothing beside a larger eps
+        if constexpr (BITS == 8)
+            if (h.eps < 0x1p-40f) over = v[e] < kLeast ? 0.f : over;   // uniform
+        p[e] = fmaf(-h.rate * m[e], over, (float)in.p.v[e] * h.keep);
         // fp32 numbers, of which the stored ones are roundings: left to itself the compiler rounds the exact sum to fp16
         asm("" : "+v"(p[e]));
         random[e] = mix(h.base + (uint32_t)(at + e));
@@ -249,7 +257,7 @@ __device__ __forceinline__ void step_pass(const tensor_desc& d, const step_now& 
             w.template store<FULL>(static_cast<float*>(d.v) + first + at, n);
         }
     } else {
-        constexpr float kLeast = 0x1p-120f, kMost = 0x1.fffffep+127f;
+        constexpr float kMost = 0x1.fffffep+127f;
         float top = 0.f;
         uint32_t top_v = 0, low_v = 0;                // low_v: the largest complement
 #pragma unroll
