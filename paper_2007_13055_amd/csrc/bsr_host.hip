@@ -282,7 +282,8 @@ static bsr_status create(bsr_matrix** out, int64_t n, int64_t k, int32_t bs_r, i
         ((uintptr_t)block_indices_dev & 3u) || ((uintptr_t)index_pointer_dev & 3u))
         return BSR_ERR_ALIGN;
     const int64_t R = n / bs_r;
-    if (workspace_bytes < plan_bytes(R, nnzb, bs_r, bs_c, k)) return BSR_ERR_WORKSPACE;
+    const size_t needed = plan_bytes(R, nnzb, bs_r, bs_c, k);
+    if (workspace_bytes < needed) return BSR_ERR_WORKSPACE;
 
     std::unique_ptr<bsr_matrix> held(new bsr_matrix());
     bsr_matrix* const W = held.get();
@@ -340,6 +341,7 @@ static bsr_status create(bsr_matrix** out, int64_t n, int64_t k, int32_t bs_r, i
         if (c > 8 && (double)c > 4.0 * W->mean_row_blocks) ++W->long_rows; else break;
     }
     W->row_order = static_cast<const int32_t*>(workspace_dev);
+    W->workspace_bytes = needed;
     W->row_desc = W->row_order + order_words;
     W->slot_blocks.resize((size_t)R);
     for (int64_t s = 0; s < R; ++s) W->slot_blocks[(size_t)s] = cnt[(size_t)W->staging[(size_t)s]];
@@ -706,7 +708,12 @@ bsr_status bsr_spmm_epilogue(const bsr_matrix* W, int64_t m, const void* X_dev, 
                              {e.bias_dev, (size_t)W->n * (e.bias_dtype == BSR_F32 ? 4 : 2)},
                              {e.residual_dev, ((size_t)(m - 1) * (size_t)ld + (size_t)W->n) * y_size},
                              {e.through_dev, out},
-                             {W->data, (size_t)W->nnzb * (size_t)W->bs_r * (size_t)W->bs_c * x_size}};
+                             {W->data, (size_t)W->nnzb * (size_t)W->bs_r * (size_t)W->bs_c * x_size},
+                             // what addresses are made of, in this call and the next
+                             {W->indices, (size_t)W->nnzb * sizeof(int32_t)},
+                             {W->indptr, ((size_t)W->R + 1) * sizeof(int32_t)},
+                             {W->row_order, W->workspace_bytes},
+                             {W->scratch, std::min(W->scratch_bytes, mfma_thin_scratch_bytes(W, m))}};
     const byte_range y{Y_dev, out}, z{e.z_dev, out};
     if (overlap(y, z)) return BSR_ERR_OVERLAP;
     for (const byte_range& r : in)

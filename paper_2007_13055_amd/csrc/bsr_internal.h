@@ -56,6 +56,7 @@ struct bsr_matrix {
     const void* data = nullptr;              // [nnzb][bs_r][bs_c]
     const int32_t* indices = nullptr;        // [nnzb]
     const int32_t* indptr = nullptr;         // [R+1]
+    size_t workspace_bytes = 0;              // of the workspace (it begins at row_order): what bsr_workspace_size() names
 
     // ---- plan (paper, Discussion: unequal block-rows need different treatment) ----
     // Block-rows ordered by stored-block count, longest first; a workgroup's slot s works on
