@@ -741,7 +741,9 @@ bsr_status bsr_adamw_step(const bsr_adamw* opt, const bsr_adamw_hyper* hyper, vo
     const bsr_adamw_hyper& y = *hyper;
     // (negated: NaN is refused too)
     if (!(y.beta1 >= 0 && y.beta1 < 1) || !(y.beta2 >= 0 && y.beta2 < 1) || !(y.eps >= 0) || (!y.step_dev && y.step < 1) ||
-        (!y.lr_dev && !(y.lr >= 0)) || (!y.grad_scale_dev && y.grad_scale != y.grad_scale)) return BSR_ERR_SHAPE;
+        (!y.lr_dev && !(y.lr >= 0))) return BSR_ERR_SHAPE;
+    const float size = std::fabs(y.grad_scale);       // its square has to be an fp32 number, with room for 1 - beta2
+    if (!y.grad_scale_dev && !(size == 0.f || (size >= 0x1p-40f && size <= 0x1p40f))) return BSR_ERR_SHAPE;
     for (const void* p : {(const void*)y.lr_dev, (const void*)y.grad_scale_dev})
         if (reinterpret_cast<uintptr_t>(p) & 3u) return BSR_ERR_ALIGN;
     if (reinterpret_cast<uintptr_t>(y.step_dev) & 7u) return BSR_ERR_ALIGN;

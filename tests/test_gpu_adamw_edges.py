@@ -103,3 +103,19 @@ def test_second_moments_that_8_bits_hold_as_zero(eps):
     assert bool(p.isfinite().all()) and bool((p[:256] == 0).all()) and bool((p[768:] == 0).all())
     # at most what two steps of the formula give for what is held at least: m hat / root of v hat <= 2 here
     assert bool(((p[256:512] - first[256:512]).abs() <= 2 * 2 * lr).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("scale", [2.0 ** -40, -1.0, 2.0 ** 40])
+def test_the_largest_and_smallest_scales(bits, scale):
+    """Gradients times the scale's inverse take the step that they take by themselves: a power of two moves exponents only."""
+    import torch
+    import paper_2007_13055_amd as lib
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    g = torch.randn(5000, generator=gen, device="cuda")
+    p, q = torch.zeros(5000, device="cuda"), torch.zeros(5000, device="cuda")
+    opt, one = lib.bsr_adamw_create([p], [g / scale], state_bits=bits), lib.bsr_adamw_create([q], [g], state_bits=bits)
+    for t in (1, 2):
+        lib.bsr_adamw_step(opt, t, grad_scale=scale, seed=1)
+        lib.bsr_adamw_step(one, t, seed=1)
+    assert torch.equal(p, q) and _same(_state(opt), _state(one))
