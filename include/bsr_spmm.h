@@ -182,9 +182,10 @@ typedef struct {
 } bsr_epilogue;
 
 /*
- * As bsr_spmm() -- the same kernels, choices (bsr_tune() included), streams and captures -- with `epilogue` (HOST, read
- * during the call).  Y and Z must overlap neither each other nor any input (a residual is not added in place), nor the
- * handle's arrays, its workspace and what has been lent as scratch.
+ * As bsr_spmm() -- the same kernels, choices, streams and captures; those of bsr_tune(), which times the product alone, too, but
+ * three or four blocks in flight are two here -- with `epilogue` (HOST, read during the call).  Y and Z must overlap neither
+ * each other nor any input (a residual is not added in place), nor the handle's arrays, its workspace and what has been lent
+ * as scratch.
  * Errors: as bsr_spmm(), plus NULL (epilogue), DTYPE (act, bias_dtype), SHAPE (residual_ld below n, or m * residual_ld
  * >= 2^37), ALIGN (a pointer not 16-byte aligned, or rows of a residual that are neither contiguous nor multiples of
  * 16 bytes apart), OVERLAP, DEVICE.

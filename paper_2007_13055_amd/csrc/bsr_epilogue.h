@@ -49,7 +49,11 @@ bsr_status with_epilogue(const spmm_args& a, F launch)
     const int32_t act = e.act;
     // Where neither is in the 256 MB cache behind the L2s, both ways take as long (within 3 % from 34 to 134 MB).  A residual that
     // the kernel that wrote it left there is read faster through the caches (two 105 MB ones in turn: 89 us, past them 99;
-    // 34 MB: 30 and 36), unless it pushes the result and itself out: two of 134 MB, 154 us, past the caches 136.
+    // 34 MB: 30 and 36), unless it pushes the result and itself out: two of 134 MB, 154 us, past the caches 136.  The rule knows
+    // the result's size alone.  A residual of 126 MB that the kernel before has just written, one set over and over (k = 1024,
+    // 10 %), is read either way as long with 64x64 f16 blocks (67 us) and faster through the caches with 32x32 f16 (79 us, past them 98),
+    // 16x16 f16 with fp32 results (68, 74) and fp32 blocks (134 MB, 32x32: 104, 116); two sets in turn of the same past
+    // them (f16 16x16 87, through them 94; 32x32 98, 99); 201 MB is faster past them in all of these (103 and 112, 146 and 162).
     const bool once = (int64_t)a.m * a.W->n * (a.y_dtype == BSR_F32 ? 4 : 2) > ((int64_t)112 << 20);
     return launch(epilogue_args{e.bias_dev, e.residual_dev, act == BSR_ACT_NONE ? nullptr : e.through_dev, e.z_dev,
                                 e.residual_ld ? e.residual_ld : a.W->n, act, e.bias_dtype == BSR_F32, once});
