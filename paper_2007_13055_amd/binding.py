@@ -164,14 +164,34 @@ def _dtype_name(t):
 
 
 class BsrMatrix:
-    """Owns the device tensors of one W (they must outlive the C handle) and the handle itself."""
+    """Owns the device tensors of one W (they must outlive the C handle) and the handle itself.
+
+    Products may run on any stream of its device, and it may be dropped while they are still to run.  A graph that one was
+    captured into reads its buffers at every replay: it must outlive the graph."""
 
     def __init__(self, handle, n, k, bs_r, bs_c, dtype, tensors):
         self.handle, self.n, self.k, self.bs_r, self.bs_c, self.dtype = handle, n, k, bs_r, bs_c, dtype
         self._tensors = tensors            # block_data, block_indices, index_pointer, workspace (device)
         self._scratch = None               # device scratch lent to the handle (see ensure_scratch)
         nnzb = int(tensors[0].shape[0]) if tensors[0].dim() == 3 else 0
-        self._core = _native_module().Core(handle.value, n, k, nnzb, bs_r, bs_c, _DTYPE_CODE[dtype])   # what the calls read
+        import torch
+        home = torch.cuda.current_stream()
+        self._streams = {home.cuda_stream: home}   # the one its tensors were made on, the others that have been given products
+        self._core = _native_module().Core(handle.value, n, k, nnzb, bs_r, bs_c, _DTYPE_CODE[dtype], home.cuda_stream)   # what the calls read
+
+    def _on_stream(self, address):
+        """A product on another stream than the last one, torch's current, is about to be queued: the memory of its plan is not
+        to be used again before that has run, even if nothing else holds it by then."""
+        if address in self._streams:
+            return
+        import torch
+        stream = torch.cuda.current_stream(self._tensors[0].device)
+        if stream.cuda_stream != address:
+            return                         # another device's stream: not this allocator's business
+        for t in (*self._tensors, self._scratch):
+            if t is not None:
+                t.record_stream(stream)
+        self._streams[address] = stream
 
     @property
     def block_data(self):
@@ -184,6 +204,8 @@ class BsrMatrix:
         have = self._scratch.numel() if self._scratch is not None else 0
         if need > have:
             self._scratch = torch.empty(need, dtype=torch.uint8, device=self._tensors[0].device)
+            for stream in self._streams.values():      # products on any of them may use it
+                self._scratch.record_stream(stream)
             st = load_library().bsr_set_scratch(self.handle, self._scratch.data_ptr(), self._scratch.numel())
             if st != 0:
                 raise BsrError(st, "bsr_set_scratch")
@@ -318,7 +340,7 @@ STATIC_SCRATCH_BYTES = 8 << 20
 def bsr_spmm_static(W: BsrMatrix, X, Y):
     """bsr_spmm for thin-block W on the library's built-in scratch array: nothing is allocated or lent, so Y
     must be given.  X (m, k) fp32, Y (m, n) fp32, both contiguous device tensors.  Returns Y."""
-    return _native.spmm_static(W._core, X, Y)
+    return _native.spmm_static(W, W._core, X, Y)
 
 
 def bsr_tune(W: BsrMatrix, X, Y=None, y_dtype=None, trials: int = 20):
@@ -393,20 +415,20 @@ class BsrAdamW:
         self.exp_avg, self.exp_avg_sq, self.scales = exp_avg, exp_avg_sq, scales
         self.handle, self.device, self._keep = None, None, []
         self._address, self._index, self._counts = 0, 0, tuple(int(p.numel()) for p in params)   # what the calls read
-        self._home, self._streams = 0, set()   # the stream its buffers were made on, the others that have been given work
+        self._known, self._streams = 0, set()   # the stream that was given work last; all, the one its buffers were made on first
 
     def _on_stream(self, address):
-        """Work on another stream than the home one, torch's current, is about to be queued: its buffers' memory is not to be
+        """Work on another stream than the last one, torch's current, is about to be queued: its buffers' memory is not to be
         used again before that has run, even if nothing else holds them by then."""
-        if address in self._streams:
-            return
-        import torch
-        stream = torch.cuda.current_stream(self.device)
-        for held in (self.params, self.grads, self.master, self.exp_avg, self.exp_avg_sq, self.scales, self._keep):
-            for t in held:
-                if isinstance(t, torch.Tensor):
-                    t.record_stream(stream)
-        self._streams.add(address)
+        if address not in self._streams:
+            import torch
+            stream = torch.cuda.current_stream(self.device)
+            for held in (self.params, self.grads, self.master, self.exp_avg, self.exp_avg_sq, self.scales, self._keep):
+                for t in held:
+                    if isinstance(t, torch.Tensor):
+                        t.record_stream(stream)
+            self._streams.add(address)
+        self._known = address
 
     def close(self):
         if self.handle:
@@ -505,7 +527,8 @@ def bsr_adamw_create(params, grads, *, weight_decay=0.0, state_bits=32, moments=
     if st != 0:
         raise BsrError(st, "bsr_adamw_create")
     opt.handle, opt._address, opt._index = handle, handle.value, device.index
-    opt._home = torch.cuda.current_stream().cuda_stream
+    opt._known = torch.cuda.current_stream().cuda_stream
+    opt._streams.add(opt._known)
     return opt
 
 
@@ -514,7 +537,7 @@ def bsr_adamw_step(opt: BsrAdamW, step, *, lr=1e-3, betas=(0.9, 0.999), eps=1e-8
 
     step counts from 1.  step, lr and grad_scale may be GPU tensors of one int64, fp32 and fp32, which a step captured into a
     graph reads at every replay; a grad_scale of 0 skips the step, and so does a step below 1 on the GPU.  seed: of the random roundings."""
-    _native.adamw_step(opt, opt._address, opt._index, opt._home, step, lr, betas[0], betas[1], eps, grad_scale, seed)
+    _native.adamw_step(opt, opt._address, opt._index, opt._known, step, lr, betas[0], betas[1], eps, grad_scale, seed)
 
 
 def bsr_adamw_moments(opt: BsrAdamW, dtype="f32", out=None):
@@ -524,5 +547,5 @@ def bsr_adamw_moments(opt: BsrAdamW, dtype="f32", out=None):
         import torch
         new = lambda p: torch.empty(p.numel(), dtype=_torch_dtype(dtype), device=opt.device)  # noqa: E731
         out = [(new(p), new(p)) for p in opt.params]
-    _native.adamw_moments(opt, opt._address, opt._index, opt._home, opt._counts, out if isinstance(out, list) else list(out))
+    _native.adamw_moments(opt, opt._address, opt._index, opt._known, opt._counts, out if isinstance(out, list) else list(out))
     return out

@@ -39,6 +39,7 @@ struct core_object {
     int64_t bs_r, bs_c;
     int dtype;
     size_t scratch_bytes;                             // what has been lent so far
+    uintptr_t known;                                  // the stream that was given work last, which the owner knows; to begin with its own
 };
 
 constexpr at::ScalarType kTypes[3] = {at::kFloat, at::kHalf, at::kBFloat16};
@@ -46,9 +47,10 @@ constexpr at::ScalarType kTypes[3] = {at::kFloat, at::kHalf, at::kBFloat16};
 int core_init(PyObject* self, PyObject* args, PyObject*)
 {
     core_object* c = reinterpret_cast<core_object*>(self);
-    unsigned long long handle = 0;
+    unsigned long long handle = 0, known = 0;
     long long n, k, nnzb, bs_r, bs_c;
-    if (!PyArg_ParseTuple(args, "KLLLLLi", &handle, &n, &k, &nnzb, &bs_r, &bs_c, &c->dtype)) return -1;
+    if (!PyArg_ParseTuple(args, "KLLLLLiK", &handle, &n, &k, &nnzb, &bs_r, &bs_c, &c->dtype, &known)) return -1;
+    c->known = (uintptr_t)known;
     c->handle = reinterpret_cast<bsr_matrix*>(handle);
     c->n = n; c->k = k; c->nnzb = nnzb; c->bs_r = bs_r; c->bs_c = bs_c;
     c->scratch_bytes = 0;
@@ -148,6 +150,20 @@ bool ensure_scratch(PyObject* W, const core_object* c, int64_t m)
 
 void* stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
+// A call on another stream than the one before it (`known`; to begin with the one on which the owner's buffers -- plan, moments --
+// were made): the owner has the allocator told, once a stream (its _on_stream), or that would give them away, as soon as the
+// owner is dropped, to what their own stream is given next, while this call is still to read its tables.  False with an error set.
+bool told_of_stream(PyObject* owner, uintptr_t known, uintptr_t* now_known = nullptr)
+{
+    const uintptr_t now = reinterpret_cast<uintptr_t>(stream());
+    if (now == known) return true;
+    PyObject* done = PyObject_CallMethod(owner, "_on_stream", "K", (unsigned long long)now);
+    if (!done) return false;
+    Py_DECREF(done);
+    if (now_known) *now_known = now;
+    return true;
+}
+
 // A result: through torch's dispatcher, so that its modes and its deterministic fill see it.
 at::Tensor result(at::IntArrayRef shape, int code, const at::Tensor& like)
 {
@@ -175,7 +191,7 @@ PyObject* spmm(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     const int y_code = name_code(a[4], c->dtype);
     if (y_code < 0 || !ensure_scratch(a[0], c, m)) return nullptr;
     const long path = PyLong_AsLong(a[5]);
-    if (path == -1 && PyErr_Occurred()) return nullptr;
+    if ((path == -1 && PyErr_Occurred()) || !told_of_stream(a[0], c->known, &c->known)) return nullptr;
     at::Tensor fresh;
     PyObject* out = a[3];
     if (out == Py_None) {
@@ -200,21 +216,22 @@ PyObject* spmm(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
-// spmm_static(core, X, Y) -> Y
+// spmm_static(W, core, X, Y) -> Y
 PyObject* spmm_static(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
-    if (nargs != 3) return value_error("spmm_static takes 3 arguments");
-    core_object* c = core_of(a[0]);
+    if (nargs != 4) return value_error("spmm_static takes 4 arguments");
+    core_object* c = core_of(a[1]);
     const at::Tensor *X = nullptr, *Y = nullptr;
-    if (!c || !tensor_of(a[1], "X", &X) || !tensor_of(a[2], "Y", &Y)) return nullptr;
-    const int x_code = type_code(*X, a[1]);
+    if (!c || !tensor_of(a[2], "X", &X) || !tensor_of(a[3], "Y", &Y)) return nullptr;
+    const int x_code = type_code(*X, a[2]);
     if (x_code < 0) return nullptr;
     if (X->dim() != 2 || X->size(1) != c->k || x_code != c->dtype || !X->is_contiguous())
         return value_error("X must be a contiguous (m, k) tensor of W's dtype");
     const int64_t m = X->size(0);
     if (!dims2(*Y, m, c->n) || Y->scalar_type() != at::kFloat || !Y->is_contiguous())
         return value_error("Y must be a contiguous (m, n) fp32 tensor");
+    if (!told_of_stream(a[0], c->known, &c->known)) return nullptr;
     const void* xp = X->data_ptr();
     void* yp = Y->data_ptr();
     bsr_status st;
@@ -223,8 +240,8 @@ PyObject* spmm_static(PyObject*, PyObject* const* a, Py_ssize_t nargs)
         st = g_spmm_static(c->handle, m, xp, yp, BSR_F32, stream());
     }
     if (st != BSR_OK) return failed(st, "bsr_spmm_static");
-    Py_INCREF(a[2]);
-    return a[2];
+    Py_INCREF(a[3]);
+    return a[3];
     END_HANDLE_TH_ERRORS
 }
 
@@ -248,7 +265,7 @@ PyObject* sddmm(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     const int d_code = name_code(a[5], c->dtype);
     if (d_code < 0) return nullptr;
     const int lend = PyObject_IsTrue(a[6]);
-    if (lend < 0 || (lend && !ensure_scratch(a[0], c, m))) return nullptr;
+    if (lend < 0 || (lend && !ensure_scratch(a[0], c, m)) || !told_of_stream(a[0], c->known, &c->known)) return nullptr;
     at::Tensor fresh;
     PyObject* out = a[4];
     if (out == Py_None) {
@@ -374,7 +391,7 @@ PyObject* spmm_epilogue(PyObject*, PyObject* const* a, Py_ssize_t nargs)
         !matrix_of(a[3], "Y", m, c->n, y_code, device, &Y)) return nullptr;
     if (through) ep.through_dev = through->data_ptr();
     const int keep_z = PyObject_IsTrue(a[10]);
-    if (keep_z < 0 || !ensure_scratch(a[0], c, m)) return nullptr;
+    if (keep_z < 0 || !ensure_scratch(a[0], c, m) || !told_of_stream(a[0], c->known, &c->known)) return nullptr;
     at::Tensor fresh_y, fresh_z;
     if (!Y) {
         fresh_y = result({m, c->n}, y_code, *X);
@@ -506,33 +523,26 @@ long long integer(PyObject* o)                        // whatever int() takes
 }
 double real(PyObject* o) { return PyFloat_AsDouble(o); }
 
+// Of an optimizer's owner, as above; a call that the entry point refuses (closed, or not on its device) is not told of.
+// (Its owner keeps the stream that it knows.)
+bool told_of_stream(PyObject* owner, const bsr_adamw* opt, int device, PyObject* known)
+{
+    const unsigned long long address = PyLong_AsUnsignedLongLong(known);
+    if (PyErr_Occurred()) return false;
+    return !opt || (int)c10::hip::current_device() != device || told_of_stream(owner, (uintptr_t)address);
+}
+
 const bsr_adamw* adamw_of(PyObject* address)          // 0: closed, which the entry points refuse
 {
     return reinterpret_cast<const bsr_adamw*>(PyLong_AsUnsignedLongLong(address));
 }
 
-// A call on another stream than `home`, on which the handle's buffers were made: the owner has the allocator told
-// (BsrAdamW._on_stream), or it would give them away, as soon as the owner is dropped, to what home is given next, while this
-// call is still to read its tables.  False with an error set.
-bool told_of_stream(PyObject* owner, int device, PyObject* home)
-{
-    const unsigned long long made_on = PyLong_AsUnsignedLongLong(home);
-    if (PyErr_Occurred()) return false;
-    if ((int)c10::hip::current_device() != device) return true;   // refused by the entry point
-    const unsigned long long now = reinterpret_cast<uintptr_t>(stream());
-    if (now == made_on) return true;
-    PyObject* done = PyObject_CallMethod(owner, "_on_stream", "K", now);
-    if (!done) return false;
-    Py_DECREF(done);
-    return true;
-}
-
-// adamw_step(owner, handle's address, device, stream it was made on, step, lr, beta1, beta2, eps, grad_scale, seed)
+// adamw_step(owner, handle's address, device, stream the owner knows, step, lr, beta1, beta2, eps, grad_scale, seed)
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
     if (nargs != 11) return value_error("adamw_step takes 11 arguments");
-    PyObject *owner = a[0], *home = a[3];
+    PyObject *owner = a[0], *known = a[3];
     const bsr_adamw* opt = adamw_of(a[1]);
     const int device = (int)PyLong_AsLong(a[2]);
     if (PyErr_Occurred()) return nullptr;
@@ -548,7 +558,7 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     h.beta2 = real(a[5]);
     h.eps = real(a[6]);
     h.seed = (uint32_t)PyLong_AsUnsignedLongLongMask(a[8]);
-    if (PyErr_Occurred() || (opt && !told_of_stream(owner, device, home))) return nullptr;
+    if (PyErr_Occurred() || !told_of_stream(owner, opt, device, known)) return nullptr;
     bsr_status st;
     {
         pybind11::gil_scoped_release no_gil;
@@ -559,13 +569,13 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
-// adamw_moments(owner, handle's address, device, stream it was made on, tuple of the tensors' elements, list of pairs of tensors)
+// adamw_moments(owner, handle's address, device, stream the owner knows, tuple of the tensors' elements, list of pairs of tensors)
 PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t nargs)
 {
     HANDLE_TH_ERRORS
     if (nargs != 6 || !PyTuple_Check(a[4]) || !PyList_Check(a[5]))
         return value_error("adamw_moments takes an owner, an address, a device, a stream, a tuple and a list");
-    PyObject *owner = a[0], *home = a[3];
+    PyObject *owner = a[0], *known = a[3];
     const bsr_adamw* opt = adamw_of(a[1]);
     const int device = (int)PyLong_AsLong(a[2]);
     if (PyErr_Occurred()) return nullptr;
@@ -590,7 +600,7 @@ PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t nargs)
             out[k].push_back(t->data_ptr());
         }
     }
-    if (opt && !told_of_stream(owner, device, home)) return nullptr;
+    if (!told_of_stream(owner, opt, device, known)) return nullptr;
     out[0].push_back(nullptr);                        // an address for an empty list
     out[1].push_back(nullptr);
     bsr_status st;
@@ -629,7 +639,7 @@ PyObject* bind(PyObject*, PyObject* args)
 PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, "Take the C library's entry points and the error class."},
     {"spmm", reinterpret_cast<PyCFunction>(spmm), METH_FASTCALL, "spmm(W, core, X, Y, y_dtype, path) -> Y"},
-    {"spmm_static", reinterpret_cast<PyCFunction>(spmm_static), METH_FASTCALL, "spmm_static(core, X, Y) -> Y"},
+    {"spmm_static", reinterpret_cast<PyCFunction>(spmm_static), METH_FASTCALL, "spmm_static(W, core, X, Y) -> Y"},
     {"sddmm", reinterpret_cast<PyCFunction>(sddmm), METH_FASTCALL, "sddmm(W, core, G, X, D, d_dtype, lend) -> D"},
     {"spmm_epilogue", reinterpret_cast<PyCFunction>(spmm_epilogue), METH_FASTCALL,
      "spmm_epilogue(W, core, X, Y, y_dtype, bias, act, residual, through, Z, keep_z) -> Y or (Y, Z)"},
