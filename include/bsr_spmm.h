@@ -109,7 +109,8 @@ bsr_status bsr_workspace_size(int64_t n, int64_t k, int32_t bs_r, int32_t bs_c, 
  *                                                  this call only
  *   workspace_dev      DEVICE, at least bsr_workspace_size() bytes, 16-byte aligned
  * The four device buffers stay owned by the caller and must outlive the handle, the products that are
- * still to run (on any stream) and the graphs that hold some; their contents (block values included) may change between products as long as the pattern does not.
+ * still to run (on any stream) and the graphs that hold some; their contents (block values included) may
+ * change between products as long as the pattern does not.
  * nnzb == 0 is valid (Y becomes all zeros); then block_data_dev / block_indices_* may be NULL.
  * On error *out is set to NULL.
  */
