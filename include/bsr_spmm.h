@@ -442,6 +442,166 @@ bsr_status bsr_adamw_moments(const bsr_adamw* opt, bsr_dtype dtype, void* const*
 void bsr_adamw_destroy(bsr_adamw* opt);
 
 /*
+ * A pair of projections whose results gate one another: Wg and Wu, (n, k) each, in blocks of the same shape, as ONE handle W
+ * of 2n rows in which block-row 2r is block-row r of Wg and block-row 2r + 1 that of Wu.  The halves of a result are then made
+ * by neighbouring block-rows, and W stays a matrix like any other: bsr_sddmm(W, dZ, X) is the gradient of its blocks,
+ * bsr_spmm(handle of W^T, dZ) that of X, bsr_adamw_step and bsr_muon_step update it.
+ *     z_g = X Wg^T + bias_g      z_u = X Wu^T + bias_u      H[i][j] = act(z_g[i][j]) z_u[i][j]
+ * z, biases and gradients of both are kept in W's order, bs_r columns of one half and bs_r of the other in turn: with u = bs_r
+ * and j = r u + a, column 2 r u + a is z_g's, column 2 r u + u + a z_u's.  All of it is fp32 arithmetic on the sums; H and Z
+ * are rounded once, to nearest-even, and H is made of the z before that rounding.
+ *   H_dev          DEVICE, m*n elements of h_dtype (W's dtype or BSR_F32), every one written
+ *   gated (HOST)   act; bias_dev: DEVICE, 2n elements of bias_dtype (W's dtype or BSR_F32), or NULL; z_dev: DEVICE, Z, m*2n
+ *                  elements of h_dtype, every one written, or NULL
+ *   workspace_dev  DEVICE, bsr_spmm_gated_workspace_size() bytes (0: none, it may be NULL), overwritten.  Calls that may run at
+ *                  the same time, replayed graphs among them, need one each
+ * Streams, captures and choices of kernel as bsr_spmm().  H, Z and the workspace must overlap neither one another nor an input,
+ * nor the handle's arrays, its workspace and what has been lent as scratch.
+ * Errors: as bsr_spmm_epilogue(), plus SHAPE (an odd number of block-rows) and WORKSPACE.
+ */
+typedef struct {
+    bsr_act act;
+    bsr_dtype bias_dtype;
+    const void* bias_dev;
+    void* z_dev;
+} bsr_gated;
+bsr_status bsr_spmm_gated_workspace_size(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype, size_t* bytes);
+bsr_status bsr_spmm_gated(const bsr_matrix* W, int64_t m, const void* X_dev, void* H_dev, bsr_dtype h_dtype, const bsr_gated* gated,
+                          void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Its gradient, from G = dL/dH and the Z that was kept:
+ *     dz_g = G z_u act'(z_g)      dz_u = G act(z_g)      db[j] = sum over i of dZ[i][j]
+ * One pass over G and Z; the sums are fp32, of dZ before its rounding, and added in a fixed order (no atomics).
+ *   unit           columns of a half that stand together in Z and dZ: W's bs_r; it divides n
+ *   G_dev          DEVICE, m*n elements of g_dtype      Z_dev  DEVICE, m*2n elements of g_dtype
+ *   DZ_dev         DEVICE, m*2n elements of dz_dtype (g_dtype, or any type where g_dtype is BSR_F32), or NULL; it may be Z_dev
+ *                  itself where the types are the same
+ *   DB_dev         DEVICE, 2n floats, or NULL (not both NULL); m == 0: zeros
+ *   workspace_dev  DEVICE, bsr_gated_backward_workspace_size() bytes (0: none), overwritten; read only where DB_dev is given.
+ *                  Calls that may run at the same time, replayed graphs among them, need one each.
+ * Asynchronous on hip_stream.  Errors: NULL, SHAPE (m or n negative, unit below 1 or no divisor of n, m >= 2^30, n >= 2^27, or
+ * m*n >= 2^39), DTYPE, ALIGN (a pointer not 16-byte aligned), WORKSPACE, OVERLAP, HIP.
+ */
+bsr_status bsr_gated_backward_workspace_size(int64_t m, int64_t n, int32_t unit, size_t* bytes);
+bsr_status bsr_gated_backward(int64_t m, int64_t n, int32_t unit, bsr_act act, bsr_dtype g_dtype, const void* G_dev, const void* Z_dev,
+                              bsr_dtype dz_dtype, void* DZ_dev, float* DB_dev, void* workspace_dev, size_t workspace_bytes,
+                              void* hip_stream);
+
+/*
+ * The norms around a block of a network whose blocks add to a stream S of hidden states: what the block's result B meets on
+ * its way into the stream, and what the next block is given, in one pass.
+ *     b = post(B)        S'[i][j] = stream_scale S[i][j] + branch_scale gate[j] b[i][j]        U = pre(S')
+ * post, pre: none; x / sqrt(mean(x^2) + eps); (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps), over a row, times a weight, plus
+ * a bias.  fp32 arithmetic; U is made of S' before its rounding; each result is rounded once, to nearest-even.
+ *   S_dev          DEVICE, m*n elements of s_dtype (b_dtype or BSR_F32)
+ *   B_dev          DEVICE, m*n elements of b_dtype, or NULL: no block has run yet (S' = stream_scale S; post and gate are not looked at)
+ *   S_out_dev      DEVICE, S', m*n elements of s_dtype, or NULL; it may be S_dev itself
+ *   U_dev          DEVICE, U, m*n elements of b_dtype, or NULL (always where pre is none; not both NULL); it may be B_dev itself
+ *   how (HOST)     weights, biases and gate: DEVICE, n elements of w_dtype (b_dtype or BSR_F32), or NULL (1, 0 and 1)
+ * A NaN or an infinity reaches its own row only.  Mean squares are fp32 numbers: values beyond 2^63 in size count as infinite
+ * there, and with eps = 0 rows whose mean square is below 2^-126 have no defined norm.
+ * Asynchronous on hip_stream.  Errors: NULL, SHAPE (m or n negative, m >= 2^30, n > 16384, eps negative), DTYPE (an unknown norm
+ * too), ALIGN (a pointer not 16-byte aligned), UNSUPPORTED (U_dev without pre), OVERLAP, HIP.
+ */
+typedef enum { BSR_NORM_NONE = 0, BSR_NORM_RMS = 1, BSR_NORM_LAYER = 2 } bsr_norm;
+typedef struct {
+    bsr_norm post, pre;
+    bsr_dtype w_dtype;
+    const void* post_weight_dev;
+    const void* post_bias_dev;
+    const void* gate_dev;
+    const void* pre_weight_dev;
+    const void* pre_bias_dev;
+    double eps;
+    float stream_scale, branch_scale;
+} bsr_residual;
+bsr_status bsr_residual_norm(int64_t m, int64_t n, bsr_dtype s_dtype, const void* S_dev, bsr_dtype b_dtype, const void* B_dev,
+                             void* S_out_dev, void* U_dev, const bsr_residual* how, void* hip_stream);
+
+/*
+ * Its gradient, from GS = dL/dS' (what reaches S' otherwise) and GU = dL/dU, at S' as it was stored: with g = GS + pre'(GU),
+ *     dS = stream_scale g      dB = post'(branch_scale gate g)
+ * and, summed over the rows, the gradients of the five vectors.
+ *   S_dev          DEVICE, S', m*n elements of s_dtype (not read, may be NULL, where pre is none)
+ *   B_dev          as given to bsr_residual_norm(); NULL: DB_dev and the gradients of post and gate have to be NULL
+ *   GS_dev, GU_dev DEVICE, m*n elements of s_dtype and b_dtype, or NULL (zeros; GU_dev always where pre is none)
+ *   DS_dev, DB_dev DEVICE, m*n elements of s_dtype and b_dtype, or NULL: not wanted; DS_dev may be GS_dev or S_dev itself, DB_dev
+ *                  GU_dev or B_dev
+ *   grads (HOST)   DEVICE, n floats each, or NULL: not wanted (also for a vector that is not there: it counts as 1 or 0); m == 0:
+ *                  zeros.  fp32 sums in a fixed order (no atomics)
+ *   workspace_dev  DEVICE, bsr_residual_norm_backward_workspace_size() bytes, overwritten; it may be NULL where no sum is
+ *                  wanted and n <= 8192.  Calls that may run at the same time, replayed graphs among them, need one each.
+ * Asynchronous on hip_stream.  Errors: as bsr_residual_norm(), plus WORKSPACE, UNSUPPORTED (what belongs to a norm or a branch
+ * that is not there) and NULL (nothing wanted).
+ */
+typedef struct {
+    float* post_weight_dev;
+    float* post_bias_dev;
+    float* gate_dev;
+    float* pre_weight_dev;
+    float* pre_bias_dev;
+} bsr_residual_grads;
+bsr_status bsr_residual_norm_backward_workspace_size(int64_t m, int64_t n, size_t* bytes);
+bsr_status bsr_residual_norm_backward(int64_t m, int64_t n, bsr_dtype s_dtype, const void* S_dev, bsr_dtype b_dtype, const void* B_dev,
+                                      const void* GS_dev, const void* GU_dev, void* DS_dev, void* DB_dev, const bsr_residual* how,
+                                      const bsr_residual_grads* grads, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * One step over the stored blocks of many matrices whose update is orthogonalised block by block: every singular value of a
+ * block's update is brought near 1 by Newton-Schulz steps, products alone, in fp32 on the matrix cores.  With g the gradient
+ * times grad_scale,
+ *     M = momentum M + g                 V = g + momentum M (nesterov) or M
+ *     X = V / (|V| + eps), |V| the block's Frobenius norm;  ns_steps times  X = a X + b (X X^T) X + c (X X^T)^2 X
+ *     p = p (1 - lr weight_decay) - lr scale X
+ * Biases and other tensors that are not blocks take bsr_adamw_step().
+ *   blocks, bs_r, bs_c   the tensor: a W's block_data, sides from 1 to 64 (a side of 1: V / |V| times what the steps make of 1)
+ *   param_dev, master_dev, grad_dev, t_param_dev, t_perm_host, weight_decay   as in bsr_adamw_tensor: a 16-bit parameter without
+ *                        a master copy is rounded at random so that its mean is kept, by a hash of seed, step, the tensor's
+ *                        place in the list and the element's in the tensor
+ *   momentum_dev         DEVICE, M, a float an element, updated; zeros to begin with
+ *   scale                of the update
+ * Not finite gradients reach M there and p in their whole block; a loop that scales its loss looks for them and sets
+ * grad_scale_dev to 0, for which everything stays as it is.  A block of zeros has an update of 0 (eps > 0).
+ */
+typedef struct bsr_muon bsr_muon;       /* opaque handle: the list of tensors (device pointers not owned) */
+typedef struct {
+    int64_t blocks;
+    int32_t bs_r, bs_c;
+    bsr_dtype dtype, grad_dtype;
+    void* param_dev;
+    float* master_dev;
+    const void* grad_dev;
+    float* momentum_dev;
+    void* t_param_dev;
+    const int32_t* t_perm_host;
+    float weight_decay, scale;
+} bsr_muon_tensor;
+
+/* A step's settings; the *_dev members as in bsr_adamw_hyper (step: of the random roundings alone). */
+typedef struct {
+    double lr, momentum, eps;           /* lr >= 0, 0 <= momentum < 1, eps > 0 (2^-100 to 1) */
+    float a, b, c;                      /* of the Newton-Schulz steps */
+    int32_t ns_steps, nesterov;         /* 0 to 16 steps */
+    int64_t step;                       /* t >= 1 */
+    float grad_scale;                   /* 1: gradients as they are; 0: the step is skipped (else 2^-40 to 2^40 in size) */
+    uint32_t seed;
+    const float* lr_dev;
+    const int64_t* step_dev;
+    const float* grad_scale_dev;
+} bsr_muon_hyper;
+
+/*
+ * bsr_muon_workspace_size, bsr_muon_create, bsr_muon_step, bsr_muon_destroy: as bsr_adamw_*.  Errors: as there; SHAPE for sides
+ * beyond 64, too.
+ */
+bsr_status bsr_muon_workspace_size(int64_t n_tensors, const bsr_muon_tensor* tensors, size_t* bytes);
+bsr_status bsr_muon_create(bsr_muon** out, int64_t n_tensors, const bsr_muon_tensor* tensors, void* workspace_dev, size_t workspace_bytes,
+                           void* hip_stream);
+bsr_status bsr_muon_step(const bsr_muon* opt, const bsr_muon_hyper* hyper, void* hip_stream);
+void bsr_muon_destroy(bsr_muon* opt);
+
+/*
  * Measurement helper for the benchmark, not part of the product (no passage of the paper defines it): one
  * launch of a kernel that only issues independent matrix-core instructions of the given input type
  * (8 accumulator chains per wavefront, 32 wavefronts per CU, `iters` rounds, no memory traffic), so that

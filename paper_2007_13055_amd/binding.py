@@ -1,7 +1,8 @@
 """Binding for libbsr_spmm.so: same names as the C entry points, marshalling only.
 
 What is called once a product or a step (bsr_spmm, bsr_spmm_ex, bsr_spmm_static, bsr_spmm_epilogue, bsr_epilogue_backward,
-bsr_sddmm, bsr_adamw_step, bsr_adamw_moments) goes through the native module _binding, whose calls cost about what the launch
+bsr_spmm_gated, bsr_gated_backward, bsr_residual_norm, bsr_residual_norm_backward, bsr_sddmm, bsr_adamw_step, bsr_adamw_moments,
+bsr_muon_step) goes through the native module _binding, whose calls cost about what the launch
 itself does; everything called once per matrix goes through ctypes."""
 from __future__ import annotations
 
@@ -40,6 +41,39 @@ class AdamWHyper(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
                 ("step", ctypes.c_int64), ("grad_scale", ctypes.c_float), ("seed", ctypes.c_uint32),
                 ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p), ("grad_scale_dev", ctypes.c_void_p)]
+
+
+class Gated(ctypes.Structure):
+    """bsr_gated of the C header."""
+    _fields_ = [("act", ctypes.c_int), ("bias_dtype", ctypes.c_int), ("bias_dev", ctypes.c_void_p), ("z_dev", ctypes.c_void_p)]
+
+
+class Residual(ctypes.Structure):
+    """bsr_residual of the C header."""
+    _fields_ = [("post", ctypes.c_int), ("pre", ctypes.c_int), ("w_dtype", ctypes.c_int), ("post_weight_dev", ctypes.c_void_p),
+                ("post_bias_dev", ctypes.c_void_p), ("gate_dev", ctypes.c_void_p), ("pre_weight_dev", ctypes.c_void_p),
+                ("pre_bias_dev", ctypes.c_void_p), ("eps", ctypes.c_double), ("stream_scale", ctypes.c_float), ("branch_scale", ctypes.c_float)]
+
+
+class ResidualGrads(ctypes.Structure):
+    """bsr_residual_grads of the C header."""
+    _fields_ = [("post_weight_dev", ctypes.c_void_p), ("post_bias_dev", ctypes.c_void_p), ("gate_dev", ctypes.c_void_p),
+                ("pre_weight_dev", ctypes.c_void_p), ("pre_bias_dev", ctypes.c_void_p)]
+
+
+class MuonTensor(ctypes.Structure):
+    """bsr_muon_tensor of the C header."""
+    _fields_ = [("blocks", ctypes.c_int64), ("bs_r", ctypes.c_int32), ("bs_c", ctypes.c_int32), ("dtype", ctypes.c_int), ("grad_dtype", ctypes.c_int),
+                ("param_dev", ctypes.c_void_p), ("master_dev", ctypes.c_void_p), ("grad_dev", ctypes.c_void_p), ("momentum_dev", ctypes.c_void_p),
+                ("t_param_dev", ctypes.c_void_p), ("t_perm_host", ctypes.c_void_p), ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class MuonHyper(ctypes.Structure):
+    """bsr_muon_hyper of the C header."""
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("eps", ctypes.c_double), ("a", ctypes.c_float), ("b", ctypes.c_float),
+                ("c", ctypes.c_float), ("ns_steps", ctypes.c_int32), ("nesterov", ctypes.c_int32), ("step", ctypes.c_int64),
+                ("grad_scale", ctypes.c_float), ("seed", ctypes.c_uint32), ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p),
+                ("grad_scale_dev", ctypes.c_void_p)]
 
 
 _lib = None
@@ -95,6 +129,19 @@ def load_library():
     lib.bsr_adamw_moments.argtypes = [vp, ctypes.c_int, ctypes.POINTER(vp), ctypes.POINTER(vp), vp]
     lib.bsr_adamw_destroy.argtypes = [vp]
     lib.bsr_adamw_destroy.restype = None
+    lib.bsr_spmm_gated_workspace_size.argtypes = [vp, i64, ctypes.c_int, ctypes.POINTER(sz)]
+    lib.bsr_spmm_gated.argtypes = [vp, i64, vp, vp, ctypes.c_int, ctypes.POINTER(Gated), vp, sz, vp]
+    lib.bsr_gated_backward_workspace_size.argtypes = [i64, i64, i32, ctypes.POINTER(sz)]
+    lib.bsr_gated_backward.argtypes = [i64, i64, i32, ctypes.c_int, ctypes.c_int, vp, vp, ctypes.c_int, vp, vp, vp, sz, vp]
+    lib.bsr_residual_norm.argtypes = [i64, i64, ctypes.c_int, vp, ctypes.c_int, vp, vp, vp, ctypes.POINTER(Residual), vp]
+    lib.bsr_residual_norm_backward_workspace_size.argtypes = [i64, i64, ctypes.POINTER(sz)]
+    lib.bsr_residual_norm_backward.argtypes = [i64, i64, ctypes.c_int, vp, ctypes.c_int, vp, vp, vp, vp, vp, ctypes.POINTER(Residual),
+                                               ctypes.POINTER(ResidualGrads), vp, sz, vp]
+    lib.bsr_muon_workspace_size.argtypes = [i64, ctypes.POINTER(MuonTensor), ctypes.POINTER(sz)]
+    lib.bsr_muon_create.argtypes = [ctypes.POINTER(vp), i64, ctypes.POINTER(MuonTensor), vp, sz, vp]
+    lib.bsr_muon_step.argtypes = [vp, ctypes.POINTER(MuonHyper), vp]
+    lib.bsr_muon_destroy.argtypes = [vp]
+    lib.bsr_muon_destroy.restype = None
     lib.bsr_probe_mfma.argtypes = [ctypes.c_int, i32, vp, vp, ctypes.POINTER(ctypes.c_double)]
     lib.bsr_probe_mfma.restype = ctypes.c_int
     lib.bsr_status_string.argtypes = [ctypes.c_int]
@@ -103,7 +150,9 @@ def load_library():
               "bsr_query_path", "bsr_scratch_size", "bsr_set_scratch", "bsr_tune", "bsr_tune_result",
               "bsr_transpose_pattern", "bsr_transpose_values", "bsr_sddmm", "bsr_spmm_epilogue",
               "bsr_epilogue_backward_workspace_size", "bsr_epilogue_backward", "bsr_adamw_workspace_size", "bsr_adamw_create",
-              "bsr_adamw_step", "bsr_adamw_moments"):
+              "bsr_adamw_step", "bsr_adamw_moments", "bsr_spmm_gated_workspace_size", "bsr_spmm_gated", "bsr_gated_backward_workspace_size",
+              "bsr_gated_backward", "bsr_residual_norm", "bsr_residual_norm_backward_workspace_size", "bsr_residual_norm_backward",
+              "bsr_muon_workspace_size", "bsr_muon_create", "bsr_muon_step"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -125,7 +174,10 @@ def _native_module():
     _binding.bind(*(ctypes.cast(f, ctypes.c_void_p).value
                     for f in (lib.bsr_spmm_ex, lib.bsr_spmm_static, lib.bsr_sddmm_ws, lib.bsr_scratch_size,
                               lib.bsr_sddmm_workspace_size, lib.bsr_spmm_epilogue, lib.bsr_epilogue_backward,
-                              lib.bsr_epilogue_backward_workspace_size, lib.bsr_adamw_step, lib.bsr_adamw_moments)), BsrError)
+                              lib.bsr_epilogue_backward_workspace_size, lib.bsr_adamw_step, lib.bsr_adamw_moments,
+                              lib.bsr_spmm_gated, lib.bsr_spmm_gated_workspace_size, lib.bsr_gated_backward, lib.bsr_gated_backward_workspace_size,
+                              lib.bsr_residual_norm, lib.bsr_residual_norm_backward, lib.bsr_residual_norm_backward_workspace_size,
+                              lib.bsr_muon_step)), BsrError)
     _native = _binding
     return _native
 
@@ -332,6 +384,89 @@ def bsr_epilogue_backward(G, Z=None, act="none", DZ=None, dz_dtype=None, DB=None
     Without an activation dZ is G: G is returned unless its type changes or a DZ is given.  need_dz, need_db: leave out the
     one or the other (None in its place)."""
     return _native_module().epilogue_backward(G, Z, act, DZ, dz_dtype, DB, need_dz, need_db)
+
+
+def bsr_gated_arrays(gate, up):
+    """(block_data, block_indices, index_pointer) of the one matrix of 2n rows that holds two of the same block shape and sizes,
+    a block-row of gate's and one of up's in turn (for bsr_create, bsr_create_transposed).  gate, up: such triples, numpy or
+    torch; the blocks stay where and of the type that they are."""
+    import torch
+    halves, starts = [], []
+    for data, idx, ptr in (gate, up):
+        data = data if isinstance(data, torch.Tensor) else np.asarray(data)
+        if data.ndim != 3:
+            raise ValueError("block_data must be (nnzb, bs_r, bs_c)")
+        idx, ptr = (_i32(v.cpu().numpy() if isinstance(v, torch.Tensor) else v) for v in (idx, ptr))
+        if len(idx) != len(data) or len(ptr) < 1 or ptr[0] != 0 or ptr[-1] != len(idx) or np.any(np.diff(ptr) < 0):
+            raise ValueError("index_pointer must start at 0, never decrease and end at the number of blocks")
+        halves.append((data, idx, np.diff(ptr).astype(np.int64)))
+        starts.append(ptr[:-1].astype(np.int64))
+    (gd, gi, gc), (ud, ui, uc) = halves
+    if gd.shape[1:] != ud.shape[1:] or gd.dtype != ud.dtype or isinstance(gd, torch.Tensor) != isinstance(ud, torch.Tensor) or len(gc) != len(uc):
+        raise ValueError("gate and up must have the same block-rows, block shape and type")
+    counts = np.stack((gc, uc), 1).reshape(-1)
+    first = np.stack((starts[0], starts[1] + len(gi)), 1).reshape(-1)     # of each block-row, in gate's blocks and up's behind them
+    ptr = np.zeros(len(counts) + 1, dtype=np.int32)
+    np.cumsum(counts, out=ptr[1:])
+    order = np.repeat(first - ptr[:-1], counts) + np.arange(int(ptr[-1]))
+    idx = np.concatenate((gi, ui))[order]
+    if isinstance(gd, torch.Tensor):
+        return torch.cat((gd, ud))[torch.from_numpy(order).to(gd.device)], idx, ptr
+    return np.concatenate((gd, ud))[order], idx, ptr
+
+
+def bsr_spmm_gated(W: BsrMatrix, X, H=None, h_dtype=None, *, bias=None, act="silu", Z=None, keep_z=False):
+    """H = act(X Wg^T + bias_g) * (X Wu^T + bias_u), H (m, n): W (2n, k) from bsr_gated_arrays, a block-row of Wg and one of Wu
+    in turn; bias (2n,) in that order, of W's dtype or fp32.
+
+    act "none" | "relu" | "gelu" | "gelu_tanh" | "silu".  Z: a buffer (m, 2n) of H's type for the sums, bias added, in W's order;
+    keep_z: a new one.  Returns H, or (H, Z) where Z or keep_z is given.  H and Z must not overlap each other or an input."""
+    return _native.spmm_gated(W, W._core, X, H, h_dtype, bias, act, Z, keep_z)
+
+
+def bsr_gated_backward(G, Z, bs_r, act="silu", DZ=None, dz_dtype=None, DB=None, *, need_dz=True, need_db=True):
+    """(DZ, DB), the gradients of bsr_spmm_gated's sums (in Z's order) and of its bias (fp32), from G = dL/dH (m, n) and the
+    Z (m, 2n) that it kept; bs_r: W's.  dz_dtype: G's type, or any where G is fp32.  DZ may be Z itself.  need_dz, need_db: leave
+    out the one or the other (None in its place)."""
+    return _native_module().gated_backward(G, Z, bs_r, act, DZ, dz_dtype, DB, need_dz, need_db)
+
+
+def bsr_residual_norm(S, B=None, *, post="none", pre="rms", post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None, eps=1e-6,
+                      stream_scale=1.0, branch_scale=1.0, out=None, U=None, u_dtype=None, need_sum=True):
+    """(S', U): S' = stream_scale S + branch_scale gate post(B), U = pre(S'), row by row in one pass.
+
+    S (m, n): the stream, fp32 or of B's type; B (m, n): what a block adds to it, or None (S' = stream_scale S).  post, pre:
+    "none" | "rms" | "layer"; weights, biases and gate (n,), all of B's type or all fp32, or None.  out, U: buffers; out may be S
+    itself, U B.  Without a B U is of u_dtype (S's type).  pre "none": no U (None).  need_sum: leave out S'."""
+    return _native_module().residual_norm(S, B, post, pre, post_weight, post_bias, gate, pre_weight, pre_bias, eps, stream_scale, branch_scale, out, U,
+                                          u_dtype, need_sum)
+
+
+_VECTORS = ("post_weight", "post_bias", "gate", "pre_weight", "pre_bias")
+
+
+def bsr_residual_norm_backward(S, B, GS, GU, *, post="none", pre="rms", post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None,
+                               eps=1e-6, stream_scale=1.0, branch_scale=1.0, DS=None, DB=None, need_ds=True, need_db=True, grads=None):
+    """(DS, DB, grads): the gradients of bsr_residual_norm's S, B and vectors, from S = the S' that it gave, its B and settings,
+    GS = dL/dS' (or None: zeros) and GU = dL/dU (or None).
+
+    grads: None (a new fp32 tensor for each vector that is given) or a dict of names and (n,) fp32 tensors to fill; returned as
+    a dict.  DS may be GS or S itself, DB GU or B.  need_ds, need_db: leave out the one or the other (None in its place)."""
+    given = (post_weight, post_bias, gate, pre_weight, pre_bias)
+    if grads is None:
+        want = [None if v is None else True for v in given]
+        if B is None:
+            want[:3] = (None,) * 3
+        if post == "none" or post is None:
+            want[:2] = (None,) * 2
+        if pre == "none" or pre is None:
+            want[3:] = (None,) * 2
+    else:
+        if not set(grads) <= set(_VECTORS):
+            raise ValueError(f"grads: names among {', '.join(_VECTORS)}")
+        want = [grads.get(k) for k in _VECTORS]
+    ds, db, sums = _native_module().residual_norm_backward(S, B, GS, GU, post, pre, *given, eps, stream_scale, branch_scale, DS, DB, need_ds, need_db, want)
+    return ds, db, {k: v for k, v in zip(_VECTORS, sums) if v is not None}
 
 
 STATIC_SCRATCH_BYTES = 8 << 20
@@ -549,3 +684,123 @@ def bsr_adamw_moments(opt: BsrAdamW, dtype="f32", out=None):
         out = [(new(p), new(p)) for p in opt.params]
     _native.adamw_moments(opt, opt._address, opt._index, opt._known, opt._counts, out if isinstance(out, list) else list(out))
     return out
+
+
+class BsrMuon:
+    """Owns the tensors of one list (parameters, gradients, momentum, ...; they must outlive the C handle) and the handle.
+
+    Steps may run on any stream of its device, and it may be dropped while they are still to run.  A graph that a step was
+    captured into reads its buffers at every replay: it must outlive the graph.
+
+    params, grads, master, momentum: lists in the order given to bsr_muon_create (None where a tensor has none)."""
+
+    def __init__(self, params, grads, master, momentum):
+        self.params, self.grads, self.master, self.momentum = params, grads, master, momentum
+        self.handle, self.device, self._keep = None, None, []
+        self._address, self._index = 0, 0       # what the calls read
+        self._known, self._streams = 0, set()   # the stream that was given work last; all, the one its buffers were made on first
+
+    def _on_stream(self, address):
+        """As BsrAdamW's."""
+        if address not in self._streams:
+            import torch
+            stream = torch.cuda.current_stream(self.device)
+            for held in (self.params, self.grads, self.master, self.momentum, self._keep):
+                for t in held:
+                    if isinstance(t, torch.Tensor):
+                        t.record_stream(stream)
+            self._streams.add(address)
+        self._known = address
+
+    def close(self):
+        if self.handle:
+            self._address = 0
+            load_library().bsr_muon_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def bsr_muon_create(params, grads, *, weight_decay=0.0, momentum=None, master=None, transposed=None, scale=None) -> BsrMuon:
+    """The handle of steps over a list of block_data tensors whose updates are orthogonalised block by block, on the current GPU.
+
+    params, grads: contiguous (stored blocks, bs_r, bs_c), sides from 1 to 64, f32, f16 or bf16; a gradient has its parameter's
+    type or fp32 and is read by every step from where it is (let bsr_sddmm write there).  weight_decay, scale: one number or one
+    a tensor; scale is the update's, None: sqrt(max(1, bs_r / bs_c)).  momentum: None (zeros) or fp32 tensors.  master,
+    transposed: as bsr_adamw_create's."""
+    import torch
+    lib = load_library()
+    _native_module()
+    params, grads = list(params), list(grads)
+    n = len(params)
+    one_each = lambda v: [float(v)] * n if isinstance(v, (int, float)) else [float(x) for x in v]  # noqa: E731
+    for given in (grads, momentum, transposed, master if isinstance(master, (list, tuple)) else None):
+        if given is not None and len(given) != n:
+            raise ValueError("one gradient (momentum, master copy, transpose) a parameter is wanted")
+    device = torch.device("cuda", torch.cuda.current_device())
+    f32 = torch.float32
+    for i, p in enumerate(params):
+        if p.dim() != 3:
+            raise ValueError(f"params[{i}] must be (stored blocks, bs_r, bs_c)")
+    decay = one_each(weight_decay)
+    scales = [max(1.0, p.shape[1] / max(p.shape[2], 1)) ** 0.5 for p in params] if scale is None else one_each(scale)
+    if len(decay) != n or len(scales) != n:
+        raise ValueError("one weight_decay (scale), or one a parameter, is wanted")
+    opt = BsrMuon(params, grads, [None] * n, [None] * n)
+    opt.device = device
+    table = (MuonTensor * max(n, 1))()
+    for i, (p, g) in enumerate(zip(params, grads)):
+        count = p.numel()
+        _adamw_buffer(p, f"params[{i}]", (f32, torch.float16, torch.bfloat16), count, device)
+        _adamw_buffer(g, f"grads[{i}]", (p.dtype, f32), count, device)
+        own = master[i] if isinstance(master, (list, tuple)) else (p.detach().to(f32, copy=True) if master and p.dtype != f32 else None)
+        opt.master[i] = None if own is None else _adamw_buffer(own, f"master[{i}]", (f32,), count, device)
+        held = momentum[i] if momentum is not None else torch.zeros(count, dtype=f32, device=device)
+        opt.momentum[i] = _adamw_buffer(held, f"momentum[{i}]", (f32,), count, device)
+        t = table[i]
+        t.blocks, t.bs_r, t.bs_c = (int(v) for v in p.shape)
+        t.dtype, t.grad_dtype, t.weight_decay, t.scale = _DTYPE_CODE[_dtype_name(p)], _DTYPE_CODE[_dtype_name(g)], decay[i], scales[i]
+        t.param_dev, t.grad_dev, t.momentum_dev = p.data_ptr(), g.data_ptr(), opt.momentum[i].data_ptr()
+        t.master_dev = None if own is None else own.data_ptr()
+        turned = transposed[i] if transposed is not None else None
+        if turned is not None:
+            copy, perm = turned
+            copy = copy.block_data if isinstance(copy, BsrMatrix) else copy
+            if count and tuple(copy.shape) != (p.shape[0], p.shape[2], p.shape[1]):
+                raise ValueError(f"transposed[{i}]: (stored blocks, bs_c, bs_r) for a parameter (stored blocks, bs_r, bs_c)")
+            perm = _i32(perm.cpu().numpy() if isinstance(perm, torch.Tensor) else perm)
+            if perm.shape[0] != p.shape[0]:
+                raise ValueError(f"transposed[{i}]: one entry of perm a stored block")
+            if count:
+                _adamw_buffer(copy, f"transposed[{i}]", (p.dtype,), count, device)
+                t.t_param_dev, t.t_perm_host = copy.data_ptr(), perm.ctypes.data
+            opt._keep += [copy, perm]
+    size = ctypes.c_size_t(0)
+    st = lib.bsr_muon_workspace_size(n, table, ctypes.byref(size))
+    if st != 0:
+        raise BsrError(st, "bsr_muon_workspace_size")
+    workspace = torch.empty(size.value, dtype=torch.uint8, device=device)
+    opt._keep.append(workspace)
+    handle = ctypes.c_void_p()
+    st = lib.bsr_muon_create(ctypes.byref(handle), n, table, workspace.data_ptr(), workspace.numel(), torch.cuda.current_stream().cuda_stream)
+    if st != 0:
+        raise BsrError(st, "bsr_muon_create")
+    opt.handle, opt._address, opt._index = handle, handle.value, device.index
+    opt._known = torch.cuda.current_stream().cuda_stream
+    opt._streams.add(opt._known)
+    return opt
+
+
+def bsr_muon_step(opt: BsrMuon, step, *, lr=0.02, momentum=0.95, nesterov=True, ns_steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7,
+                  grad_scale=1.0, seed=0):
+    """One step on torch's current stream, updating opt's parameters, master copies, momentum and transposes in place.
+
+    coefficients: a, b, c of the Newton-Schulz steps X = a X + b (X X^T) X + c (X X^T)^2 X, of which there are ns_steps (0 to 16).
+    step counts from 1 (for the random roundings).  step, lr and grad_scale may be GPU tensors of one int64, fp32 and fp32, which a
+    step captured into a graph reads at every replay; a grad_scale of 0 skips the step, and so does a step below 1 on the GPU."""
+    a, b, c = coefficients
+    _native_module().muon_step(opt, opt._address, opt._index, opt._known, step, lr, momentum, nesterov, ns_steps, a, b, c, eps, grad_scale, seed)

@@ -32,9 +32,10 @@
 #include <new>
 #include <stdexcept>
 
-#include "bsr_mfma_common.h"
+#include "bsr_optimizer.h"
 
 using namespace bsr_dev;
+using namespace bsr_list;
 
 namespace {
 
@@ -75,32 +76,6 @@ struct step_args {
     const int64_t* step_dev;
     const float* grad_scale_dev;
 };
-
-// Two rounds of xor-shift and multiply.
-__host__ __device__ __forceinline__ uint32_t mix(uint32_t x)
-{
-    x ^= x >> 16;
-    x *= 0xBB67AE85u;
-    x ^= x >> 15;
-    x *= 0x6A09E667u;
-    return x ^ (x >> 16);
-}
-__host__ __device__ __forceinline__ uint32_t step_key(uint32_t seed, uint64_t step) { return mix(seed + 0x9E3779B1u * (uint32_t)step); }
-
-template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false); }
-// Largest v of the wavefront (the steps of a sum over 64 lanes).  On the bits of numbers that are not negative, whose order
-// theirs is: a maximum of floats costs another instruction for each operand, to quieten a NaN.
-__device__ __forceinline__ uint32_t wave_max(uint32_t v)
-{
-    v = max(v, dpp<0xB1>(v));
-    v = max(v, dpp<0x4E>(v));
-    v = max(v, dpp<0x141>(v));
-    v = max(v, dpp<0x140>(v));
-    v = max(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x401F));
-    return max((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 32));
-}
-__device__ __forceinline__ uint32_t bits_of(float v) { return __builtin_bit_cast(uint32_t, v); }
-__device__ __forceinline__ float float_of(uint32_t v) { return __builtin_bit_cast(float, v); }
 
 // Four neighbouring elements as loaded.  FULL: all of them are there, else the first n (any n; the others as zeros).
 template <typename T> struct run4 {
@@ -150,23 +125,6 @@ __device__ __forceinline__ void decode_second(float (&v)[4], uint32_t codes, flo
         const float c = (float)((codes >> (8 * e)) & 255u);
         v[e] = c > 0.f ? second_of(c - 1.f, start, spacing) : 0.f;
     }
-}
-
-// fp32 to 16 bits, away from zero with the probability that keeps the mean; `random`: 16 random bits.
-__device__ __forceinline__ bf16_t round_at_random(bf16_t, float x, uint32_t random)
-{
-    // an infinity's low bits are zeros and stay below the place; of a NaN the arithmetic has set the highest bit, which stays
-    const uint32_t u = bits_of(x) + (x == x ? random & 0xFFFFu : 0u);
-    return __builtin_bit_cast(bf16_t, (uint16_t)(u >> 16));
-}
-__device__ __forceinline__ f16_t round_at_random(f16_t, float x, uint32_t random)
-{
-    // steps of fp16 at x: 2^(exponent - 10), 2^-24 among its subnormal numbers; x in such steps keeps 13 bits behind the point
-    const int exponent = max((int)((__builtin_bit_cast(uint32_t, x) >> 23) & 255u) - 127, -14);
-    if (exponent > 15) return (f16_t)x;
-    const float steps = ldexpf(fabsf(x), 10 - exponent);
-    const float whole = floorf(steps + (float)(random & 0x1FFFu) * (1.f / 8192.f));
-    return (f16_t)copysignf(ldexpf(whole, exponent - 10), x);
 }
 
 // What a wavefront reads for 256 elements.  T: the parameter's type, GT: the gradient's, BITS: of the moments.
@@ -450,9 +408,6 @@ __global__ __launch_bounds__(kThreads) void bsr_adamw_values(const tensor_desc* 
     }
 }
 
-size_t size_of(bsr_dtype t) { return t == BSR_F32 ? 4 : 2; }
-bool known(bsr_dtype t) { return (int)t >= (int)BSR_F32 && (int)t <= (int)BSR_BF16; }
-size_t words_of(size_t bytes) { return (bytes + 255) / 256 * 64; }
 int log2_of(int64_t v) { int l = 0; while (((int64_t)1 << l) < v) ++l; return l; }
 // Whether the step's own kernel writes the transposes of such blocks: they are whole in a chunk.
 bool turns(const bsr_adamw_tensor& t) { return kChunk % ((int64_t)t.bs_r * t.bs_c) == 0; }
@@ -474,24 +429,6 @@ bool transposable(const bsr_adamw_tensor& t)
     const int64_t u = 16 / (int64_t)size_of(t.dtype), block = (int64_t)t.bs_r * t.bs_c;
     if (t.bs_r % u == 0 && t.bs_c % u == 0 && t.count / (u * u) < ((int64_t)1 << 31)) return true;
     return block <= 32 * 1024 && (size_t)t.bs_r * (size_t)(t.bs_c + 1) * size_of(t.dtype) <= 64 * 1024;
-}
-
-struct used_range { uintptr_t from, to; bool written; };
-void add_range(std::vector<used_range>& all, const void* p, size_t bytes, bool written)
-{
-    if (p && bytes) all.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written});
-}
-bool by_start(const used_range& a, const used_range& b) { return a.from < b.from; }
-// Whether all that is written is apart from everything else of these, which are in order.
-bool apart(const std::vector<used_range>& all)
-{
-    uintptr_t end = 0, written_end = 0;               // of what begins before
-    for (const used_range& x : all) {
-        if (x.from < (x.written ? end : written_end)) return false;
-        end = std::max(end, x.to);
-        if (x.written) written_end = std::max(written_end, x.to);
-    }
-    return true;
 }
 
 }  // namespace
@@ -677,20 +614,6 @@ bsr_status launch_type(const bsr_adamw* opt, const bsr_adamw::launch_t& l, const
     return f32_grad ? launch_kind<T, float, false>(opt, l, h, stream) : launch_kind<T, T, false>(opt, l, h, stream);
 }
 
-// The tables are there for what `stream` is given next.  What is recorded into a graph cannot wait for an upload outside of
-// it, so a capture right behind bsr_adamw_create() waits here, on the host.
-void ready_for(const bsr_adamw* opt, hipStream_t stream)
-{
-    if (opt->uploaded && is_capturing(stream) && !upload_landed(opt->uploaded, opt->landed)) {
-        hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;      // in the default mode the wait would end the capture
-        const bool swapped = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
-        if (hipEventSynchronize(opt->uploaded) == hipSuccess) opt->landed.store(true, std::memory_order_release);
-        if (swapped) (void)hipThreadExchangeStreamCaptureMode(&mode);
-        (void)hipGetLastError();
-    }
-    order_after_upload(stream, opt->uploaded, opt->landed);
-}
-
 bool on_its_device(const bsr_adamw* opt)
 {
     int dev = -1;
@@ -749,7 +672,7 @@ bsr_status bsr_adamw_step(const bsr_adamw* opt, const bsr_adamw_hyper* hyper, vo
     if (reinterpret_cast<uintptr_t>(y.step_dev) & 7u) return BSR_ERR_ALIGN;
     if (!on_its_device(opt)) return BSR_ERR_DEVICE;
     hipStream_t stream = (hipStream_t)hip_stream;
-    ready_for(opt, stream);
+    ready_for(opt->uploaded, opt->landed, stream);
     step_args h{};
     h.lr = (float)y.lr;
     h.beta1 = (float)y.beta1;
@@ -806,7 +729,7 @@ bsr_status bsr_adamw_moments(const bsr_adamw* opt, bsr_dtype dtype, void* const*
     }
     if (!on_its_device(opt)) return BSR_ERR_DEVICE;
     hipStream_t stream = (hipStream_t)hip_stream;
-    ready_for(opt, stream);
+    ready_for(opt->uploaded, opt->landed, stream);
     for (size_t s = 0; s < n; s += kOutputs) {
         const size_t end = std::min(n, s + kOutputs);
         const int32_t first = opt->first_chunk[s], count = opt->first_chunk[end] - first;

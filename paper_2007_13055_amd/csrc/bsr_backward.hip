@@ -176,13 +176,18 @@ bsr_status launch_types(const backward_shape& s, int64_t m, int64_t n, bsr_act a
     };
     const bsr_status st = db ? go(std::true_type{}) : go(std::false_type{});
     if (st != BSR_OK || !db || s.chunks == 1) return st;
-    hipLaunchKernelGGL(bsr_backward_sums, dim3((unsigned)((n + kSumCols - 1) / kSumCols)), dim3(256), 0, stream, ws, db, (int)n, s.chunks);
-    return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    return launch_backward_sums(ws, db, n, s.chunks, stream);
 }
 
 bool sizes_fit(int64_t m, int64_t n) { return m >= 0 && n >= 0 && m < ((int64_t)1 << 30) && n < ((int64_t)1 << 28); }
 
 }  // namespace
+
+bsr_status launch_backward_sums(const float* partial, float* db, int64_t n, int chunks, hipStream_t stream)
+{
+    hipLaunchKernelGGL(bsr_backward_sums, dim3((unsigned)((n + kSumCols - 1) / kSumCols)), dim3(256), 0, stream, partial, db, (int)n, chunks);
+    return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+}
 
 extern "C" {
 
@@ -215,8 +220,7 @@ bsr_status bsr_epilogue_backward(int64_t m, int64_t n, bsr_act act, bsr_dtype g_
     hipStream_t stream = (hipStream_t)hip_stream;
     if (m == 0) {                                     // no rows: the sums are zero
         if (!DB_dev) return BSR_OK;
-        hipLaunchKernelGGL(bsr_backward_sums, dim3((unsigned)((n + kSumCols - 1) / kSumCols)), dim3(256), 0, stream, DB_dev, DB_dev, (int)n, 0);
-        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+        return launch_backward_sums(DB_dev, DB_dev, n, 0, stream);
     }
     const backward_shape s = split(m, n, g_dtype == BSR_F32 ? 4 : 8);
     size_t need = DB_dev && s.chunks > 1 ? (size_t)s.chunks * (size_t)n * sizeof(float) : 0;

@@ -134,6 +134,13 @@ template <typename F> __device__ __forceinline__ void with_act(int act, F f)
     else if (act == BSR_ACT_SILU) f(std::integral_constant<int, BSR_ACT_SILU>{});
 }
 
+// The same where there may be none.
+template <typename F> __device__ __forceinline__ void with_act_or_none(int act, F f)
+{
+    if (act == BSR_ACT_NONE) f(std::integral_constant<int, BSR_ACT_NONE>{});
+    else with_act(act, f);
+}
+
 // N consecutive elements (1, 4 or 8) as loaded, at an address that is a multiple of their size up to 16 bytes.
 template <typename T, int N> struct run_of {
     static constexpr int K = (int)(16 / sizeof(T)) < N ? (int)(16 / sizeof(T)) : N;   // of a load

@@ -688,6 +688,20 @@ bsr_status bsr_spmm_ex(const bsr_matrix* W, int64_t m, const void* X_dev, void* 
     return multiply(spmm_args{W, m, X_dev, Y_dev, y_dtype, (hipStream_t)hip_stream}, path);
 }
 
+// Whether results of a product with m rows lie over what the handle reads: W, and what addresses are made of in this call and
+// the next.
+static bool over_handle(const bsr_matrix* W, int64_t m, const byte_range& out)
+{
+    const size_t x_size = W->dtype == BSR_F32 ? 4 : 2;
+    for (const byte_range& r : {byte_range{W->data, (size_t)W->nnzb * (size_t)W->bs_r * (size_t)W->bs_c * x_size},
+                                byte_range{W->indices, (size_t)W->nnzb * sizeof(int32_t)},
+                                byte_range{W->indptr, ((size_t)W->R + 1) * sizeof(int32_t)},
+                                byte_range{W->row_order, W->workspace_bytes},
+                                byte_range{W->scratch, std::min(W->scratch_bytes, mfma_thin_scratch_bytes(W, m))}})
+        if (overlap(out, r)) return true;
+    return false;
+}
+
 bsr_status bsr_spmm_epilogue(const bsr_matrix* W, int64_t m, const void* X_dev, void* Y_dev, bsr_dtype y_dtype,
                              const bsr_epilogue* epilogue, void* hip_stream)
 {
@@ -707,22 +721,72 @@ bsr_status bsr_spmm_epilogue(const bsr_matrix* W, int64_t m, const void* X_dev, 
     const byte_range in[] = {{X_dev, (size_t)m * (size_t)W->k * x_size},
                              {e.bias_dev, (size_t)W->n * (e.bias_dtype == BSR_F32 ? 4 : 2)},
                              {e.residual_dev, ((size_t)(m - 1) * (size_t)ld + (size_t)W->n) * y_size},
-                             {e.through_dev, out},
-                             {W->data, (size_t)W->nnzb * (size_t)W->bs_r * (size_t)W->bs_c * x_size},
-                             // what addresses are made of, in this call and the next
-                             {W->indices, (size_t)W->nnzb * sizeof(int32_t)},
-                             {W->indptr, ((size_t)W->R + 1) * sizeof(int32_t)},
-                             {W->row_order, W->workspace_bytes},
-                             {W->scratch, std::min(W->scratch_bytes, mfma_thin_scratch_bytes(W, m))}};
+                             {e.through_dev, out}};
     const byte_range y{Y_dev, out}, z{e.z_dev, out};
     if (overlap(y, z)) return BSR_ERR_OVERLAP;
     for (const byte_range& r : in)
         if (overlap(y, r) || overlap(z, r)) return BSR_ERR_OVERLAP;
+    if (over_handle(W, m, y) || over_handle(W, m, z)) return BSR_ERR_OVERLAP;
     int dev = -1;
     if (hipGetDevice(&dev) != hipSuccess || dev != W->device) return BSR_ERR_DEVICE;
     spmm_args a{W, m, X_dev, Y_dev, y_dtype, (hipStream_t)hip_stream};
     a.epilogue = epilogue;
     return multiply(a, BSR_PATH_AUTO);
+}
+
+// Bytes of the fp32 sums that a gated product leaves in its workspace: none where Z takes them.
+static size_t gated_sums_bytes(const bsr_matrix* W, int64_t m) { return ((size_t)m * (size_t)W->n * sizeof(float) + 255) & ~(size_t)255; }
+
+static bsr_status check_gated_args(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype)
+{
+    if (!W) return BSR_ERR_NULL;
+    if (m < 0 || W->R % 2 != 0 || m * std::max<int64_t>(W->k, W->n) >= kInt32Limit) return BSR_ERR_SHAPE;
+    if (h_dtype != W->dtype && h_dtype != BSR_F32) return BSR_ERR_DTYPE;
+    return BSR_OK;
+}
+
+bsr_status bsr_spmm_gated_workspace_size(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype, size_t* bytes)
+{
+    if (!bytes) return BSR_ERR_NULL;
+    *bytes = 0;
+    const bsr_status st = check_gated_args(W, m, h_dtype);
+    if (st == BSR_OK) *bytes = gated_sums_bytes(W, m);
+    return st;
+}
+
+bsr_status bsr_spmm_gated(const bsr_matrix* W, int64_t m, const void* X_dev, void* H_dev, bsr_dtype h_dtype, const bsr_gated* gated,
+                          void* workspace_dev, size_t workspace_bytes, void* hip_stream)
+{
+    if (!gated) return BSR_ERR_NULL;
+    bsr_status st = check_gated_args(W, m, h_dtype);
+    if (st != BSR_OK) return st;
+    const bsr_gated& e = *gated;
+    if (!known_act(e.act) || (e.bias_dev && e.bias_dtype != W->dtype && e.bias_dtype != BSR_F32)) return BSR_ERR_DTYPE;
+    if (m == 0 || W->n == 0) return BSR_OK;
+    if (!H_dev || (W->k > 0 && !X_dev)) return BSR_ERR_NULL;
+    for (const void* p : {X_dev, (const void*)H_dev, e.bias_dev, (const void*)e.z_dev, (const void*)workspace_dev})
+        if (!aligned16(p)) return BSR_ERR_ALIGN;
+    const bool in_place = e.z_dev && h_dtype == BSR_F32;              // Z itself takes the fp32 sums
+    const size_t need = in_place ? 0 : gated_sums_bytes(W, m);
+    if (need && (!workspace_dev || workspace_bytes < need)) return BSR_ERR_WORKSPACE;
+    const size_t h_size = h_dtype == BSR_F32 ? 4 : 2, x_size = W->dtype == BSR_F32 ? 4 : 2, sums = (size_t)m * (size_t)W->n;
+    const byte_range x{X_dev, (size_t)m * (size_t)W->k * x_size}, bias{e.bias_dev, (size_t)W->n * (e.bias_dtype == BSR_F32 ? 4 : 2)};
+    const byte_range out[] = {{H_dev, sums / 2 * h_size}, {e.z_dev, sums * h_size}, {need ? workspace_dev : nullptr, need}};
+    for (const byte_range& r : out)
+        if (overlap(r, x) || overlap(r, bias) || over_handle(W, m, r)) return BSR_ERR_OVERLAP;
+    if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2])) return BSR_ERR_OVERLAP;
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev != W->device) return BSR_ERR_DEVICE;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    float* const z = static_cast<float*>(in_place ? e.z_dev : workspace_dev);
+    bsr_epilogue bias_only{};
+    bias_only.bias_dtype = e.bias_dtype;
+    bias_only.bias_dev = e.bias_dev;
+    spmm_args a{W, m, X_dev, z, BSR_F32, stream};
+    if (e.bias_dev) a.epilogue = &bias_only;
+    st = multiply(a, BSR_PATH_AUTO);
+    if (st != BSR_OK) return st;
+    return launch_gate_pass(m, W->n / 2, W->bs_r, e.act, z, h_dtype, H_dev, in_place ? nullptr : e.z_dev, stream);
 }
 
 // Candidate settings per kernel family for this W, m and type of result (the search space of bsr_tune).

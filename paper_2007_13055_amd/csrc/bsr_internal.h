@@ -319,6 +319,11 @@ bsr_status launch_sddmm_thin(const bsr_matrix* W, int m, const void* G, const vo
 // XT[c][i] = X[i][c], rows of XT (m rounded up to 4) floats apart
 bsr_status launch_transpose_f32(const float* X, float* XT, int m, int k, hipStream_t stream);
 
+// db[j] = sum of partial[c][j] over `chunks` chunks (none: zeros), in a fixed order (bsr_backward.hip).
+bsr_status launch_backward_sums(const float* partial, float* db, int64_t n, int chunks, hipStream_t stream);
+// H = act(z_g) z_u from fp32 sums z [m][2n] in units of `unit` columns; z_out (may be null): they, rounded to H's type.
+bsr_status launch_gate_pass(int64_t m, int64_t n, int32_t unit, bsr_act act, const float* z, bsr_dtype h_dtype, void* h, void* z_out, hipStream_t stream);
+
 // Expands to a chain of `if (shape matches) return FN<T, O, BR, BC>(args...)` over the block
 // shapes the matrix-core kernels are instantiated for.
 #define BSR_MFMA_SHAPES(FN, T, O, br, bc, ...)                                             \

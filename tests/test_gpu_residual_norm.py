@@ -1,0 +1,288 @@
+"""bsr_residual_norm and its gradient against the formulas in 64 bits."""
+import numpy as np
+import pytest
+
+from act_reference import ROUNDING
+from gpu_util import torch_dtype
+from norm_reference import backward, forward
+
+pytestmark = pytest.mark.gpu
+
+VECTORS = ("post_weight", "post_bias", "gate", "pre_weight", "pre_bias")
+# rows by columns: every number of lanes a row, one and several runs a lane, ends inside one, the longest; several rows a team
+SIZES = [(1, 1), (3, 5), (70, 8), (33, 64), (5, 100), (9, 129), (1, 511), (17, 1024), (1100, 1030), (3, 2049), (2100, 4096), (3, 4104), (4, 8191), (2, 8200), (300, 16384)]
+KINDS = [("rms", "rms"), ("layer", "layer"), ("none", "rms"), ("rms", "none"), ("layer", "rms"), ("none", "none")]
+TYPES = [("f32", "f32", "f32"), ("f32", "bf16", "bf16"), ("f32", "f16", "f32"), ("bf16", "bf16", "f32"), ("f16", "f16", "f16")]
+
+
+def _f64(t):
+    import torch
+    return t.to(torch.float64).cpu().numpy()
+
+
+def _close(got, want, bound, dtype, what):
+    u, tiny = ROUNDING[dtype]
+    got = _f64(got)
+    assert np.all(np.isfinite(got)), what
+    over = np.abs(got - want) - (bound + u * (np.abs(want) + bound) + tiny)
+    assert np.all(over <= 0), (what, float(over.max()), np.unravel_index(int(np.argmax(over)), over.shape))
+
+
+def _make(m, n, s_t, b_t, w_t, seed, have=VECTORS, shift=0.1):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    new = lambda shape, t, scale=1.0, shift=0.0: (torch.randn(shape, generator=gen, device="cuda") * scale + shift).to(torch_dtype(t))  # noqa: E731
+    S, B = new((m, n), s_t, 2.0, shift), new((m, n), b_t, 0.7, shift)
+    GS, GU = new((m, n), s_t, 0.1), new((m, n), b_t, 0.1)
+    v = {k: new((n,), w_t, 0.3, 0.5 if k != "post_bias" else 0.0) for k in VECTORS if k in have}
+    return S, B, GS, GU, v
+
+
+def _of(v, post, pre):
+    return {k: t for k, t in v.items() if not (post == "none" and k in VECTORS[:2]) and not (pre == "none" and k in VECTORS[3:])}
+
+
+def _guarded(m, n, dtype):
+    """A buffer with a border behind it that nothing may touch."""
+    import torch
+    flat = torch.full((m * n + 64,), 7.0, dtype=torch_dtype(dtype), device="cuda")
+    return flat[:m * n].view(m, n), flat[m * n:]
+
+
+@pytest.mark.parametrize("i,size", list(enumerate(SIZES)))
+@pytest.mark.parametrize("post,pre", KINDS[:4])
+def test_sizes(i, size, post, pre):
+    """All sizes, the types in turn."""
+    _check(*size, *TYPES[(i + KINDS.index((post, pre))) % len(TYPES)], post, pre, VECTORS, 0.5, 0.75, i)
+
+
+@pytest.mark.parametrize("post,pre", KINDS)
+@pytest.mark.parametrize("s_t,b_t,w_t", TYPES)
+def test_types(s_t, b_t, w_t, post, pre):
+    _check(37, 321, s_t, b_t, w_t, post, pre, VECTORS, 1.0, 1.0, 3)
+
+
+@pytest.mark.parametrize("have", [(), ("gate",), ("post_weight", "pre_weight"), ("post_bias",), ("pre_bias", "gate")])
+def test_vectors_left_out(have):
+    _check(40, 200, "f32", "bf16", "bf16", "rms", "layer", have, 1.0, 1.0, 4)
+
+
+def _check(m, n, s_t, b_t, w_t, post, pre, have, alpha, beta, seed):
+    import torch
+    import paper_2007_13055_amd as lib
+    S, B, GS, GU, v = _make(m, n, s_t, b_t, w_t, seed, have)
+    v = _of(v, post, pre)
+    how = dict(post=post, pre=pre, stream_scale=beta, branch_scale=alpha, **v)
+    (out, border), (U, border_u) = _guarded(m, n, s_t), _guarded(m, n, b_t)
+    total, u = lib.bsr_residual_norm(S, B, **how, out=out, U=U if pre != "none" else None)
+    assert total is out and (u is U if pre != "none" else u is None)
+    v64 = {k: _f64(t) for k, t in v.items()}
+    want, after = forward(_f64(S), _f64(B), post, pre, v64, alpha, beta)
+    _close(total, *want, s_t, "S'")
+    if after is not None:
+        _close(u, *after, b_t, "U")
+    assert bool((border == 7).all()) and bool((border_u == 7).all())
+    # the gradient, at the stored sum
+    (DS, border), (DB, border_u) = _guarded(m, n, s_t), _guarded(m, n, b_t)
+    ds, db, grads = lib.bsr_residual_norm_backward(total, B, GS, GU if pre != "none" else None, **how, DS=DS, DB=DB)
+    want = backward(_f64(total), _f64(B), _f64(GS), _f64(GU), post, pre, v64, alpha, beta)
+    _close(ds, *want["dS"], s_t, "dS")
+    _close(db, *want["dB"], b_t, "dB")
+    assert set(grads) == set(v)
+    for k, t in grads.items():
+        assert t.dtype == torch.float32
+        _close(t, *want[k], "f32", k)
+    assert bool((border == 7).all()) and bool((border_u == 7).all())
+    # the same bits again, in place, and without the sums
+    again = lib.bsr_residual_norm_backward(total, B, GS, GU if pre != "none" else None, **how)
+    assert torch.equal(again[0], ds) and torch.equal(again[1], db) and all(torch.equal(again[2][k], grads[k]) for k in grads)
+    gs, gu = GS.clone(), GU.clone()
+    lib.bsr_residual_norm_backward(total, B, gs, gu if pre != "none" else None, **how, DS=gs, DB=gu if pre != "none" else None, grads={})
+    assert torch.equal(gs, ds) and (pre == "none" or torch.equal(gu, db))
+    s, b = S.clone(), B.clone()
+    lib.bsr_residual_norm(s, b, **how, out=s, U=b if pre != "none" else None)
+    assert torch.equal(s, total) and (pre == "none" or torch.equal(b, u))
+
+
+def test_against_differences():
+    """The gradient along a direction against the 64-bit formulas' difference quotient."""
+    import torch
+    import paper_2007_13055_amd as lib
+    rng = np.random.default_rng(1)
+    m, n = 6, 300
+    for post, pre in KINDS[:5]:
+        v64 = {k: rng.normal(0.5, 0.3, n).astype(np.float32).astype(np.float64) for k in VECTORS}
+        x = {"S": rng.normal(0, 2, (m, n)), "B": rng.normal(0, 1, (m, n)), "GS": rng.normal(0, 1, (m, n)), "GU": rng.normal(0, 1, (m, n))}
+        x = {k: t.astype(np.float32).astype(np.float64) for k, t in x.items()}
+        direction = {k: rng.normal(0, 1, t.shape) for k, t in {**{k: x[k] for k in ("S", "B")}, **v64}.items()}
+
+        def loss(t):
+            (total, _), after = forward(x["S"] + t * direction["S"], x["B"] + t * direction["B"], post, pre, {k: a + t * direction[k] for k, a in v64.items()}, 0.5, 0.75)
+            return (total * x["GS"]).sum() + (0 if after is None else (after[0] * x["GU"]).sum())
+
+        (total, _), _ = forward(x["S"], x["B"], post, pre, v64, 0.5, 0.75)
+        dev = lambda a: torch.from_numpy(a).float().cuda()  # noqa: E731
+        v = _of({k: dev(a) for k, a in v64.items()}, post, pre)
+        ds, db, grads = lib.bsr_residual_norm_backward(dev(total), dev(x["B"]), dev(x["GS"]), dev(x["GU"]) if pre != "none" else None, post=post, pre=pre,
+                                                       stream_scale=0.75, branch_scale=0.5, **v)
+        parts = [_f64(ds) * direction["S"], _f64(db) * direction["B"]] + [_f64(g) * direction[k] for k, g in grads.items()]
+        got, size = sum(p.sum() for p in parts), sum(np.abs(p).sum() for p in parts)
+        h = 1e-5
+        want = (loss(h) - loss(-h)) / (2 * h)
+        # fp32 gradients: each within some 100 roundings of its terms, which are a few times its size (S' was rounded too)
+        assert abs(got - want) <= 2e-4 * size, (post, pre, got, want)
+
+
+def test_a_large_mean_does_not_cancel():
+    import paper_2007_13055_amd as lib
+    S, B, GS, GU, v = _make(20, 1500, "f32", "f32", "f32", 5, shift=300.0)
+    how = dict(post="layer", pre="layer")
+    total, u = lib.bsr_residual_norm(S, B, **how)
+    want, after = forward(_f64(S), _f64(B), "layer", "layer", {}, 1.0, 1.0)
+    _close(total, *want, "f32", "S'")
+    _close(u, *after, "f32", "U")
+    # The bound itself has not grown beyond use.  By its terms: B's mean, 300, is off by 48 2^-24 300 = 8.6e-4, relative to 0.7 1.2e-3,
+    # which S' inherits; with S's own mean and subtractions, relative to S' spread of 2.2: 3e-3, of the centred values and of the
+    # root alike, times 1 + 4.5 (the largest value): 0.0165.  Without centring first the mean square, 9e4, would be off by 0.26.
+    assert after[1].max() < 0.02
+
+
+def test_rows_that_are_not_finite_stay_alone():
+    import torch
+    import paper_2007_13055_amd as lib
+    for n in (40, 1000, 5000):
+        S, B, GS, GU, v = _make(24, n, "f32", "bf16", "bf16", 6)
+        how = dict(post="rms", pre="layer", **_of(v, "rms", "layer"))
+        clean = lib.bsr_residual_norm(S, B, **how)
+        back = lib.bsr_residual_norm_backward(clean[0], B, GS, GU, **how)
+        bad = S.clone()
+        bad[3, n // 2], bad[11, 0], bad[17] = float("nan"), float("inf"), 0.0
+        got = lib.bsr_residual_norm(bad, B, **how)
+        rest = [i for i in range(24) if i not in (3, 11, 17)]
+        assert all(torch.equal(g[rest], c[rest]) for g, c in zip(got, clean))
+        assert bool(got[1][3].isnan().all()) and bool(got[1][11].isnan().any()) and bool(got[1][17].isfinite().all())
+        bad = clean[0].clone()
+        bad[3, 1] = float("nan")
+        ds, db, _ = lib.bsr_residual_norm_backward(bad, B, GS, GU, **how)
+        rest = [i for i in range(24) if i != 3]
+        assert torch.equal(ds[rest], back[0][rest]) and torch.equal(db[rest], back[1][rest]) and bool(ds[3].isnan().any())
+
+
+def test_zero_rows():
+    """A row of zeros has zeros as its norm (eps > 0), finite gradients."""
+    import torch
+    import paper_2007_13055_amd as lib
+    z = torch.zeros((5, 700), device="cuda")
+    for kind in ("rms", "layer"):
+        total, u = lib.bsr_residual_norm(z, z, post=kind, pre=kind)
+        assert bool((total == 0).all()) and bool((u == 0).all())
+        ds, db, _ = lib.bsr_residual_norm_backward(z, z, torch.ones_like(z), torch.ones_like(z), post=kind, pre=kind)
+        assert bool(ds.isfinite().all()) and bool(db.isfinite().all())
+
+
+def test_without_a_branch_and_without_parts():
+    import torch
+    import paper_2007_13055_amd as lib
+    S, B, GS, GU, v = _make(21, 640, "f32", "bf16", "f32", 7)
+    total, u = lib.bsr_residual_norm(S, pre_weight=v["pre_weight"], u_dtype="bf16")
+    assert total is S and u.dtype == torch.bfloat16
+    want, after = forward(_f64(S), None, "none", "rms", {"pre_weight": _f64(v["pre_weight"])}, 1.0, 1.0)
+    _close(u, *after, "bf16", "U")
+    half, u2 = lib.bsr_residual_norm(S, stream_scale=0.5, u_dtype="f32")
+    assert torch.equal(half, S * 0.5) and u2.dtype == torch.float32
+    none, u3 = lib.bsr_residual_norm(S, B, need_sum=False)
+    assert none is None and torch.equal(u3, lib.bsr_residual_norm(S, B)[1])
+    ds, db, grads = lib.bsr_residual_norm_backward(S, None, None, GU, pre_weight=v["pre_weight"])
+    want = backward(_f64(S), None, np.zeros((21, 640)), _f64(GU), "none", "rms", {"pre_weight": _f64(v["pre_weight"])}, 1.0, 1.0)
+    _close(ds, *want["dS"], "f32", "dS")
+    assert db is None and set(grads) == {"pre_weight"}
+    _close(grads["pre_weight"], *want["pre_weight"], "f32", "pre_weight")
+    # the gradient of a vector that is not there: it counts as 1 or 0
+    buffers = {k: torch.full((640,), 7.0, device="cuda") for k in VECTORS}
+    out = lib.bsr_residual_norm_backward(S, B, GS, GU, post="layer", pre="rms", need_ds=False, need_db=False, grads=buffers)
+    assert out[0] is None and out[1] is None and all(out[2][k] is buffers[k] for k in VECTORS)
+    want = backward(_f64(S), _f64(B), _f64(GS), _f64(GU), "layer", "rms", {}, 1.0, 1.0)
+    for k in VECTORS:
+        _close(buffers[k], *want[k], "f32", k)
+
+
+@pytest.mark.parametrize("n", [100, 3000, 9000])
+def test_empty(n):
+    import torch
+    import paper_2007_13055_amd as lib
+    S = torch.zeros((0, n), device="cuda")
+    total, u = lib.bsr_residual_norm(S, S.clone(), post="rms")
+    assert total.shape == u.shape == (0, n)
+    sums = {k: torch.full((n,), 7.0, device="cuda") for k in ("gate", "pre_weight")}
+    lib.bsr_residual_norm_backward(S, S.clone(), S.clone(), S.clone(), post="rms", grads=sums)
+    assert all(bool((t == 0).all()) for t in sums.values())
+    none = torch.zeros((4, 0), device="cuda")
+    lib.bsr_residual_norm(none, none.clone())
+    lib.bsr_residual_norm_backward(none, none.clone(), none.clone(), None)
+
+
+@pytest.mark.parametrize("n", [96, 5000, 10000])
+def test_captured_and_replayed(n):
+    """Forward and gradient in one graph, with eager work between its replays."""
+    import torch
+    import paper_2007_13055_amd as lib
+    S, B, GS, GU, v = _make(50, n, "f32", "bf16", "bf16", 8)
+    how = dict(post="rms", pre="rms", **_of(v, "rms", "rms"))
+    run = lambda: (lib.bsr_residual_norm(S, B, **how), lib.bsr_residual_norm_backward(S, B, GS, GU, **how))  # noqa: E731
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        (total, u), (ds, db, grads) = run()
+    for k in range(4):
+        for t in (S, B, GS, GU):
+            t.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        (total2, u2), (ds2, db2, grads2) = run()
+        assert torch.equal(total, total2) and torch.equal(u, u2) and torch.equal(ds, ds2) and torch.equal(db, db2)
+        assert all(torch.equal(grads[q], grads2[q]) for q in grads)
+
+
+def test_on_another_stream():
+    import torch
+    import paper_2007_13055_amd as lib
+    S, B, GS, GU, v = _make(300, 4096, "f32", "bf16", "bf16", 9)
+    how = dict(post="rms", pre="rms", **_of(v, "rms", "rms"))
+    want = lib.bsr_residual_norm_backward(S, B, GS, GU, **how)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = [lib.bsr_residual_norm_backward(S, B, GS, GU, **how) for _ in range(3)]
+    here = lib.bsr_residual_norm_backward(S, B, GS, GU, **how)            # at the same time, with a workspace of its own
+    torch.cuda.synchronize()
+    for g in got + [here]:
+        assert torch.equal(g[0], want[0]) and torch.equal(g[1], want[1]) and all(torch.equal(g[2][k], want[2][k]) for k in want[2])
+
+
+def test_refusals():
+    import torch
+    import paper_2007_13055_amd as lib
+    S = torch.zeros((4, 64), device="cuda")
+    b = S.bfloat16()
+    w = torch.ones(64, device="cuda")
+    bad = [lambda: lib.bsr_residual_norm(b, S), lambda: lib.bsr_residual_norm(S, b[:3]), lambda: lib.bsr_residual_norm(S.t(), b),
+           lambda: lib.bsr_residual_norm(S, b, pre_weight=w[:63]), lambda: lib.bsr_residual_norm(S, b, pre_weight=w.half()),
+           lambda: lib.bsr_residual_norm(S, b, pre_weight=w, gate=w.bfloat16()), lambda: lib.bsr_residual_norm(S, b, pre="none", U=b),
+           lambda: lib.bsr_residual_norm(S, b, pre_weight=w.cpu()), lambda: lib.bsr_residual_norm(S.cpu()), lambda: lib.bsr_residual_norm(S, b, u_dtype="f16"),
+           lambda: lib.bsr_residual_norm_backward(None, b, S, b), lambda: lib.bsr_residual_norm_backward(S, b, S, b, pre="none"),
+           lambda: lib.bsr_residual_norm_backward(S, b, S, b, grads={"weight": w}), lambda: lib.bsr_residual_norm_backward(S, b, S, b, grads={"gate": w.half()}),
+           lambda: lib.bsr_residual_norm_backward(None, None, None, None)]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(KeyError):
+        lib.bsr_residual_norm(S, b, pre="batch")
+    wide = torch.zeros((2, 16392), device="cuda")
+    for call in (lambda: lib.bsr_residual_norm(wide), lambda: lib.bsr_residual_norm_backward(wide, None, wide.clone(), None),
+                 lambda: lib.bsr_residual_norm(S, eps=-1.0), lambda: lib.bsr_residual_norm(S, b, out=S, U=S.view(torch.bfloat16).view(-1)[:256].view(4, 64)),
+                 lambda: lib.bsr_residual_norm_backward(S, b, S, b, post="none", grads={"post_weight": w}),
+                 lambda: lib.bsr_residual_norm_backward(S, None, S, b, grads={"gate": w}),
+                 lambda: lib.bsr_residual_norm_backward(S, b, S.clone(), b.clone(), grads={"gate": w, "pre_weight": w}),
+                 lambda: lib.bsr_residual_norm_backward(S, b, S.clone(), b.clone(), gate=w, grads={"gate": w})):
+        with pytest.raises(lib.BsrError):
+            call()
