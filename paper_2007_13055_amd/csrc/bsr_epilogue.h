@@ -26,7 +26,7 @@
 
 // `e` as the kernels take it; null pointers: that part is left out.
 struct epilogue_args {
-    static constexpr bool on = true;
+    static constexpr bool on = true, gated = false;
     const void* bias;                                 // [n], W's type or fp32
     const void* residual;                             // [m] rows of n elements of Y's type, residual_ld apart
     const void* through;                              // Z0 [m][n], Y's type
@@ -37,7 +37,21 @@ struct epilogue_args {
     int32_t once;                                     // residual and Z0 are read past the caches
 };
 struct no_epilogue {
-    static constexpr bool on = false;
+    static constexpr bool on = false, gated = false;
+};
+
+// The gated product's last stage (bsr_spmm_gated): a workgroup has the sums of block-rows 2r and 2r + 1, z_g and z_u,
+//     z += bias         Z = z, if wanted         H = act(z_g) z_u
+// n is W's, twice H's; a half's columns stand together in units of bs_r.
+struct gated_args {
+    typedef bsr_dev::i32x4 i32x4;
+    static constexpr bool on = false, gated = true;
+    const void* bias;                                 // [n], W's type or fp32, in W's order
+    void* z;                                          // Z [m][n], H's type
+    const int32_t* indptr;                            // W's
+    const i32x4* pairs;                               // W's gate_pairs
+    int32_t act;
+    int32_t bias_f32;
 };
 
 // Calls launch(no_epilogue) or launch(epilogue_args), as the product asks for.
@@ -57,6 +71,15 @@ bsr_status with_epilogue(const spmm_args& a, F launch)
     const bool once = (int64_t)a.m * a.W->n * (a.y_dtype == BSR_F32 ? 4 : 2) > ((int64_t)112 << 20);
     return launch(epilogue_args{e.bias_dev, e.residual_dev, act == BSR_ACT_NONE ? nullptr : e.through_dev, e.z_dev,
                                 e.residual_ld ? e.residual_ld : a.W->n, act, e.bias_dtype == BSR_F32, once});
+}
+
+// The same, in the kernels that also finish gated products.
+template <typename F>
+bsr_status with_epilogue_or_gate(const spmm_args& a, F launch)
+{
+    if (!a.gated) return with_epilogue(a, launch);
+    const bsr_gated& e = *a.gated;
+    return launch(gated_args{e.bias_dev, e.z_dev, a.W->indptr, reinterpret_cast<const bsr_dev::i32x4*>(a.W->gate_pairs), (int32_t)e.act, e.bias_dtype == BSR_F32});
 }
 
 namespace bsr_dev {
@@ -188,7 +211,7 @@ template <bool NT = false, typename O, int N> __device__ __forceinline__ void st
 // result.  Apart from finish(), so that a kernel can have the reads under way before it has its sums.
 template <typename T, int N> struct bias_run {
     float b[N];
-    __device__ __forceinline__ void fetch(const epilogue_args& ep, int j)
+    template <typename E> __device__ __forceinline__ void fetch(const E& ep, int j)   // epilogue_args or gated_args
     {
 #pragma unroll
         for (int e = 0; e < N; ++e) b[e] = 0.f;
@@ -238,6 +261,30 @@ __device__ __forceinline__ void finish(const epilogue_args& ep, float (&v)[N], i
     bias.fetch(ep, j);
     reads.fetch(ep, i, j, n);
     finish<T, O>(ep, bias, reads, v, i, j, n);
+}
+
+// Gated sums g, u of a piece of row i, whose columns in W's order begin at j and j + unit: Z stored if wanted, H into g.
+template <typename T, typename O, int N>
+__device__ __forceinline__ void finish_gate(const gated_args& ep, const bias_run<T, N>& bg, const bias_run<T, N>& bu, float (&g)[N], float (&u)[N], int i,
+                                            int j, int unit, int n)
+{
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        g[e] += bg.b[e];
+        u[e] += bu.b[e];
+    }
+    if (ep.z) {
+        O* const z = static_cast<O*>(ep.z) + (size_t)i * (size_t)n + (size_t)j;
+        store_run<true>(z, g);
+        store_run<true>(z + unit, u);
+    }
+    with_act_or_none(ep.act, [&](auto act) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            g[e] = act_value<decltype(act)::value>(g[e]) * u[e];
+            asm("" : "+v"(g[e]));                     // an fp32 number: left to itself the compiler rounds the exact product to fp16
+        }
+    });
 }
 
 // As store4: 4 consecutive columns of row i.

@@ -470,6 +470,18 @@ static bsr_status create(bsr_matrix** out, int64_t n, int64_t k, int32_t bs_r, i
         W->block_row = W->row_order + at;
         words = (at + (size_t)nnzb + 63) & ~(size_t)63;
     }
+    if (R % 2 == 0 && mfma_supports(W)) {             // gated products: pairs of block-rows, most stored blocks first
+        const size_t at = words;
+        W->staging.resize(at + 2 * (size_t)R + 64, 0);
+        std::vector<int32_t> order((size_t)R / 2);
+        std::iota(order.begin(), order.end(), 0);
+        auto blocks = [&](int32_t q) { return index_pointer_host[2 * q + 2] - index_pointer_host[2 * q]; };
+        std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return blocks(a) > blocks(b); });
+        for (size_t i = 0; i < order.size(); ++i)
+            for (int e = 0; e < 4; ++e) W->staging[at + 4 * i + (size_t)e] = e == 0 ? order[i] : index_pointer_host[2 * order[i] + e - 1];
+        W->gate_pairs = W->row_order + at;
+        words = (at + 2 * (size_t)R + 63) & ~(size_t)63;
+    }
     build_group_plan(W, index_pointer_host, block_indices_host, &words);
     build_thinrow_plan(W, index_pointer_host, block_indices_host, &words);
     build_wide_plan(W, index_pointer_host, block_indices_host, &words);
@@ -734,8 +746,38 @@ bsr_status bsr_spmm_epilogue(const bsr_matrix* W, int64_t m, const void* X_dev, 
     return multiply(a, BSR_PATH_AUTO);
 }
 
-// Bytes of the fp32 sums that a gated product leaves in its workspace: none where Z takes them.
-static size_t gated_sums_bytes(const bsr_matrix* W, int64_t m) { return ((size_t)m * (size_t)W->n * sizeof(float) + 255) & ~(size_t)255; }
+// Which kernel makes a gated product's results.  `sums`: the product's own choice, into a workspace, and a pass over that.
+enum class gated_kernel { sums, wave, ksplit, tile, sweep };
+static gated_kernel gated_choice(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype)
+{
+    // 8-wide blocks: where whole 16x16 tiles hold them (or outputs would have to be summed again, bsr_mfma_sweep.hip); it reads X
+    // once for all outputs and is quicker than the kernel of tiles and a pass behind it from 16 rows on in all of 40 products
+    // (64 x (512, 2 x 768) bf16 8x8 5 %: 4.4 us, 6.3; 64 x (1024, 2 x 2048) fp32 8x8 20 % 8.1, 11.4), below that by estimates
+    const bool sweeps = mfma_small_supports(W) && mfma_sweep_supports(W) && (m >= 16 || sweep_gates_quicker(W, m, h_dtype));
+    if (W->env_tune.from_env && W->env_tune.variant > 0) {
+        const int v = W->env_tune.variant;
+        return v == 2 && mfma_supports(W) ? gated_kernel::ksplit : v == 3 && mfma_supports(W) && W->bs_r >= 32 ? gated_kernel::tile
+             : v == 6 && mfma_sweep_supports(W) ? gated_kernel::sweep : v == 7 ? gated_kernel::wave : gated_kernel::sums;
+    }
+    if (W->nnzb == 0 || (auto_path(W, m, h_dtype) == BSR_PATH_WAVE && !sweeps)) return gated_kernel::wave;
+    if (mfma_supports(W)) {
+        if (mfma_sweep_supports(W) && sweep_gates_quicker(W, m, h_dtype)) return gated_kernel::sweep;
+        // workgroups of the tile kernel: with fewer it waits for its loads, a block after the other
+        const int64_t tiles = (m + 127) / 128 * (W->R / 2);
+        if (W->bs_r >= 32 && m >= 512 && tiles >= (W->bs_r == 64 ? 400 : 2000)) return gated_kernel::tile;
+        return mfma_ksplit_reaches(W) ? gated_kernel::ksplit : gated_kernel::sums;
+    }
+    return sweeps ? gated_kernel::sweep : gated_kernel::sums;
+}
+
+// Bytes of the fp32 sums that a gated product leaves in its workspace: none where a kernel makes H by itself, whatever is
+// captured (the sweep kernel's plan may not be there then: 16x16 blocks have the k-split kernel).
+static size_t gated_sums_bytes(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype)
+{
+    const gated_kernel g = gated_choice(W, m, h_dtype);
+    if (g != gated_kernel::sums && (g != gated_kernel::sweep || W->sw_created || (mfma_supports(W) && mfma_ksplit_reaches(W)))) return 0;
+    return ((size_t)m * (size_t)W->n * sizeof(float) + 255) & ~(size_t)255;
+}
 
 static bsr_status check_gated_args(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype)
 {
@@ -750,7 +792,7 @@ bsr_status bsr_spmm_gated_workspace_size(const bsr_matrix* W, int64_t m, bsr_dty
     if (!bytes) return BSR_ERR_NULL;
     *bytes = 0;
     const bsr_status st = check_gated_args(W, m, h_dtype);
-    if (st == BSR_OK) *bytes = gated_sums_bytes(W, m);
+    if (st == BSR_OK) *bytes = gated_sums_bytes(W, m, h_dtype);
     return st;
 }
 
@@ -767,7 +809,7 @@ bsr_status bsr_spmm_gated(const bsr_matrix* W, int64_t m, const void* X_dev, voi
     for (const void* p : {X_dev, (const void*)H_dev, e.bias_dev, (const void*)e.z_dev, (const void*)workspace_dev})
         if (!aligned16(p)) return BSR_ERR_ALIGN;
     const bool in_place = e.z_dev && h_dtype == BSR_F32;              // Z itself takes the fp32 sums
-    const size_t need = in_place ? 0 : gated_sums_bytes(W, m);
+    const size_t need = in_place ? 0 : gated_sums_bytes(W, m, h_dtype);
     if (need && (!workspace_dev || workspace_bytes < need)) return BSR_ERR_WORKSPACE;
     const size_t h_size = h_dtype == BSR_F32 ? 4 : 2, x_size = W->dtype == BSR_F32 ? 4 : 2, sums = (size_t)m * (size_t)W->n;
     const byte_range x{X_dev, (size_t)m * (size_t)W->k * x_size}, bias{e.bias_dev, (size_t)W->n * (e.bias_dtype == BSR_F32 ? 4 : 2)};
@@ -778,6 +820,25 @@ bsr_status bsr_spmm_gated(const bsr_matrix* W, int64_t m, const void* X_dev, voi
     int dev = -1;
     if (hipGetDevice(&dev) != hipSuccess || dev != W->device) return BSR_ERR_DEVICE;
     hipStream_t stream = (hipStream_t)hip_stream;
+    const gated_kernel choice = gated_choice(W, m, h_dtype);
+    if (choice != gated_kernel::sums) {
+        order_after_upload(stream, W->plan_uploaded, W->plan_landed);
+        if (W->debug && (st = debug_check_device_arrays(W, stream)) != BSR_OK) return st;
+        spmm_args a{W, m, X_dev, H_dev, h_dtype, stream};
+        a.gated = gated;
+        tune_opts t = W->env_tune;
+        t.variant = 0;
+        if (choice == gated_kernel::wave) return launch_wave(a, t);
+        if (choice == gated_kernel::sweep) {
+            st = launch_mfma_sweep(a, t);
+            if (st != BSR_ERR_UNSUPPORTED) return st;
+            // its plan is not there (a capture behind bsr_create, or no host memory): nothing was launched
+            if (mfma_supports(W) && mfma_ksplit_reaches(W)) return launch_mfma_ksplit(a, t);
+        } else {
+            if (choice == gated_kernel::tile) t.mt = 1;
+            return choice == gated_kernel::tile ? launch_mfma_tile(a, t) : launch_mfma_ksplit(a, t);
+        }
+    }
     float* const z = static_cast<float*>(in_place ? e.z_dev : workspace_dev);
     bsr_epilogue bias_only{};
     bias_only.bias_dtype = e.bias_dtype;

@@ -69,6 +69,10 @@ struct bsr_matrix {
     // dispatcher puts on one CU carry about the same number of stored blocks (see ksplit_items()).
     // Pair table of the stripe kernel (16x16 blocks): pair_ptr[R+1], pairs[entries][4] (see bsr_create).
     const int32_t* pair_ptr = nullptr;
+    // For gated products (blocks that mfma_supports() names, an even number of block-rows): the pairs of block-rows 2q and 2q + 1 by
+    // their stored blocks, most first, {q, first stored block, first of 2q + 1, end}, [R / 2][4] (device).  Sorted or not, us: 4096 x
+    // (1024, 2 x 4096) bf16 32x32 20 % 52, 64; 64x64 37, 41; 8192 x (8192, 2 x 8192) f16 64x64 5 %, power law 230, 272.
+    const int32_t* gate_pairs = nullptr;
     const int32_t* pairs = nullptr;
     int32_t* item_desc = nullptr;            // kItemSlots tables of item_capacity descriptors each
     size_t item_capacity = 0;                // descriptors that fit one table
@@ -202,6 +206,7 @@ struct spmm_args {
     hipStream_t stream;
     int first_slot = 0;                      // tile kernel: leave out the slots before this one (another kernel multiplies them)
     const bsr_epilogue* epilogue = nullptr;  // what happens to the sums before they are stored (bsr_epilogue.h); null: nothing
+    const bsr_gated* gated = nullptr;        // the gated product's last stage; then Y is H and y_dtype its type (wave, k-split, tile and sweep kernels)
 };
 
 // A call's buffers, for the checks of what is written against what else there is.  A null pointer overlaps nothing.
@@ -291,6 +296,8 @@ bool mfma_sweep_supports(const bsr_matrix* W);
 // Whether the sweep kernel takes less time, by estimates, than the kernel that would run else.
 enum class sweep_rival { ksplit, stripes, tiles };
 bool sweep_is_quicker(const bsr_matrix* W, int64_t m, bsr_dtype y_dtype, sweep_rival than);
+// The same of a gated product, against the k-split kernel (16x16 blocks) or the wavefront kernels (others).
+bool sweep_gates_quicker(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype);
 // 16-bit W with a side of 8: whether some m leaves it to the kernel of 16x16 tiles, so that those are listed (may throw).
 bool sweep_leaves_tiles(bsr_matrix* W, const int32_t* index_pointer_host, const int32_t* block_indices_host);
 bool sweep_takes(const bsr_matrix* W);              // by its shape, type and sizes

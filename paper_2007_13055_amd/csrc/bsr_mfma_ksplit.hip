@@ -110,6 +110,8 @@ __global__ __launch_bounds__(BS_R == 16 ? 1024 : 512) void bsr_mfma_ksplit(const
     const int hw_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nw_max = blockDim.x >> 6;
     const int li = lane % MM, h = lane / MM;
+    // (gated: the workgroup has two block-rows, half of its wavefronts each; their descriptors are made here)
+    const int half = E::gated ? hw_wave / (nw_max >> 1) : 0, nw_half = E::gated ? nw_max >> 1 : nw_max;
     // One read of the workgroup's descriptor, a word per lane: block-row, first stored block, count,
     // m-tile, first block-columns.  With a work-item table (items = the number of CUs it was laid out
     // for, else 0) workgroup b takes entry b --
@@ -117,19 +119,35 @@ __global__ __launch_bounds__(BS_R == 16 ? 1024 : 512) void bsr_mfma_ksplit(const
     // entry with block-row -1 is a filler; without one, workgroup b takes slot b mod R of m-tile b div R.
     const int32_t* __restrict__ desc =
         row_desc + (size_t)(items ? blockIdx.x : blockIdx.x % (unsigned)R) * kRowDescWords;
-    const int dword = lane < kRowDescWords ? desc[lane] : 0;
-    const int r = __builtin_amdgcn_readlane(dword, 0);
-    if (r < 0) return;                                // whole workgroup leaves together
-    const int p0 = __builtin_amdgcn_readlane(dword, 1), cnt = __builtin_amdgcn_readlane(dword, 2);
+    int dword = 0, r, p0, cnt, cnts[2] = {0, 0};
+    if constexpr (E::gated) {
+        const i32x4 pair = ep.pairs[blockIdx.x % (unsigned)R];   // R: their number
+        const int first = pair.y, up = pair.z, end = pair.w;
+        r = pair.x;
+        cnts[0] = up - first;
+        cnts[1] = end - up;
+        p0 = half ? up : first;
+        cnt = cnts[half];
+        if (lane >= kRowDescColsAt && lane < kRowDescWords && lane - kRowDescColsAt < cnt) dword = indices[p0 + lane - kRowDescColsAt];
+    } else {
+        dword = lane < kRowDescWords ? desc[lane] : 0;
+        r = __builtin_amdgcn_readlane(dword, 0);
+        if (r < 0) return;                            // whole workgroup leaves together
+        p0 = __builtin_amdgcn_readlane(dword, 1);
+        cnt = __builtin_amdgcn_readlane(dword, 2);
+    }
     const int i_base = (items ? __builtin_amdgcn_readlane(dword, 3) : (int)(blockIdx.x / (unsigned)R)) * MM;
     // wavefronts that take part: about `per` stored blocks each, at most all of the workgroup's;
     // the others go straight to the barrier
-    const int nw = max(1, min(nw_max, (cnt + per - 1) / per));
+    auto taking = [&](int count) { return max(1, min(nw_half, (count + per - 1) / per)); };
+    const int nw = taking(cnt);
     // Wavefront w of a workgroup runs on SIMD w mod 4 and the low-numbered wavefronts get a block-row's
     // odd blocks.  The workgroups stacked on one CU (table entries b, b + #CUs, ...) therefore number
     // their wavefronts from different starts: `wave` is the number used for sharing out blocks and
     // for the order of the final sum; wavefronts nw and up take no part.
-    const int wave = hw_wave < nw ? (hw_wave + (items ? (int)(blockIdx.x / (unsigned)items) : 0)) % nw : hw_wave;
+    const int mine_hw = E::gated ? hw_wave - half * nw_half : hw_wave;
+    const int wave = mine_hw < nw ? (mine_hw + (items ? (int)(blockIdx.x / (unsigned)items) : 0)) % nw : mine_hw;
+    const int region = E::gated ? half * nw_half + wave : wave;
 
     acc_t acc[NA];
 #pragma unroll
@@ -137,7 +155,7 @@ __global__ __launch_bounds__(BS_R == 16 ? 1024 : 512) void bsr_mfma_ksplit(const
 #pragma unroll
         for (int e = 0; e < NE; ++e) acc[u][e] = 0.f;
 
-    unsigned char* wl = lds + (size_t)wave * geo::REGION;      // this wavefront's W block, [BS_R][P]
+    unsigned char* wl = lds + (size_t)region * geo::REGION;    // this wavefront's W block, [BS_R][P]
     unsigned char* xl = wl + BS_R * P;                         // and X tile, [MM][P]
 
     if (wave < nw && wave < cnt) {                     // this wavefront has at least one block
@@ -245,6 +263,30 @@ __global__ __launch_bounds__(BS_R == 16 ? 1024 : 512) void bsr_mfma_ksplit(const
 
     // fixed-order sum over the partial tiles; each thread owns 4 consecutive columns of one row
     constexpr int QUADS = BS_R / 4;
+    if constexpr (E::gated) {
+        constexpr int U = STR * BS_R;                 // rows of a stored block: a half's columns that stand together
+        const int strip_at = STR > 1 ? (int)blockIdx.y * BS_R : 0;
+        for (int t = threadIdx.x; t < MM * QUADS; t += blockDim.x) {
+            const int i = t / QUADS, q = t - i * QUADS;
+            const int at = strip_at + 4 * q, j = 2 * r * U + at;
+            bias_run<T, 4> bg, bu;
+            bg.fetch(ep, j);
+            bu.fetch(ep, j + U);
+            f32x4 s[2];
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                s[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const int parts = min(taking(cnts[hf]), cnts[hf]);
+                for (int w = 0; w < parts; ++w)
+                    s[hf] += *reinterpret_cast<const f32x4*>(lds + (size_t)(hf * nw_half + w) * geo::REGION + ((size_t)i * LD + 4 * q) * 4);
+            }
+            if (i_base + i >= m) continue;
+            float g[4] = {s[0].x, s[0].y, s[0].z, s[0].w}, u[4] = {s[1].x, s[1].y, s[1].z, s[1].w};
+            finish_gate<T, O>(ep, bg, bu, g, u, i_base + i, j, U, n);
+            store_run(Y + (size_t)(i_base + i) * (size_t)(n / 2) + (r * U + at), g);
+        }
+        return;
+    }
     for (int t = threadIdx.x; t < MM * QUADS; t += blockDim.x) {
         const int i = t / QUADS, q = t - i * QUADS;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -260,7 +302,7 @@ bsr_status launch_ksplit_tile(const spmm_args& a, const tune_opts& tune)
 {
     typedef ksplit_geom<T, BS_R, BS_C, MM> geo;
     const bsr_matrix* W = a.W;
-    const int m = (int)a.m, n = (int)W->n, k = (int)W->k, R = W->R;
+    const int m = (int)a.m, n = (int)W->n, k = (int)W->k, R = a.gated ? W->R / 2 : W->R;   // gated: pairs of block-rows
     // 32-bit byte offsets inside a block-row's blocks and inside an m-tile's rows of X
     if ((int64_t)W->max_row_blocks * geo::BLK * STR >= ((int64_t)1 << 31) || (int64_t)MM * k * geo::S >= ((int64_t)1 << 31))
         return BSR_ERR_UNSUPPORTED;
@@ -280,18 +322,20 @@ bsr_status launch_ksplit_tile(const spmm_args& a, const tune_opts& tune)
     if (STR > 1) nw_cap = blocks * STR <= 256 ? 16 : (blocks * STR <= (W->long_rows > 0 ? 4096 : 512) ? 8 : 4);
     nw = nw < 1 ? 1 : (nw > nw_cap ? nw_cap : nw);
     if (tune.nw >= 1 && tune.nw <= (BS_R == 16 ? 16 : 8)) nw = tune.nw;
+    // gated: as many wavefronts for each of the two block-rows as one has otherwise where that fits a workgroup
+    if (a.gated) nw = std::min(2 * nw, std::min(BS_R == 16 ? 16 : 8, 160 * 1024 / geo::REGION) & ~1);
     nw = std::min(nw, 160 * 1024 / geo::REGION);
     if (blocks >= ((int64_t)1 << 31) || blocks * STR * 64 * nw >= ((int64_t)1 << 32)) return BSR_ERR_SHAPE;
     // CU-balanced work-item table when there are more items than CUs (else every item has a CU to itself)
     const int32_t* table = W->row_desc;
     int items = 0;
-    if (tune.b != 1 && blocks > 256 && blocks <= kMaxKsplitItems) {
+    if (tune.b != 1 && blocks > 256 && blocks <= kMaxKsplitItems && !a.gated) {
         const int32_t* item_table = nullptr;
         const int grid = ksplit_items(W, (int)tiles, a.stream, &item_table);
         if (grid > 0) { table = item_table; items = W->n_cu; blocks = grid; }
     }
     const size_t lds = (size_t)nw * geo::REGION;
-    return with_epilogue(a, [&](auto ep) -> bsr_status {
+    return with_epilogue_or_gate(a, [&](auto ep) -> bsr_status {
         static const hipError_t attr =
             hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_ksplit<T, O, BS_R, BS_C, MM, STR, decltype(ep)>),
                                 hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
@@ -328,7 +372,7 @@ bsr_status launch_ksplit_shape(const spmm_args& a, const tune_opts& tune)
 {
     if constexpr (BS_R >= 32) {
         if (tune.mt == 3 || (tune.mt == 0 && in_strips<T>(a.W, a.m))) return launch_ksplit_tile<T, O, 16, BS_C, 16, BS_R / 16>(a, tune);
-        const int64_t items32 = (a.m + 31) / 32 * a.W->R;
+        const int64_t items32 = (a.m + 31) / 32 * (a.gated ? a.W->R / 2 : a.W->R);
         const bool slow16 = sizeof(T) == 2 && BS_C < 32;
         bool tall = items32 >= 768 || slow16;
         if (tune.mt == 1) tall = false;

@@ -224,6 +224,53 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
     // multiple of a row's pieces.
     auto quad_of = [&](int t) { return E::on ? t / TPR % Q : t / (RP * TPR); };
     auto row_of = [&](int t) { return E::on ? t / TPR / Q : t / TPR % RP; };
+    if constexpr (E::gated) {
+        // A quad's 64 outputs are its gate's and the other half's in turn, bs_r columns each: 32 of H.
+        constexpr int TPH = 32 / EPT;                 // threads of a quad's row
+        const int c0 = tid % TPH * EPT, gate0 = (c0 & -bs_r) + c0, q0 = tid / TPH % Q;   // (a thread keeps its columns)
+        bias_run<T, EPT> bg, bu;
+#pragma unroll
+        for (int p = 0; p < 16 * SUB / RP; ++p) {
+            __syncthreads();
+            if (wave < kWaves) {
+                float* mine = tiles + (size_t)wave * RP * kLdOut;
+#pragma unroll
+                for (int ss = 0; ss < RP / 16; ++ss)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<f32x4*>(mine + (ss * 16 + li) * kLdOut + j * 16 + 4 * h) = acc[j][p * (RP / 16) + ss];
+            }
+            __syncthreads();
+            const int col = column[q0] + gate0;
+            if (p == 0) {
+                const int at = min(col, n - bs_r - EPT);
+                bg.fetch(ep, at);
+                bu.fetch(ep, at + bs_r);
+            }
+            for (int t = tid; t < Q * RP * TPH; t += 64 * (kWaves + kLoaders)) {
+                const int row = t / TPH / Q, i = i_base + p * RP + row;
+                if (col >= n || i >= m) continue;
+                const float* src = tiles + ((size_t)(q0 * KS) * RP + row) * kLdOut + gate0;
+                float g[EPT], u[EPT];
+                load_run<float>(g, src);
+                load_run<float>(u, src + bs_r);
+                for (int s = 1; s < KS; ++s) {
+                    src += RP * kLdOut;
+                    float a[EPT], b[EPT];
+                    load_run<float>(a, src);
+                    load_run<float>(b, src + bs_r);
+#pragma unroll
+                    for (int e = 0; e < EPT; ++e) {
+                        g[e] += a[e];
+                        u[e] += b[e];
+                    }
+                }
+                finish_gate<T, O>(ep, bg, bu, g, u, i, col, bs_r, n);
+                store_run(Y + (size_t)i * (size_t)(n / 2) + (size_t)(column[q0] / 2 + c0), g);
+            }
+        }
+        return;
+    }
     [[maybe_unused]] bias_run<T, EPT> bias;
 #pragma unroll
     for (int p = 0; p < 16 * SUB / RP; ++p) {
@@ -336,7 +383,7 @@ bsr_status launch_sub(const spmm_args& a, int q_log)
     const int64_t blocks = (int64_t)padded * n_groups;
     if (blocks >= ((int64_t)1 << 31)) return BSR_ERR_SHAPE;
     constexpr size_t ring = (size_t)kRing * SUB * kPitch, out = (size_t)kWaves * (SUB >= 2 ? kRowsOut : 16) * kLdOut * sizeof(float);
-    return with_epilogue(a, [&](auto ep) -> bsr_status {
+    auto launch = [&](auto ep) -> bsr_status {
         static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&bsr_mfma_sweep<T, O, SUB, OWN, decltype(ep)>),
                                                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)std::max(ring, out));
         if (attr != hipSuccess) return BSR_ERR_HIP;
@@ -347,7 +394,9 @@ bsr_status launch_sub(const spmm_args& a, int q_log)
                            n_tiles, padded, W->sw_quads, W->sw_windows, q_log, W->bs_r, W->bs_c * (int)sizeof(T),
                            W->indptr, W->indices, ep);
         return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
-    });
+    };
+    if constexpr (OWN) return a.gated ? BSR_ERR_UNSUPPORTED : with_epilogue(a, launch);
+    else return with_epilogue_or_gate(a, launch);
 }
 
 // A result in fp32 keeps as many chains of additions as the kernel of 16x16 tiles gives it: 8 where that starts few
@@ -484,6 +533,21 @@ bool sweep_is_quicker(const bsr_matrix* W, int64_t m, bsr_dtype y_dtype, sweep_r
         (!quicker(W, m, y_dtype, than, W->nnzb / (4 * slots * (16 / W->bs_r)), W->max_row_blocks / slots) || !count_rounds(W)))
         return false;
     return quicker(W, m, y_dtype, than, W->sw.rounds, W->sw.longest);
+}
+
+// Fitted to 56 gated bf16 products of 16x16 blocks (8 to 4096 rows, (512 .. 6000, 2 x 768 .. 2 x 4096), 5 and 20 %): this kernel's
+// estimate is within 12 % of its time, the k-split kernel's within 30 % (where they differ most it is the slower by far: 4096 x
+// (1024, 2 x 4096), 5 %: 94 us, this one 34); the choice costs 0.4 us at most.  Below 16 rows of 8-wide blocks the wavefront
+// kernels start a wavefront for each output and four rows of X (8 x (1024, 2 x 4096) 20 %: 7.2 us, this one 5.4) and read X through
+// L2 once for each output (8 x (6000, 2 x 2048) 20 %: 13.1, 9.5; 5 %: 5.8, 7.8).
+bool sweep_gates_quicker(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype)
+{
+    if (!count_rounds(W)) return false;
+    const double mt = (double)((m + 15) / 16);
+    const double us = 2.8 + 1.03 * choose(W, m, most_quads(W, m, h_dtype == BSR_F32), W->sw.rounds, W->sw.longest).us + 1e-6 * mt * (double)W->n;
+    if (W->bs_r == 16 && W->bs_c == 16) return us < 2.9 + 1.4e-3 * mt * (W->R / 2) + 5.5e-5 * mt * (double)W->nnzb + 0.03 * W->max_row_blocks;
+    const double waves = (double)(W->n / 2) * (double)(m > 8 ? (m + 7) / 8 : (m + 3) / 4);
+    return us < 3.4 + 4.4e-4 * waves + 0.7e-7 * (W->dtype == BSR_F32 ? 4 : 2) * (double)m * (double)W->nnzb * W->bs_r * W->bs_c;
 }
 
 bool sweep_leaves_tiles(bsr_matrix* W, const int32_t* indptr, const int32_t* indices)

@@ -40,8 +40,11 @@ struct slot_groups {
     int start[kMaxGroups + 1];
 };
 
+// Wavefronts a SIMD that a gated product's registers are held to (two halves' sums, and the compiler takes more than it needs).
+template <typename T> constexpr int gated_waves(int bs_r, int bs_c) { return sizeof(T) == 4 ? (bs_r * bs_c > 1024 ? 2 : 3) : bs_r == 64 ? 3 : 4; }
+
 template <typename T, typename O, int BS_R, int BS_C, int MT, int D, typename E>
-__global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, const T* __restrict__ data,
+__global__ __launch_bounds__(256, E::gated ? gated_waves<T>(BS_R, BS_C) : 1) void bsr_mfma_tile(const T* __restrict__ X, const T* __restrict__ data,
                                                      const int32_t* __restrict__ indices,
                                                      const int32_t* __restrict__ row_desc, O* __restrict__ Y,
                                                      int m, int k, int n, int R, int n_tiles, slot_groups groups, E ep)
@@ -88,18 +91,42 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
     if (tile >= n_tiles) return;                      // whole workgroup leaves together
     const int i_base = tile * TM;
 
+    // (gated: the slots are pairs of block-rows, whose stored blocks follow one another; from block pm on they are the second's)
     const int32_t* __restrict__ desc = row_desc + (size_t)slot * kRowDescWords;
-    const int r = desc[0];
-    const int p0 = desc[1], p1 = p0 + desc[2];
+    int r, p0, p1, pm = 0;
+    if constexpr (E::gated) {
+        const i32x4 pair = ep.pairs[slot];
+        r = pair.x;
+        p0 = pair.y;
+        pm = pair.z;
+        p1 = pair.w;
+    } else {
+        r = desc[0];
+        p0 = desc[1];
+        p1 = p0 + desc[2];
+    }
 
     typedef f32x16 acc_t;
-    acc_t acc[NA][MT];
+    acc_t acc[NA][MT], first[E::gated ? NA : 1][E::gated ? MT : 1];   // first: the gate's sums, once they are done
+    auto clear = [&]() {
 #pragma unroll
-    for (int u = 0; u < NA; ++u)
+        for (int u = 0; u < NA; ++u)
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+            for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[u][t][e] = 0.f;
+                for (int e = 0; e < 16; ++e) acc[u][t][e] = 0.f;
+    };
+    clear();
+    auto next_half = [&]() {
+        if constexpr (E::gated) {
+#pragma unroll
+            for (int u = 0; u < NA; ++u)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) first[u][t] = acc[u][t];
+            clear();
+        }
+    };
+    if (E::gated) next_half();
 
     // staging map: thread tid moves 16-byte chunk tid + 256*j.  The first NLX chunks per thread
     // are X rows, the next NLW the W block (NLX, NLW known at compile time, so every trip issues
@@ -193,7 +220,7 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
 #pragma unroll
         for (int d = 0; d < D; ++d) {                 // the first D block-columns come from the descriptor
             const int j0 = min(d, p1 - 1 - p0);
-            fetch(d, p0 + d, j0 < kRowDescCols ? desc[kRowDescColsAt + j0] : indices[p0 + j0]);
+            fetch(d, p0 + d, !E::gated && j0 < kRowDescCols ? desc[kRowDescColsAt + j0] : indices[p0 + j0]);
         }
         for (int p = p0; p < p1; p += D) {
 #pragma unroll
@@ -204,6 +231,7 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
                 __syncthreads();                      // tile of block p+d visible
                 fetch(d, p + d + D, __builtin_amdgcn_readfirstlane(cidx[d]));
                 if (p + d < p1) compute();            // uniform over the workgroup
+                if (E::gated && p + d == pm - 1) next_half();   // uniform
                 __syncthreads();                      // everyone done reading before the next stash
             }
         }
@@ -220,6 +248,44 @@ __global__ __launch_bounds__(256) void bsr_mfma_tile(const T* __restrict__ X, co
     constexpr int OC = OB / 16;                       // 16-byte pieces per output row
     constexpr int RPP = 64 / OC;                      // rows one wavefront stores per pass
     static_assert(OB % 16 == 0 && 64 % OC == 0 && (MT * MM) % RPP == 0, "output tile splits into 16-byte pieces");
+    if constexpr (E::gated) {
+        // Both halves' sums in fp32, 16 rows at a time: a lane finishes pieces of H of the same columns.
+        constexpr int FS = 2 * BS_R * 4 + 16;         // padded LDS stride: the gate's columns, then the others
+        constexpr int EPP = 16 / (int)sizeof(O);      // outputs of a piece
+        unsigned char* fl = lds + (size_t)wave * 16 * FS;
+        const int frow = lane / OC, at = (lane - frow * OC) * EPP, j = 2 * r * BS_R + at;
+        bias_run<T, EPP> bg, bu;
+        bg.fetch(ep, j);
+        bu.fetch(ep, j + BS_R);
+        static_assert(!E::gated || MT == 1, "one tile along m");
+#pragma unroll 1                                      // (side by side the steps take registers of which the wavefronts are short)
+        for (int q = 0; q < 2; ++q) {
+            wave_lds_fence();                         // the other lanes have read the rows before
+            if (li / 16 == q)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                    for (int u = 0; u < NA; ++u)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const acc_t& a = hf ? acc[u][0] : first[u][0];
+                            *reinterpret_cast<f32x4*>(fl + (size_t)(li % 16) * FS + (hf * BS_R + u * 32 + 8 * g + 4 * h) * 4) =
+                                f32x4{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]};
+                        }
+            wave_lds_fence();
+#pragma unroll 1
+            for (int pass = 0; pass < 16 / RPP; ++pass) {
+                const int row = pass * RPP + frow, i = i_base + wave * MM + q * 16 + row;
+                float g[EPP], u[EPP];
+                load_run<float>(g, reinterpret_cast<const float*>(fl + (size_t)row * FS) + at);
+                load_run<float>(u, reinterpret_cast<const float*>(fl + (size_t)row * FS) + BS_R + at);
+                if (i >= m) continue;
+                finish_gate<T, O>(ep, bg, bu, g, u, i, j, BS_R, n);
+                store_run<true>(Y + (size_t)i * (size_t)(n / 2) + (r * BS_R + at), g);
+            }
+        }
+        return;
+    }
     if constexpr (E::on) {
         // The same with the sums in fp32 (rounded once, behind the epilogue), 16 rows at a time: no more LDS than the
         // staging takes, so as many workgroups share a CU as without an epilogue.
@@ -293,7 +359,7 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
         return BSR_ERR_UNSUPPORTED;
     } else {
         const bsr_matrix* W = a.W;
-        const int m = (int)a.m, n = (int)W->n, k = (int)W->k, R = W->R;
+        const int m = (int)a.m, n = (int)W->n, k = (int)W->k, R = a.gated ? W->R / 2 : W->R;   // gated: pairs of block-rows
         auto go = [&](auto mt_tag, auto d_tag) -> bsr_status {
             constexpr int MT = decltype(mt_tag)::value;
             constexpr int D = decltype(d_tag)::value;
@@ -306,16 +372,18 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
             const int first = std::min(std::max(a.first_slot, 0), R);
             if (first >= R) return BSR_OK;
             {
-                const int n_long = std::max(W->long_rows, first);
+                const int n_long = a.gated ? first : std::max(W->long_rows, first);   // (pairs come as they are)
                 const size_t block_bytes = (size_t)BS_R * BS_C * sizeof(T);
-                int64_t target = tune.b > 0 ? tune.b : (int64_t)((3u << 19) / block_bytes);
+                // (gated: the longest pairs in groups of 64 blocks, then an m-tile through all others: 8192 x (8192, 2 x 8192) f16
+                // 64x64 5 %, power law 206 us, in groups of 1.5 MB 224; 4096 x (2048, 2 x 2048) bf16 64x32 10 % 19.5, 23.0)
+                int64_t target = tune.b > 0 ? tune.b : a.gated ? 64 : (int64_t)((3u << 19) / block_bytes);
                 if (target < 1) target = 1;
                 int g = 0;
                 groups.start[0] = first;
                 if (n_long > first) groups.start[++g] = n_long;
                 int64_t acc_blocks = 0;
                 for (int s = n_long; s < R; ++s) {
-                    acc_blocks += W->slot_blocks[(size_t)s];
+                    acc_blocks += a.gated ? std::max<int64_t>(W->nnzb / R, 1) : W->slot_blocks[(size_t)s];
                     if (acc_blocks >= target && g < kMaxGroups - 1 && s + 1 < R) { groups.start[++g] = s + 1; acc_blocks = 0; }
                 }
                 groups.start[++g] = R;
@@ -326,7 +394,8 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
             if (blocks >= ((int64_t)1 << 31) || blocks * 256 >= ((int64_t)1 << 32)) return BSR_ERR_SHAPE;
             const size_t lds_stage = (size_t)(TM + BS_R) * (BS_C * sizeof(T) + 16);
             auto launch = [&](auto ep) -> bsr_status {
-                const size_t lds_out = decltype(ep)::on ? (size_t)4 * 16 * (BS_R * 4 + 16) : (size_t)TM * (BS_R * sizeof(O) + 16);
+                const size_t lds_out = decltype(ep)::gated ? (size_t)4 * 16 * (2 * BS_R * 4 + 16)
+                                     : decltype(ep)::on ? (size_t)4 * 16 * (BS_R * 4 + 16) : (size_t)TM * (BS_R * sizeof(O) + 16);
                 const size_t lds = lds_stage > lds_out ? lds_stage : lds_out;
                 if (lds > 48 * 1024) {                // above the default dynamic-LDS limit: raise it once
                     static const hipError_t attr = hipFuncSetAttribute(
@@ -340,11 +409,14 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
                 return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
             };
             if constexpr (D > 2) return launch(no_epilogue{});
-            else return with_epilogue(a, launch);
+            else if constexpr (MT > 1) return a.gated ? BSR_ERR_UNSUPPORTED : with_epilogue(a, launch);   // (two halves' sums of 64x64 fp32 blocks: no registers)
+            else return with_epilogue_or_gate(a, launch);
         };
         // (three and four blocks in flight are candidates of bsr_tune() alone: with an epilogue two take their place, for
         // the same sums -- each further one is 18 more kernels of this file, which takes longest to compile)
-        const int depth = std::min(tune.a > 0 ? tune.a : 2, a.epilogue ? 2 : 4);
+        // Gated: one, which leaves room for more wavefronts beside two halves' sums (two, us, and one: 4096 x (1024, 2 x 4096) bf16
+        // 32x32 5 % 24.4, 22.0; fp32 64x64 10 % 88, 84; 2048 x (4096, 2 x 4096) fp32 32x32 10 % 152, 141; f16 64x64 within 3 %).
+        const int depth = std::min(tune.a > 0 ? tune.a : a.gated ? 1 : 2, a.epilogue || a.gated ? 2 : 4);
         if (tune.mt == 1) {
             if (depth == 1) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
             if (depth == 2) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});

@@ -68,6 +68,45 @@ __global__ __launch_bounds__(256) void bsr_wave_generic(const T* __restrict__ X,
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int js = (int)(blockIdx.x % (unsigned)col_groups) * 4 + wave;     // slot*bs_r + a
     const int i0 = (int)(blockIdx.x / (unsigned)col_groups) * TM;
+    if constexpr (E::gated) {                        // column a of block-rows 2 pair and 2 pair + 1, whose stored blocks follow one another
+        if (js >= n / 2) return;
+        const int pair = js / bs_r, a = js - pair * bs_r, j = 2 * pair * bs_r + a;
+        const int p0 = ep.indptr[2 * pair], pm = ep.indptr[2 * pair + 1], vpr = bs_c / VEC;
+        const int first_up = (pm - p0) * vpr, len = (ep.indptr[2 * pair + 2] - p0) * vpr;
+        float g[TM], u[TM];
+#pragma unroll
+        for (int t = 0; t < TM; ++t) g[t] = u[t] = 0.f;
+        auto add = [&](float (&acc)[TM], int e) {
+            const int q = e / vpr, c = (e - q * vpr) * VEC, p = p0 + q;
+            const vec_t w = *reinterpret_cast<const vec_t*>(data + ((size_t)p * bs_r + a) * bs_c + c);
+            const int col = indices[p] * bs_c + c;
+            vec_t x[TM];
+#pragma unroll
+            for (int t = 0; t < TM; ++t) x[t] = *reinterpret_cast<const vec_t*>(X + (size_t)min(i0 + t, m - 1) * (size_t)k + col);
+#pragma unroll
+            for (int t = 0; t < TM; ++t)
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) acc[t] = fmaf(to_f32(x[t].v[v]), to_f32(w.v[v]), acc[t]);
+        };
+        for (int e = lane; e < first_up; e += 64) add(g, e);
+        for (int e = first_up + lane; e < len; e += 64) add(u, e);
+        float gate[1] = {0.f}, up[1] = {0.f};
+#pragma unroll
+        for (int t = 0; t < TM; ++t) {               // lane t finishes row t
+            const float sg = wave_sum(g[t]), su = wave_sum(u[t]);
+            gate[0] = lane == t ? sg : gate[0];
+            up[0] = lane == t ? su : up[0];
+        }
+        const int i = i0 + lane;
+        if (lane < TM && i < m) {
+            bsr_dev::bias_run<T, 1> bg, bu;
+            bg.fetch(ep, j);
+            bu.fetch(ep, j + bs_r);
+            bsr_dev::finish_gate<T, O>(ep, bg, bu, gate, up, i, j, bs_r, n);
+            Y[(size_t)i * (size_t)(n / 2) + js] = from_f32<O>(gate[0]);
+        }
+        return;
+    }
     if (js >= n) return;                             // whole wave leaves together; no barrier in this kernel
     const int slot = js / bs_r, a = js - slot * bs_r;
     const int32_t* __restrict__ desc = row_desc + (size_t)slot * kRowDescWords;
@@ -123,13 +162,13 @@ bsr_status launch_generic(const spmm_args& a, const tune_opts& tune)
 {
     const bsr_matrix* W = a.W;
     const int m = (int)a.m, n = (int)W->n, k = (int)W->k;
-    const int col_groups = (n + 3) / 4;
+    const int col_groups = ((a.gated ? n / 2 : n) + 3) / 4;
     auto go = [&](auto tm_tag, auto vec_tag) -> bsr_status {
         constexpr int TM = decltype(tm_tag)::value, VEC = decltype(vec_tag)::value;
         const int64_t row_groups = (m + TM - 1) / TM;
         const int64_t blocks = row_groups * col_groups;
         if (blocks >= ((int64_t)1 << 31) || blocks * 256 >= ((int64_t)1 << 32)) return BSR_ERR_SHAPE;
-        return with_epilogue(a, [&](auto ep) -> bsr_status {
+        return with_epilogue_or_gate(a, [&](auto ep) -> bsr_status {
             hipLaunchKernelGGL((bsr_wave_generic<T, O, TM, VEC, decltype(ep)>), dim3((unsigned)blocks), dim3(256), 0, a.stream,
                                (const T*)a.X, (const T*)W->data, W->indices, W->row_desc, (O*)a.Y, m, k, n,
                                (int)W->bs_r, (int)W->bs_c, col_groups, ep);
