@@ -61,59 +61,145 @@ struct muon_args {
 // Wavefronts of a workgroup, a block each: as many as 64 KB of LDS hold, four at most.
 constexpr int waves_of(int rt, int ct) { return rt * ct > 8 ? 2 : 4; }
 
-template <typename T> __device__ __forceinline__ f32x4 load_as(const void* p, size_t at, int count, bool whole)
+// Where four neighbouring elements of a lane are: `count` of them belong to the block, from `at` on.
+struct run_at { size_t at; int count; };
+
+// Tiles of a tensor of type T as fp32 numbers, zeros where a run ends.  All reads are under way before the first is used.  WHOLE: runs
+// hold four elements or none, at a multiple of their size; `safe`: an element to read where there is none.
+template <typename T, bool WHOLE, int CT, int RT, typename F>
+__device__ __forceinline__ void load_runs(f32x4 (&v)[CT][RT], const void* p, size_t safe, F run_of)
 {
     typedef T t4 __attribute__((ext_vector_type(4)));
-    const T* const from = static_cast<const T*>(p) + at;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (whole) {
-        if (count >= 4) {
-            const t4 t = *reinterpret_cast<const t4*>(from);
+    const T* const from = static_cast<const T*>(p);
+    if constexpr (WHOLE) {
+        t4 raw[CT][RT];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = (float)t[e];
-        }
+        for (int J = 0; J < CT; ++J)
+#pragma unroll
+            for (int I = 0; I < RT; ++I) {
+                const run_at r = run_of(J, I);
+                raw[J][I] = *reinterpret_cast<const t4*>(from + (r.count >= 4 ? r.at : safe));
+            }
+#pragma unroll
+        for (int J = 0; J < CT; ++J)
+#pragma unroll
+            for (int I = 0; I < RT; ++I)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[J][I][e] = run_of(J, I).count >= 4 ? (float)raw[J][I][e] : 0.f;
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < count) v[e] = (float)from[e];
+        for (int J = 0; J < CT; ++J)
+#pragma unroll
+            for (int I = 0; I < RT; ++I)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const run_at r = run_of(J, I, e);
+                    const float x = (float)from[r.count > 0 ? r.at : safe];
+                    v[J][I][e] = r.count > 0 ? x : 0.f;
+                }
     }
-    return v;
 }
-// Up to four neighbouring elements of a tensor of any type; `whole`: four or none, at a multiple of their size.
-__device__ __forceinline__ f32x4 load4(const void* p, int dtype, size_t at, int count, bool whole)
-{
-    if (dtype == BSR_F32) return load_as<float>(p, at, count, whole);    // uniform
-    if (dtype == BSR_F16) return load_as<f16_t>(p, at, count, whole);
-    return load_as<bf16_t>(p, at, count, whole);
-}
-template <typename T> __device__ __forceinline__ void put4(T* to, const T (&v)[4], int count, bool whole)
+template <typename T, bool WHOLE, typename F> __device__ __forceinline__ void store_run4(T* to, const T (&v)[4], int J, int I, F run_of)
 {
     typedef T t4 __attribute__((ext_vector_type(4)));
-    if (whole) {
-        if (count >= 4) *reinterpret_cast<t4*>(to) = t4{v[0], v[1], v[2], v[3]};
+    if constexpr (WHOLE) {
+        const run_at r = run_of(J, I);
+        if (r.count >= 4) *reinterpret_cast<t4*>(to + r.at) = t4{v[0], v[1], v[2], v[3]};
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < count) to[e] = v[e];
+        for (int e = 0; e < 4; ++e) {
+            const run_at r = run_of(J, I, e);
+            if (r.count > 0) to[r.at] = v[e];
+        }
     }
 }
 
-// RT, CT: 16x16 tiles of a block down and across.
-template <int RT, int CT>
-__global__ __launch_bounds__(64 * waves_of(RT, CT)) void bsr_muon_blocks(const muon_desc* __restrict__ tensors, const int2* __restrict__ chunks, muon_args h)
+__device__ __forceinline__ double shared_sum(double v, int lane_xor)
+{
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const int lo = __shfl_xor((int)(unsigned)u, lane_xor), hi = __shfl_xor((int)(unsigned)(u >> 32), lane_xor);
+    return v + __builtin_bit_cast(double, (unsigned long long)(unsigned)lo | ((unsigned long long)(unsigned)hi << 32));
+}
+
+// fp32 products on the bf16 matrix cores, which take a sixteenth of the time: x = hi + mid + lo, three bf16 numbers, exactly (8 of
+// its 24 bits each), and of the nine products of two such sums the six largest; the others are below 2^-26 of the whole, less
+// than fp32 products lose by rounding.  A lane's eight terms are those of two tiles, four each.
+struct parts { u32x4 hi, mid, lo; };
+__device__ __forceinline__ parts parts_of(const f32x4& a, const f32x4& b)
+{
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    parts out;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        f32x2 x = q < 2 ? f32x2{a[2 * q], a[2 * q + 1]} : f32x2{b[2 * q - 4], b[2 * q - 3]};
+        uint32_t w[3];
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+            w[part] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+            if (part < 2) {
+                x.x -= __builtin_bit_cast(float, w[part] << 16);
+                x.y -= __builtin_bit_cast(float, w[part] & 0xFFFF0000u);
+            }
+        }
+        out.hi[q] = w[0];
+        out.mid[q] = w[1];
+        out.lo[q] = w[2];
+    }
+    return out;
+}
+__device__ __forceinline__ void mfma_bf16(f32x4& acc, const u32x4& a, const u32x4& b)
+{
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+// acc[t] += left^T right[t], the small products first
+template <int S> __device__ __forceinline__ void add_row(f32x4 (&acc)[S], const parts& left, const parts (&right)[S])
+{
+#pragma unroll
+    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.lo, right[t].hi);
+#pragma unroll
+    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.hi, right[t].lo);
+#pragma unroll
+    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.mid, right[t].mid);
+#pragma unroll
+    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.mid, right[t].hi);
+#pragma unroll
+    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.hi, right[t].mid);
+#pragma unroll
+    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.hi, right[t].hi);
+}
+// acc[s][t] += operand(s)^T operand(t)
+template <int R, int S, typename F> __device__ __forceinline__ void add_product(f32x4 (&acc)[R][S], F operand)
+{
+    parts x[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) x[s] = operand(s);
+#pragma unroll
+    for (int s = 0; s < R; ++s) add_row<S>(acc[s], x[s], x);
+}
+
+// RT, CT: 16x16 tiles of a block down and across.  MODE: 0 a block a wavefront; where the smaller side is 8 at most, as many as fit
+// 16 beside one another along it, 1 down (bs_r <= bs_c), 2 across: G then holds their products with one another, too, which are
+// dropped, and P keeps them apart.  WHOLE: a lane's runs are four neighbouring elements of a block's row, or none.
+template <int RT, int CT, int MODE, bool WHOLE>
+__global__ __launch_bounds__(64 * waves_of(RT, CT), 2) void bsr_muon_blocks(const muon_desc* __restrict__ tensors, const int2* __restrict__ chunks, muon_args h)
 {
     constexpr int WAVES = waves_of(RT, CT);
-    constexpr bool TALL = RT > CT;
+    constexpr bool TALL = RT > CT || MODE == 2;
     constexpr int L = TALL ? RT : CT, S = TALL ? CT : RT;
-    constexpr int PW = S * 16 + 4, PY = RT * 16 + 4;  // pitches in LDS of W [L * 16][] and, where the block is turned, of its transpose
-    constexpr int AREA = std::max(L * 16 * PW, TALL ? CT * 16 * PY : 0);
+    static_assert(MODE == 0 || S == 1, "blocks beside one another fill one tile");
+    constexpr int PW = S * 16 + 4, PY = RT * 16 + 4;  // pitches in LDS of W [L * 16][], of the block's transpose [CT * 16][]
+    constexpr int AREA = std::max(L * 16 * PW, CT * 16 * PY);
     __shared__ __attribute__((aligned(16))) float areas[WAVES][AREA];
     const int lane = threadIdx.x & 63, i = lane & 15, c0 = (lane >> 4) * 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int2 where = chunks[blockIdx.x];            // {tensor, first block}
     const muon_desc& d = tensors[where.x];
-    const int64_t block = (int64_t)where.y + wave;
-    if (block >= d.blocks) return;                    // (no barrier below)
+    const int bs_r = d.bs_r, bs_c = d.bs_c, size = bs_r * bs_c;
+    const int small = MODE == 1 ? bs_r : bs_c, beside = MODE == 0 ? 1 : 16 / small;   // blocks of a wavefront
+    const int64_t block0 = (int64_t)where.y + (int64_t)wave * beside;
+    if (block0 >= d.blocks) return;                   // (no barrier below)
+    const int here = (int)min((int64_t)beside, d.blocks - block0);
     float* const area = areas[wave];
 
     float lr = h.lr, grad_scale = h.grad_scale;
@@ -129,61 +215,114 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT)) void bsr_muon_blocks(const m
         key = step_key(h.seed, (uint64_t)t);
     }
 
-    const int bs_r = d.bs_r, bs_c = d.bs_c;
-    const size_t first = (size_t)block * (size_t)(bs_r * bs_c);
-    const bool whole = (bs_c & 3) == 0;
-    // a lane's elements of tile (J, I): row 16 I + i of the block, columns 16 J + c0 .. + 3
-    auto count_of = [&](int J, int I) { return 16 * I + i < bs_r ? bs_c - (16 * J + c0) : 0; };
-    auto place_of = [&](int J, int I) { return (16 * I + i) * bs_c + 16 * J + c0; };
+    const size_t first = (size_t)block0 * (size_t)size;
+    // a lane's elements of tile (J, I): row 16 I + i, columns 16 J + c0 .. + 3, of the block or of the blocks beside one another
+    const int mine = MODE == 1 ? i / bs_r : 0, row0 = MODE == 1 ? i - mine * bs_r : i;
+    auto row_of = [&](int I) __attribute__((always_inline)) { return 16 * I + row0; };
+    auto run_of = [&](int J, int I, int e = 0) __attribute__((always_inline)) {
+        int b = mine, col = 16 * J + c0 + e;
+        if constexpr (MODE == 2) {
+            b = col / bs_c;
+            col -= b * bs_c;
+        }
+        const bool there = row_of(I) < bs_r && b < here;
+        return run_at{first + (size_t)(b * size + row_of(I) * bs_c + col), there ? bs_c - col : 0};
+    };
+    uint32_t mask = 0;                                // bit e: row c0 + e of G and this lane's column are of one block
+    if constexpr (MODE != 0)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mask |= (uint32_t)((c0 + e) / small == i / small) << e;
 
     f32x4 y[CT][RT];                                  // the block's transpose in result tiles
-    uint32_t top = 0;
+    auto read = [&](f32x4 (&v)[CT][RT], const void* p, int dtype) __attribute__((always_inline)) {   // dtype: uniform
+        if (dtype == BSR_F32) load_runs<float, WHOLE>(v, p, first, run_of);
+        else if (dtype == BSR_F16) load_runs<f16_t, WHOLE>(v, p, first, run_of);
+        else load_runs<bf16_t, WHOLE>(v, p, first, run_of);
+    };
+    constexpr bool kEarly = RT * CT <= 4;             // the parameter is read with the rest; larger blocks' registers are full until the steps are done
+    f32x4 param[CT][RT];
+    auto read_param = [&]() __attribute__((always_inline)) {
+        if (d.master) read(param, d.master, BSR_F32);
+        else read(param, d.param, d.dtype);
+    };
+    {
+        f32x4 m[CT][RT];
+        read(m, d.momentum, BSR_F32);
+        if (kEarly) read_param();
+        read(y, d.grad, d.grad_dtype);
 #pragma unroll
-    for (int J = 0; J < CT; ++J)
+        for (int J = 0; J < CT; ++J)
 #pragma unroll
-        for (int I = 0; I < RT; ++I) {
-            const int count = count_of(J, I);
-            const size_t at = first + (size_t)place_of(J, I);
-            f32x4 g = load4(d.grad, d.grad_dtype, at, count, whole), m = load4(d.momentum, BSR_F32, at, count, whole);
-            float mv[4];
+            for (int I = 0; I < RT; ++I) {
+                float mv[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float g = y[J][I][e] * grad_scale;
+                    mv[e] = fmaf(h.mu, m[J][I][e], g);
+                    y[J][I][e] = h.nesterov ? fmaf(h.mu, mv[e], g) : mv[e];
+                }
+                store_run4<float, WHOLE>(d.momentum, mv, J, I, run_of);
+            }
+    }
+    // A block that is not finite takes no part in the steps of those beside it, whose zeros its numbers would meet; it ends as NaN.
+    uint32_t spoilt = 0;                              // bit e: column c0 + e is of such a block
+    // |V|: squares and their sum in 64 bits, which hold those of any fp32 numbers
+    {
+        float over[4];                                // of the lane's four columns (MODE 2: they may be of four blocks)
+        auto inverse = [&](double sum) { return (float)(1.0 / (sqrt(sum) + (double)h.eps)); };
+        auto finite_sum = [&](double sum) { return sum - sum == 0.0; };
+        if constexpr (MODE == 2) {
+            double* const sums = reinterpret_cast<double*>(area);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                g[e] *= grad_scale;
-                mv[e] = fmaf(h.mu, m[e], g[e]);
-                y[J][I][e] = h.nesterov ? fmaf(h.mu, mv[e], g[e]) : mv[e];
-                top = max(top, bits_of(fabsf(y[J][I][e])));
+                double sum = 0.0;
+#pragma unroll
+                for (int I = 0; I < RT; ++I) sum += (double)y[0][I][e] * (double)y[0][I][e];
+                for (int x = 1; x < 16; x *= 2) sum = shared_sum(sum, x);
+                if (i == 0) sums[c0 + e] = sum;       // of column c0 + e
             }
-            put4(d.momentum + at, mv, count, whole);
+            wave_lds_fence();
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int b = (c0 + e) / bs_c;
+                double sum = 0.0;
+                if (b < here)
+                    for (int q = 0; q < bs_c; ++q) sum += sums[b * bs_c + q];
+                over[e] = inverse(sum);
+                spoilt |= (uint32_t)!finite_sum(sum) << e;
+            }
+            wave_lds_fence();
+        } else {
+            double sum = 0.0;
+#pragma unroll
+            for (int J = 0; J < CT; ++J)
+#pragma unroll
+                for (int I = 0; I < RT; ++I)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum += (double)y[J][I][e] * (double)y[J][I][e];
+            for (int x = MODE == 1 ? 16 : 1; x < 64; x *= 2) sum = shared_sum(sum, x);
+            if constexpr (MODE == 1) {                // of row i so far
+                double* const sums = reinterpret_cast<double*>(area);
+                if (lane < 16) sums[i] = sum;
+                wave_lds_fence();
+                sum = 0.0;
+                if (mine < here)
+                    for (int q = 0; q < bs_r; ++q) sum += sums[mine * bs_r + q];
+                wave_lds_fence();
+                spoilt = finite_sum(sum) ? 0u : 15u;
+            }
+            over[0] = over[1] = over[2] = over[3] = inverse(sum);
         }
-    // |V|, of V times a power of two that keeps the squares fp32 numbers
-    {
-        const int exponent = __builtin_amdgcn_frexp_expf(float_of(wave_max(top)));
-        float sum = 0.f;
 #pragma unroll
         for (int J = 0; J < CT; ++J)
 #pragma unroll
             for (int I = 0; I < RT; ++I)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float v = ldexpf(y[J][I][e], -exponent);
-                    sum = fmaf(v, v, sum);
-                }
-        sum += __builtin_bit_cast(float, dpp<0xB1>(bits_of(sum)));
-        sum += __builtin_bit_cast(float, dpp<0x4E>(bits_of(sum)));
-        sum += __builtin_bit_cast(float, dpp<0x141>(bits_of(sum)));
-        sum += __builtin_bit_cast(float, dpp<0x140>(bits_of(sum)));
-        sum += __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle((int)bits_of(sum), 0x401F));
-        sum = __builtin_bit_cast(float, __builtin_amdgcn_readlane((int)bits_of(sum), 0)) +
-              __builtin_bit_cast(float, __builtin_amdgcn_readlane((int)bits_of(sum), 32));
-        const float inverse = 1.f / (ldexpf(sqrtf(sum), exponent) + h.eps);
-#pragma unroll
-        for (int J = 0; J < CT; ++J)
-#pragma unroll
-            for (int I = 0; I < RT; ++I) y[J][I] *= inverse;
+                for (int e = 0; e < 4; ++e) y[J][I][e] = MODE != 0 && ((spoilt >> e) & 1) ? 0.f : y[J][I][e] * over[e];
     }
 
     f32x4 w[L][S];
-    if constexpr (TALL) {
+    auto put_y = [&]() __attribute__((always_inline)) {                              // and read turned_y: the tiles of its transpose
 #pragma unroll
         for (int J = 0; J < CT; ++J)
 #pragma unroll
@@ -191,18 +330,21 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT)) void bsr_muon_blocks(const m
 #pragma unroll
                 for (int e = 0; e < 4; ++e) area[(16 * J + c0 + e) * PY + 16 * I + i] = y[J][I][e];
         wave_lds_fence();
+    };
+    auto turned_y = [&](int I, int J) __attribute__((always_inline)) { return *reinterpret_cast<const f32x4*>(&area[(16 * J + i) * PY + 16 * I + c0]); };
+    if constexpr (TALL) {
+        put_y();
 #pragma unroll
         for (int I = 0; I < RT; ++I)
 #pragma unroll
-            for (int J = 0; J < CT; ++J) w[I][J] = *reinterpret_cast<const f32x4*>(&area[(16 * J + i) * PY + 16 * I + c0]);
-        wave_lds_fence();
+            for (int J = 0; J < CT; ++J) w[I][J] = turned_y(I, J);
     } else {
 #pragma unroll
         for (int J = 0; J < CT; ++J)
 #pragma unroll
             for (int I = 0; I < RT; ++I) w[J][I] = y[J][I];
     }
-    auto put_w = [&]() {
+    auto put_w = [&]() __attribute__((always_inline)) {
         wave_lds_fence();                             // the other lanes have read what was there
 #pragma unroll
         for (int l = 0; l < L; ++l)
@@ -212,7 +354,7 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT)) void bsr_muon_blocks(const m
                 for (int e = 0; e < 4; ++e) area[(16 * l + c0 + e) * PW + 16 * s + i] = w[l][s][e];
         wave_lds_fence();
     };
-    auto turned = [&](int s, int l) { return *reinterpret_cast<const f32x4*>(&area[(16 * l + i) * PW + 16 * s + c0]); };   // tile (s, l) of W^T
+    auto turned = [&](int s, int l) __attribute__((always_inline)) { return *reinterpret_cast<const f32x4*>(&area[(16 * l + i) * PW + 16 * s + c0]); };   // tile (s, l) of W^T
 
     for (int step = 0; step < h.ns_steps; ++step) {
         put_w();
@@ -221,41 +363,56 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT)) void bsr_muon_blocks(const m
         for (int s = 0; s < S; ++s)
 #pragma unroll
             for (int t = 0; t < S; ++t) g[s][t] = p[s][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (S == 1) {
 #pragma unroll
-        for (int l = 0; l < L; ++l)
+            for (int l = 0; l < L; ++l)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e) g[0][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[l][0][e], w[l][0][e], g[0][0], 0, 0, 0);
+            if constexpr (MODE != 0) {                // what is of two blocks is no part of either
 #pragma unroll
-                for (int s = 0; s < S; ++s)
+                for (int e = 0; e < 4; ++e) g[0][0][e] = ((mask >> e) & 1) ? g[0][0][e] : 0.f;
+            }
 #pragma unroll
-                    for (int t = 0; t < S; ++t) g[s][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[l][s][e], w[l][t][e], g[s][t], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) p[0][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(g[0][0][e], g[0][0][e], p[0][0], 0, 0, 0);
+        } else {
 #pragma unroll
-        for (int k = 0; k < S; ++k)
+            for (int k = 0; k < L; k += 2) add_product<S, S>(g, [&](int s) __attribute__((always_inline)) { return parts_of(w[k][s], k + 1 < L ? w[k + 1][s] : f32x4{}); });
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int s = 0; s < S; ++s)
-#pragma unroll
-                    for (int t = 0; t < S; ++t) p[s][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(g[k][s][e], g[k][t][e], p[s][t], 0, 0, 0);
+            for (int k = 0; k < S; k += 2) add_product<S, S>(p, [&](int s) __attribute__((always_inline)) { return parts_of(g[k][s], k + 1 < S ? g[k + 1][s] : f32x4{}); });
+        }
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
             for (int t = 0; t < S; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) p[s][t][e] = fmaf(h.b, g[s][t][e], h.c * p[s][t][e]);
+        if constexpr (S == 1) {
 #pragma unroll
-        for (int l = 0; l < L; ++l) {
-            f32x4 wt[S];
+            for (int l = 0; l < L; ++l) {
+                const f32x4 wt = turned(0, l);
+                w[l][0] *= h.a;
 #pragma unroll
-            for (int k = 0; k < S; ++k) wt[k] = turned(k, l);
+                for (int e = 0; e < 4; ++e) w[l][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(wt[e], p[0][0][e], w[l][0], 0, 0, 0);
+            }
+        } else {
+            // (a W from LDS: its registers were G^2's in the meantime)
 #pragma unroll
-            for (int t = 0; t < S; ++t) w[l][t] *= h.a;
+            for (int l = 0; l < L; ++l)
 #pragma unroll
-            for (int k = 0; k < S; ++k)
+                for (int t = 0; t < S; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                    for (int e = 0; e < 4; ++e) w[l][t][e] = h.a * area[(16 * l + c0 + e) * PW + 16 * t + i];
 #pragma unroll
-                    for (int t = 0; t < S; ++t) w[l][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(wt[k][e], p[k][t][e], w[l][t], 0, 0, 0);
+            for (int k = 0; k < S; k += 2) {
+                parts right[S];
+#pragma unroll
+                for (int t = 0; t < S; ++t) right[t] = parts_of(p[k][t], k + 1 < S ? p[k + 1][t] : f32x4{});
+#pragma unroll
+                for (int l = 0; l < L; ++l) {
+                    const parts left = parts_of(turned(k, l), k + 1 < S ? turned(k + 1, l) : f32x4{});
+                    add_row<S>(w[l], left, right);
+                }
+            }
         }
     }
     if constexpr (TALL) {
@@ -271,39 +428,69 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT)) void bsr_muon_blocks(const m
             for (int I = 0; I < RT; ++I) y[J][I] = w[J][I];
     }
 
+    if (MODE != 0 && spoilt)
+#pragma unroll
+        for (int J = 0; J < CT; ++J)
+#pragma unroll
+            for (int I = 0; I < RT; ++I)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[J][I][e] = (spoilt >> e) & 1 ? __builtin_nanf("") : y[J][I][e];
+
     const float keep = 1.f - lr * d.decay, rate = lr * d.scale;
-    const uint32_t base = mix(d.number + key) + (uint32_t)first;
-    const size_t to = d.transposed ? (size_t)d.place[block] * (size_t)(bs_r * bs_c) : 0;
-    auto update = [&](auto type, auto has_master) {
+    const uint32_t base = mix(d.number + key);
+    // the transposed copy: its rows by way of LDS, four neighbouring elements a lane, where they are whole runs of a block
+    const bool through = MODE != 2 && (bs_r & 3) == 0;
+    auto update = [&](auto type, auto has_master) __attribute__((always_inline)) {
         typedef decltype(type) T;
+        typedef T t4 __attribute__((ext_vector_type(4)));
         constexpr bool MASTER = decltype(has_master)::value;
 #pragma unroll
         for (int J = 0; J < CT; ++J)
 #pragma unroll
             for (int I = 0; I < RT; ++I) {
-                const int count = count_of(J, I), place = place_of(J, I);
-                const size_t at = first + (size_t)place;
-                const f32x4 p = load_as<std::conditional_t<MASTER, float, T>>(MASTER ? (const void*)d.master : d.param, at, count, whole);
                 float v[4];
                 T out[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] = fmaf(-rate, y[J][I][e], p[e] * keep);
+                    v[e] = fmaf(-rate, y[J][I][e], param[J][I][e] * keep);
                     asm("" : "+v"(v[e]));             // an fp32 number, of which the stored one is the rounding
                     if constexpr (MASTER || std::is_same<T, float>::value) out[e] = from_f32<T>(v[e]);
-                    else out[e] = round_at_random(T{}, v[e], mix(base + (uint32_t)(place + e)));
+                    else out[e] = round_at_random(T{}, v[e], mix(base + (uint32_t)run_of(J, I, e).at));
+                    y[J][I][e] = (float)out[e];
                 }
-                put4(static_cast<T*>(d.param) + at, out, count, whole);
-                if constexpr (MASTER) put4(d.master + at, v, count, whole);
-                if (d.transposed) {                   // uniform
-                    T* const t = static_cast<T*>(d.transposed) + to + (size_t)((16 * J + c0) * bs_r + 16 * I + i);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e < count) t[e * bs_r] = out[e];
-                }
+                store_run4<T, WHOLE>(static_cast<T*>(d.param), out, J, I, run_of);
+                if constexpr (MASTER) store_run4<float, WHOLE>(d.master, v, J, I, run_of);
             }
+        if (!d.transposed) return;                    // uniform
+        T* const t = static_cast<T*>(d.transposed);
+        if (through) {
+            wave_lds_fence();
+            put_y();
+#pragma unroll
+            for (int J = 0; J < CT; ++J)
+#pragma unroll
+                for (int I = 0; I < RT; ++I) {
+                    const f32x4 v = turned_y(I, J);
+                    const int c = 16 * J + i, at = 16 * I + c0, b = MODE == 1 ? at / bs_r : 0, a = at - b * bs_r;
+                    if (c < bs_c && a < bs_r && b < here)
+                        *reinterpret_cast<t4*>(t + (size_t)d.place[block0 + b] * (size_t)size + (size_t)(c * bs_r + a)) =
+                            t4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+                }
+        } else {
+#pragma unroll
+            for (int J = 0; J < CT; ++J)
+#pragma unroll
+                for (int I = 0; I < RT; ++I)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int all = 16 * J + c0 + e, b = MODE == 2 ? all / bs_c : mine, c = MODE == 2 ? all - b * bs_c : all;
+                        if (c < bs_c && row_of(I) < bs_r && b < here)
+                            t[(size_t)d.place[block0 + b] * (size_t)size + (size_t)(c * bs_r + row_of(I))] = (T)y[J][I][e];
+                    }
+        }
     };
-    auto update_type = [&](auto type) {
+    if (!kEarly) read_param();
+    auto update_type = [&](auto type) __attribute__((always_inline)) {
         if (d.master) update(type, std::true_type{});
         else update(type, std::false_type{});
     };
@@ -313,8 +500,14 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT)) void bsr_muon_blocks(const m
 }
 
 int tiles_of(int32_t side) { return (side + 15) / 16; }
-int kind_of(const bsr_muon_tensor& t) { return (tiles_of(t.bs_r) - 1) * 4 + tiles_of(t.bs_c) - 1; }
-int chunk_of(const bsr_muon_tensor& t) { return waves_of(tiles_of(t.bs_r), tiles_of(t.bs_c)); }   // blocks of a workgroup
+// Blocks that stand beside one another: along rows (1) or columns (2) of 8 at most, else none (0).
+int mode_of(const bsr_muon_tensor& t) { return t.bs_r <= t.bs_c ? (t.bs_r <= 8 ? 1 : 0) : t.bs_c <= 8 ? 2 : 0; }
+bool whole_of(const bsr_muon_tensor& t) { return mode_of(t) != 2 && t.bs_c % 4 == 0; }
+int kind_of(const bsr_muon_tensor& t) { return ((mode_of(t) * 4 + tiles_of(t.bs_r) - 1) * 4 + tiles_of(t.bs_c) - 1) * 2 + whole_of(t); }
+int chunk_of(const bsr_muon_tensor& t)                // blocks of a workgroup
+{
+    return waves_of(tiles_of(t.bs_r), tiles_of(t.bs_c)) * (mode_of(t) ? 16 / std::min(t.bs_r, t.bs_c) : 1);
+}
 int64_t chunks_of(const bsr_muon_tensor& t) { return (t.blocks + chunk_of(t) - 1) / chunk_of(t); }
 size_t elements_of(const bsr_muon_tensor& t) { return (size_t)t.blocks * (size_t)t.bs_r * (size_t)t.bs_c; }
 
@@ -435,19 +628,34 @@ bsr_status create_muon(bsr_muon** out, int64_t n, const bsr_muon_tensor* tensors
     return BSR_OK;
 }
 
-template <int RT, int CT> bsr_status launch_tiles(const bsr_muon* opt, const bsr_muon::launch_t& l, const muon_args& h, hipStream_t stream)
+template <int RT, int CT, int MODE> bsr_status launch_tiles(const bsr_muon* opt, const bsr_muon::launch_t& l, const muon_args& h, hipStream_t stream)
 {
-    hipLaunchKernelGGL((bsr_muon_blocks<RT, CT>), dim3((unsigned)l.count), dim3(64 * waves_of(RT, CT)), 0, stream, opt->descs, opt->chunks + l.first, h);
-    return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)l.count), dim3(64 * waves_of(RT, CT)), 0, stream, opt->descs, opt->chunks + l.first, h);
+        return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+    };
+    if constexpr (MODE != 2)
+        if (l.kind % 2) return go(bsr_muon_blocks<RT, CT, MODE, true>);
+    return go(bsr_muon_blocks<RT, CT, MODE, false>);
 }
 template <int RT> bsr_status launch_rows(const bsr_muon* opt, const bsr_muon::launch_t& l, const muon_args& h, hipStream_t stream)
 {
-    switch (l.kind % 4) {
-        case 0: return launch_tiles<RT, 1>(opt, l, h, stream);
-        case 1: return launch_tiles<RT, 2>(opt, l, h, stream);
-        case 2: return launch_tiles<RT, 3>(opt, l, h, stream);
+    switch (l.kind / 2 % 4) {
+        case 0: return launch_tiles<RT, 1, 0>(opt, l, h, stream);
+        case 1: return launch_tiles<RT, 2, 0>(opt, l, h, stream);
+        case 2: return launch_tiles<RT, 3, 0>(opt, l, h, stream);
     }
-    return launch_tiles<RT, 4>(opt, l, h, stream);
+    return launch_tiles<RT, 4, 0>(opt, l, h, stream);
+}
+bsr_status launch_kind(const bsr_muon* opt, const bsr_muon::launch_t& l, const muon_args& h, hipStream_t stream)
+{
+    const int mode = l.kind / 32, rt = l.kind / 8 % 4, ct = l.kind / 2 % 4;
+    if (mode == 1) return ct == 0 ? launch_tiles<1, 1, 1>(opt, l, h, stream) : ct == 1 ? launch_tiles<1, 2, 1>(opt, l, h, stream)
+                        : ct == 2 ? launch_tiles<1, 3, 1>(opt, l, h, stream) : launch_tiles<1, 4, 1>(opt, l, h, stream);
+    if (mode == 2) return rt == 0 ? launch_tiles<1, 1, 2>(opt, l, h, stream) : rt == 1 ? launch_tiles<2, 1, 2>(opt, l, h, stream)
+                        : rt == 2 ? launch_tiles<3, 1, 2>(opt, l, h, stream) : launch_tiles<4, 1, 2>(opt, l, h, stream);
+    return rt == 0 ? launch_rows<1>(opt, l, h, stream) : rt == 1 ? launch_rows<2>(opt, l, h, stream)
+         : rt == 2 ? launch_rows<3>(opt, l, h, stream) : launch_rows<4>(opt, l, h, stream);
 }
 
 }  // namespace
@@ -521,9 +729,7 @@ bsr_status bsr_muon_step(const bsr_muon* opt, const bsr_muon_hyper* hyper, void*
     h.step_dev = y.step_dev;
     h.grad_scale_dev = y.grad_scale_dev;
     for (const auto& l : opt->launches) {
-        const int rt = l.kind / 4;
-        const bsr_status st = rt == 0 ? launch_rows<1>(opt, l, h, stream) : rt == 1 ? launch_rows<2>(opt, l, h, stream)
-                            : rt == 2 ? launch_rows<3>(opt, l, h, stream) : launch_rows<4>(opt, l, h, stream);
+        const bsr_status st = launch_kind(opt, l, h, stream);
         if (st != BSR_OK) return st;
     }
     return BSR_OK;
