@@ -36,15 +36,18 @@ struct norm_args {
     float eps, alpha, beta, over_n;                   // over_n = 1 / n
 };
 
-// T lanes' sums of N values; `slots`: two areas of N floats a wavefront, used in turn by the calls of a workgroup.
+constexpr int kMostAtOnce = 4;                        // values a call adds: the areas' size
+// T lanes' sums of N values; `slots`: two areas of kMostAtOnce floats a wavefront, used in turn by the calls of a workgroup (of
+// one size whatever N is: a call that takes fewer must not reach into the area of the call before, which may still be read).
 template <int T, int N> struct row_sums {
     static constexpr int WAVES = T > 64 ? T / 64 : 1;
+    static_assert(N <= kMostAtOnce, "an area holds them");
     __device__ __forceinline__ static void add(float (&v)[N], float* slots, int& phase)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = lane_sum<(T > 64 ? 64 : T)>(v[i]);
         if constexpr (T > 64) {
-            float* const at = slots + phase * (WAVES * N);
+            float* const at = slots + phase * (WAVES * kMostAtOnce);
             phase ^= 1;
             if ((threadIdx.x & 63) == 0) {
 #pragma unroll
@@ -60,7 +63,6 @@ template <int T, int N> struct row_sums {
         }
     }
 };
-constexpr int kMostAtOnce = 4;                        // values a call adds: the areas' size
 
 __device__ __forceinline__ float inverse_root(float mean_square, float eps) { return __builtin_amdgcn_rsqf(mean_square + eps); }
 
