@@ -264,7 +264,7 @@ __device__ __forceinline__ void finish(const epilogue_args& ep, float (&v)[N], i
 }
 
 // Gated sums g, u of a piece of row i, whose columns in W's order begin at j and j + unit: Z stored if wanted, H into g.
-template <typename T, typename O, int N>
+template <typename T, typename O, bool NT = true, int N>
 __device__ __forceinline__ void finish_gate(const gated_args& ep, const bias_run<T, N>& bg, const bias_run<T, N>& bu, float (&g)[N], float (&u)[N], int i,
                                             int j, int unit, int n)
 {
@@ -275,8 +275,8 @@ __device__ __forceinline__ void finish_gate(const gated_args& ep, const bias_run
     }
     if (ep.z) {
         O* const z = static_cast<O*>(ep.z) + (size_t)i * (size_t)n + (size_t)j;
-        store_run<true>(z, g);
-        store_run<true>(z + unit, u);
+        store_run<NT>(z, g);
+        store_run<NT>(z + unit, u);
     }
     with_act_or_none(ep.act, [&](auto act) {
 #pragma unroll
