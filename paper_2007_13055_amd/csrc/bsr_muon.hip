@@ -13,8 +13,9 @@
 // symmetric, so that its tiles serve as either operand of G^2; P's tiles are W P's right operand.  Its left one is W^T's tiles,
 // which W passes through LDS for, written once a step by columns and read back 16 bytes a lane; the wavefront's own area, no barrier.
 //
-// What bounds it: up to 16x16 blocks memory (22 bytes an element for bf16 with a master copy and W^T), beyond that the matrix
-// cores' fp32 rate: 5 (4 L S^2 + 2 S^3) operations a block.
+// What bounds it (40 million elements, bf16 with a master copy, 805 MB; a large copy moves 5.2 bytes a ps): memory, and in the largest
+// blocks registers, which leave two wavefronts a SIMD to cover its latency.  With 0 and 5 steps, us: 16x16 146, 198; 32x32 158, 189;
+// 64x32 165, 176; 64x64 215, 285 (steps' products of three bf16 parts 64x64 422, of fp32 numbers 16x16 235).
 #include <algorithm>
 #include <cmath>
 #include <memory>
@@ -51,6 +52,7 @@ static_assert(sizeof(muon_desc) == 88, "uploaded as words");
 struct muon_args {
     float lr, mu, eps, a, b, c, grad_scale;
     int32_t ns_steps, nesterov;
+    int32_t small;                                    // the steps' numbers stay in fp16's range
     uint32_t key;                                     // of the seed and the step
     uint32_t seed;
     const float* lr_dev;
@@ -121,73 +123,106 @@ __device__ __forceinline__ double shared_sum(double v, int lane_xor)
     return v + __builtin_bit_cast(double, (unsigned long long)(unsigned)lo | ((unsigned long long)(unsigned)hi << 32));
 }
 
-// fp32 products on the bf16 matrix cores, which take a sixteenth of the time: x = hi + mid + lo, three bf16 numbers, exactly (8 of
-// its 24 bits each), and of the nine products of two such sums the six largest; the others are below 2^-26 of the whole, less
-// than fp32 products lose by rounding.  A lane's eight terms are those of two tiles, four each.
-struct parts { u32x4 hi, mid, lo; };
-__device__ __forceinline__ parts parts_of(const f32x4& a, const f32x4& b)
+// fp32 products on the 16-bit matrix cores, which take a sixteenth of the time.  A lane's eight terms are those of two tiles, four each.
+// F16: x = hi + lo, two fp16 numbers, to 2^-23 of x's power of two, and of the four products of two such sums the three largest (the
+// fourth is below 2^-22 of hi hi); for numbers that are known to stay in fp16's range.  Else: x = hi + mid + lo, three bf16 numbers,
+// exactly (8 of its 24 bits each), and of the nine products the six largest; the others are below 2^-26 of the whole.
+template <bool F16> struct parts { u32x4 p[F16 ? 2 : 3]; };                  // the largest first
+template <bool F16> __device__ __forceinline__ parts<F16> parts_of(const f32x4& a, const f32x4& b)
 {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    parts out;
+    parts<F16> out;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         f32x2 x = q < 2 ? f32x2{a[2 * q], a[2 * q + 1]} : f32x2{b[2 * q - 4], b[2 * q - 3]};
-        uint32_t w[3];
+        if constexpr (F16) {
+            const f16x2 hi = __builtin_convertvector(x, f16x2);
+            float minus = -1.f;                       // (unknown to the compiler, which then takes one instruction that reads fp16)
+            asm("" : "+s"(minus));
+            const f32x2 rest = {fmaf((float)hi.x, minus, x.x), fmaf((float)hi.y, minus, x.y)};
+            out.p[0][q] = __builtin_bit_cast(uint32_t, hi);
+            out.p[1][q] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, f16x2));
+        } else {
 #pragma unroll
-        for (int part = 0; part < 3; ++part) {
-            w[part] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
-            if (part < 2) {
-                x.x -= __builtin_bit_cast(float, w[part] << 16);
-                x.y -= __builtin_bit_cast(float, w[part] & 0xFFFF0000u);
+            for (int part = 0; part < 3; ++part) {
+                const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+                out.p[part][q] = w;
+                if (part < 2) {
+                    x.x -= __builtin_bit_cast(float, w << 16);
+                    x.y -= __builtin_bit_cast(float, w & 0xFFFF0000u);
+                }
             }
         }
-        out.hi[q] = w[0];
-        out.mid[q] = w[1];
-        out.lo[q] = w[2];
     }
     return out;
 }
-__device__ __forceinline__ void mfma_bf16(f32x4& acc, const u32x4& a, const u32x4& b)
-{
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
-}
 // acc[t] += left^T right[t], the small products first
-template <int S> __device__ __forceinline__ void add_row(f32x4 (&acc)[S], const parts& left, const parts (&right)[S])
+template <bool F16, int S> __device__ __forceinline__ void add_row(f32x4 (&acc)[S], const parts<F16>& left, const parts<F16> (&right)[S])
 {
+    auto add = [&](int u, int v) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.lo, right[t].hi);
-#pragma unroll
-    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.hi, right[t].lo);
-#pragma unroll
-    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.mid, right[t].mid);
-#pragma unroll
-    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.mid, right[t].hi);
-#pragma unroll
-    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.hi, right[t].mid);
-#pragma unroll
-    for (int t = 0; t < S; ++t) mfma_bf16(acc[t], left.hi, right[t].hi);
+        for (int t = 0; t < S; ++t) {
+            if constexpr (F16)
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, left.p[u]), __builtin_bit_cast(f16x8, right[t].p[v]), acc[t], 0, 0, 0);
+            else
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, left.p[u]), __builtin_bit_cast(bf16x8, right[t].p[v]), acc[t], 0, 0, 0);
+        }
+    };
+    if constexpr (!F16) {
+        add(2, 0);
+        add(0, 2);
+        add(1, 1);
+    }
+    add(1, 0);
+    add(0, 1);
+    add(0, 0);
 }
 // acc[s][t] += operand(s)^T operand(t)
-template <int R, int S, typename F> __device__ __forceinline__ void add_product(f32x4 (&acc)[R][S], F operand)
+template <bool F16, int R, int S, typename F> __device__ __forceinline__ void add_product(f32x4 (&acc)[R][S], F operand)
 {
-    parts x[S];
+    parts<F16> x[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) x[s] = operand(s);
 #pragma unroll
-    for (int s = 0; s < R; ++s) add_row<S>(acc[s], x[s], x);
+    for (int s = 0; s < R; ++s) add_row<F16, S>(acc[s], x[s], x);
+}
+
+// acc += left^T right for single tiles: as their fp16 parts fill half of the eight terms each, two instructions take all four products.
+struct stacked { u32x4 both, hi, lo; };               // {hi, lo}, {hi, hi}, {lo, lo}
+__device__ __forceinline__ stacked stacked_of(const f32x4& a)
+{
+    const parts<true> x = parts_of<true>(a, a);       // (the second half's arithmetic is the first's)
+    return {u32x4{x.p[0][0], x.p[0][1], x.p[1][0], x.p[1][1]}, u32x4{x.p[0][0], x.p[0][1], x.p[0][0], x.p[0][1]},
+            u32x4{x.p[1][0], x.p[1][1], x.p[1][0], x.p[1][1]}};
+}
+__device__ __forceinline__ void add_tile(f32x4& acc, const u32x4& left, const stacked& right)
+{
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, left), __builtin_bit_cast(f16x8, right.lo), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, left), __builtin_bit_cast(f16x8, right.hi), acc, 0, 0, 0);
+}
+// ... and in fp32.
+__device__ __forceinline__ void add_tile(f32x4& acc, const f32x4& left, const f32x4& right)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(left[e], right[e], acc, 0, 0, 0);
 }
 
 // RT, CT: 16x16 tiles of a block down and across.  MODE: 0 a block a wavefront; where the smaller side is 8 at most, as many as fit
 // 16 beside one another along it, 1 down (bs_r <= bs_c), 2 across: G then holds their products with one another, too, which are
-// dropped, and P keeps them apart.  WHOLE: a lane's runs are four neighbouring elements of a block's row, or none.
-template <int RT, int CT, int MODE, bool WHOLE>
+// dropped, and P keeps them apart.  WHOLE: a lane's runs are four neighbouring elements of a block's row, or none.  F16: the steps'
+// products are of fp16 parts, and W is held 64 times as large, G thus 4096 times, so that the small parts of theirs stay above fp16's
+// smallest numbers; |X| <= 3.9 keeps them below the largest (stays_small()).
+template <int RT, int CT, int MODE, bool WHOLE, bool F16>
 __global__ __launch_bounds__(64 * waves_of(RT, CT), 2) void bsr_muon_blocks(const muon_desc* __restrict__ tensors, const int2* __restrict__ chunks, muon_args h)
 {
     constexpr int WAVES = waves_of(RT, CT);
     constexpr bool TALL = RT > CT || MODE == 2;
     constexpr int L = TALL ? RT : CT, S = TALL ? CT : RT;
     static_assert(MODE == 0 || S == 1, "blocks beside one another fill one tile");
+    constexpr float kHeld = F16 ? 64.f : 1.f;         // W's scale
+    const float b = h.b / (kHeld * kHeld), c = h.c / (kHeld * kHeld * kHeld * kHeld);
     constexpr int PW = S * 16 + 4, PY = RT * 16 + 4;  // pitches in LDS of W [L * 16][], of the block's transpose [CT * 16][]
     constexpr int AREA = std::max(L * 16 * PW, CT * 16 * PY);
     __shared__ __attribute__((aligned(16))) float areas[WAVES][AREA];
@@ -269,7 +304,7 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT), 2) void bsr_muon_blocks(cons
     // |V|: squares and their sum in 64 bits, which hold those of any fp32 numbers
     {
         float over[4];                                // of the lane's four columns (MODE 2: they may be of four blocks)
-        auto inverse = [&](double sum) { return (float)(1.0 / (sqrt(sum) + (double)h.eps)); };
+        auto inverse = [&](double sum) { return (float)((double)kHeld / (sqrt(sum) + (double)h.eps)); };
         auto finite_sum = [&](double sum) { return sum - sum == 0.0; };
         if constexpr (MODE == 2) {
             double* const sums = reinterpret_cast<double*>(area);
@@ -364,35 +399,42 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT), 2) void bsr_muon_blocks(cons
 #pragma unroll
             for (int t = 0; t < S; ++t) g[s][t] = p[s][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         if constexpr (S == 1) {
+            auto square = [&](f32x4& to, const f32x4& x) __attribute__((always_inline)) {
+                if constexpr (F16) {
+                    const stacked v = stacked_of(x);
+                    add_tile(to, v.both, v);
+                } else {
+                    add_tile(to, x, x);
+                }
+            };
 #pragma unroll
-            for (int l = 0; l < L; ++l)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) g[0][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[l][0][e], w[l][0][e], g[0][0], 0, 0, 0);
+            for (int l = 0; l < L; ++l) square(g[0][0], w[l][0]);
             if constexpr (MODE != 0) {                // what is of two blocks is no part of either
 #pragma unroll
                 for (int e = 0; e < 4; ++e) g[0][0][e] = ((mask >> e) & 1) ? g[0][0][e] : 0.f;
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) p[0][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(g[0][0][e], g[0][0][e], p[0][0], 0, 0, 0);
+            square(p[0][0], g[0][0]);
         } else {
 #pragma unroll
-            for (int k = 0; k < L; k += 2) add_product<S, S>(g, [&](int s) __attribute__((always_inline)) { return parts_of(w[k][s], k + 1 < L ? w[k + 1][s] : f32x4{}); });
+            for (int k = 0; k < L; k += 2) add_product<F16, S, S>(g, [&](int s) __attribute__((always_inline)) { return parts_of<F16>(w[k][s], k + 1 < L ? w[k + 1][s] : f32x4{}); });
 #pragma unroll
-            for (int k = 0; k < S; k += 2) add_product<S, S>(p, [&](int s) __attribute__((always_inline)) { return parts_of(g[k][s], k + 1 < S ? g[k + 1][s] : f32x4{}); });
+            for (int k = 0; k < S; k += 2) add_product<F16, S, S>(p, [&](int s) __attribute__((always_inline)) { return parts_of<F16>(g[k][s], k + 1 < S ? g[k + 1][s] : f32x4{}); });
         }
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
             for (int t = 0; t < S; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[s][t][e] = fmaf(h.b, g[s][t][e], h.c * p[s][t][e]);
+                for (int e = 0; e < 4; ++e) p[s][t][e] = fmaf(b, g[s][t][e], c * p[s][t][e]);
         if constexpr (S == 1) {
+            stacked right{};
+            if constexpr (F16) right = stacked_of(p[0][0]);
 #pragma unroll
             for (int l = 0; l < L; ++l) {
                 const f32x4 wt = turned(0, l);
                 w[l][0] *= h.a;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[l][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(wt[e], p[0][0][e], w[l][0], 0, 0, 0);
+                if constexpr (F16) add_tile(w[l][0], stacked_of(wt).both, right);
+                else add_tile(w[l][0], wt, p[0][0]);
             }
         } else {
             // (a W from LDS: its registers were G^2's in the meantime)
@@ -404,13 +446,13 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT), 2) void bsr_muon_blocks(cons
                     for (int e = 0; e < 4; ++e) w[l][t][e] = h.a * area[(16 * l + c0 + e) * PW + 16 * t + i];
 #pragma unroll
             for (int k = 0; k < S; k += 2) {
-                parts right[S];
+                parts<F16> right[S];
 #pragma unroll
-                for (int t = 0; t < S; ++t) right[t] = parts_of(p[k][t], k + 1 < S ? p[k + 1][t] : f32x4{});
+                for (int t = 0; t < S; ++t) right[t] = parts_of<F16>(p[k][t], k + 1 < S ? p[k + 1][t] : f32x4{});
 #pragma unroll
                 for (int l = 0; l < L; ++l) {
-                    const parts left = parts_of(turned(k, l), k + 1 < S ? turned(k + 1, l) : f32x4{});
-                    add_row<S>(w[l], left, right);
+                    const parts<F16> left = parts_of<F16>(turned(k, l), k + 1 < S ? turned(k + 1, l) : f32x4{});
+                    add_row<F16, S>(w[l], left, right);
                 }
             }
         }
@@ -436,7 +478,7 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT), 2) void bsr_muon_blocks(cons
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y[J][I][e] = (spoilt >> e) & 1 ? __builtin_nanf("") : y[J][I][e];
 
-    const float keep = 1.f - lr * d.decay, rate = lr * d.scale;
+    const float keep = 1.f - lr * d.decay, rate = lr * d.scale / kHeld;
     const uint32_t base = mix(d.number + key);
     // the transposed copy: its rows by way of LDS, four neighbouring elements a lane, where they are whole runs of a block
     const bool through = MODE != 2 && (bs_r & 3) == 0;
@@ -497,6 +539,31 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT), 2) void bsr_muon_blocks(cons
     if (d.dtype == BSR_F32) update(0.f, std::false_type{});
     else if (d.dtype == BSR_F16) update_type(f16_t{});
     else update_type(bf16_t{});
+}
+
+// Whether X's singular values, 1 at most, stay below 3.9 through the steps, and P's below 2^15: the steps take a singular value s to
+// a s + b s^3 + c s^5, whose largest value over 0 .. s is at the end or where its slope a + 3 b s^2 + 5 c s^4 is 0.
+bool stays_small(const bsr_muon_hyper& y)
+{
+    const double a = y.a, b = y.b, c = y.c;
+    double most = 1.0 + 0x1p-10;                      // (roundings)
+    for (int step = 0; step < y.ns_steps; ++step) {
+        if (std::fabs(b) * most * most + std::fabs(c) * most * most * most * most > 0x1p15) return false;
+        double next = 0.0;
+        auto at = [&](double q) {                     // q: s^2
+            if (q >= 0.0 && q <= most * most) next = std::max(next, std::sqrt(q) * std::fabs(a + q * (b + q * c)));
+        };
+        at(most * most);
+        const double inside = 9.0 * b * b - 20.0 * a * c;
+        if (c != 0.0 && inside >= 0.0) {
+            at((-3.0 * b + std::sqrt(inside)) / (10.0 * c));
+            at((-3.0 * b - std::sqrt(inside)) / (10.0 * c));
+        }
+        if (b != 0.0) at(-a / (3.0 * b));             // c = 0, or so small that the roots above lose it
+        most = next * (1.0 + 0x1p-10);
+        if (!(most <= 3.9)) return false;
+    }
+    return true;
 }
 
 int tiles_of(int32_t side) { return (side + 15) / 16; }
@@ -634,9 +701,10 @@ template <int RT, int CT, int MODE> bsr_status launch_tiles(const bsr_muon* opt,
         hipLaunchKernelGGL(kernel, dim3((unsigned)l.count), dim3(64 * waves_of(RT, CT)), 0, stream, opt->descs, opt->chunks + l.first, h);
         return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
     };
+    const bool whole = l.kind % 2;
     if constexpr (MODE != 2)
-        if (l.kind % 2) return go(bsr_muon_blocks<RT, CT, MODE, true>);
-    return go(bsr_muon_blocks<RT, CT, MODE, false>);
+        if (whole) return h.small ? go(bsr_muon_blocks<RT, CT, MODE, true, true>) : go(bsr_muon_blocks<RT, CT, MODE, true, false>);
+    return h.small ? go(bsr_muon_blocks<RT, CT, MODE, false, true>) : go(bsr_muon_blocks<RT, CT, MODE, false, false>);
 }
 template <int RT> bsr_status launch_rows(const bsr_muon* opt, const bsr_muon::launch_t& l, const muon_args& h, hipStream_t stream)
 {
@@ -723,6 +791,7 @@ bsr_status bsr_muon_step(const bsr_muon* opt, const bsr_muon_hyper* hyper, void*
     h.grad_scale = y.grad_scale;
     h.ns_steps = y.ns_steps;
     h.nesterov = y.nesterov != 0;
+    h.small = stays_small(y);
     if (!y.step_dev) h.key = step_key(y.seed, (uint64_t)y.step);
     h.seed = y.seed;
     h.lr_dev = y.lr_dev;

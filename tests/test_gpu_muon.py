@@ -227,6 +227,26 @@ def test_other_settings(steps):
     _check_update(-_f64(p), _f64(grads[0]), steps, steps=steps, eps=1e-6, abc=abc)
 
 
+@pytest.mark.parametrize("shape", [(16, 16), (64, 64), (8, 8), (5, 7), (33, 64), (64, 16)])
+@pytest.mark.parametrize("abc,steps", [((1.9, 0.0, 0.0), 2), ((1.0, 2.8, 0.0), 1), ((0.9, 0.0, 2.9), 1), ((0.0, 0.0, 0.0), 2), ((-1.5, 0.5, 1e-30), 5),   # |X| below 3.9
+                                       ((6.0, -1.0, 0.0), 2), ((1.0, 0.0, 3.0), 2), ((2.0, 3.0, 0.0), 3), ((1.0, -4e4, 4e4), 1), ((1e9, 0.0, 0.0), 2)])
+def test_coefficients(shape, abc, steps):
+    """Steps that keep X small and steps that do not (whose products cannot be of fp16 parts); first singular values near 1."""
+    import torch
+    import paper_2007_13055_amd as lib
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    g = rand(9, *shape) * 0.05 + 2 * rand(9, shape[0], 1) * rand(9, 1, shape[1])
+    p = torch.zeros_like(g)
+    lib.bsr_muon_step(lib.bsr_muon_create([p], [g], scale=1.0), 1, lr=1.0, momentum=0.0, ns_steps=steps, coefficients=abc, eps=1e-6)
+    want = _orthogonal(_f64(g), np.float64, steps=steps, eps=1e-6, abc=abc)
+    size = max(1.0, float(np.abs(want).max()))                           # the floor's sizes are those of updates below 1.3
+    got, plain = -_f64(p), _orthogonal(_f64(g), np.float32, steps=steps, eps=1e-6, abc=abc)
+    err, ref = np.abs(got - want), np.abs(plain - want)
+    assert np.sqrt((err ** 2).mean()) <= 3 * np.sqrt((ref ** 2).mean()) + 2.0 ** -22 * size, (err.max(), ref.max())
+    assert err.max() <= 8 * ref.max() + 2.0 ** -22 * size, (err.max(), ref.max())
+
+
 def test_dropped_while_a_step_on_another_stream_is_still_to_run():
     """Its tables, momentum and master copies are no one else's before that step is done."""
     import torch
