@@ -15,7 +15,8 @@
 //
 // What bounds it (40 million elements, bf16 with a master copy, 805 MB; a large copy moves 5.2 bytes a ps): memory, and in the largest
 // blocks registers, which leave two wavefronts a SIMD to cover its latency.  With 0 and 5 steps, us: 16x16 146, 198; 32x32 158, 189;
-// 64x32 165, 176; 64x64 215, 285 (steps' products of three bf16 parts 64x64 422, of fp32 numbers 16x16 235).
+// 64x32 165, 176; 64x64 215, 285.  (16x16 with products of fp32 numbers 235; 64x64, fp32 gradients and W^T's copy with it, 318, and
+// 456 with products of three bf16 parts.)
 #include <algorithm>
 #include <cmath>
 #include <memory>
@@ -541,6 +542,212 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT), 2) void bsr_muon_blocks(cons
     else update_type(bf16_t{});
 }
 
+// The same for blocks of three and four tiles both ways, whose tiles are too many for a wavefront to hold with others beside it: a
+// block a workgroup, row l of W's tiles wavefront l's.  Each of W, G and P is split into its fp16 parts once, by the wavefronts that
+// have it, and read by all of them as operands from LDS, two regions in turn: between a region's reads and its next writes there
+// is a barrier, and three barriers make a step.  What bounds it where there are many blocks is LDS, which a wavefront a block reads
+// less of; where there are few it is the chain of a block.  fp32 64x64, us: 10 blocks 15.0, 1024 42, 2400 81 (a wavefront a block: 10
+// of f16 with W^T 37.8, 1030 50, 2400 84); 9828 blocks of bf16 with a master copy 326 and 285.
+template <int RT, int CT, bool WHOLE>
+__global__ __launch_bounds__(64 * std::max(RT, CT), 3) void bsr_muon_team(const muon_desc* __restrict__ tensors, const int2* __restrict__ chunks, muon_args h)
+{
+    constexpr bool TALL = RT > CT;
+    constexpr int L = TALL ? RT : CT, S = TALL ? CT : RT;
+    constexpr int PITCH = S * 16 + 4;
+    constexpr float kHeld = 64.f;                     // W's scale, as above
+    const float b = h.b / (kHeld * kHeld), c = h.c / (kHeld * kHeld * kHeld * kHeld);
+    __shared__ u32x4 operands[2][2][2][S][64];        // [region][hi, lo][two rows of tiles][column of tiles][lane]
+    __shared__ __attribute__((aligned(16))) float areas[L][16 * PITCH];
+    __shared__ double sums[L];
+    const int lane = threadIdx.x & 63, i = lane & 15, c0 = (lane >> 4) * 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int PER = waves_of(RT, CT);             // blocks of a chunk
+    const int2 where = chunks[blockIdx.x / PER];
+    const muon_desc& d = tensors[where.x];
+    const int bs_r = d.bs_r, bs_c = d.bs_c, size = bs_r * bs_c;
+    const int64_t block = (int64_t)where.y + (int64_t)(blockIdx.x % PER);
+    if (block >= d.blocks) return;                    // whole workgroup, as the returns below
+
+    float lr = h.lr, grad_scale = h.grad_scale;
+    uint32_t key = h.key;
+    if (h.grad_scale_dev) {
+        grad_scale = *h.grad_scale_dev;
+        if (grad_scale == 0.f) return;
+    }
+    if (h.lr_dev) lr = *h.lr_dev;
+    if (h.step_dev) {
+        const int64_t t = *h.step_dev;
+        if (t < 1) return;
+        key = step_key(h.seed, (uint64_t)t);
+    }
+
+    // tile s of this wavefront's row of W: the block's rows 16 row_tile(s) + i, columns 16 col_tile(s) + c0 .. + 3 in a lane
+    const size_t first = (size_t)block * (size_t)size;
+    auto row_of = [&](int s) __attribute__((always_inline)) { return 16 * (TALL ? wave : s) + i; };
+    auto col_of = [&](int s) __attribute__((always_inline)) { return 16 * (TALL ? s : wave) + c0; };
+    auto run_of = [&](int s, int, int e = 0) __attribute__((always_inline)) {
+        const int row = row_of(s), col = col_of(s) + e;
+        return run_at{first + (size_t)(row * bs_c + col), row < bs_r ? bs_c - col : 0};
+    };
+    auto read = [&](f32x4 (&v)[S][1], const void* p, int dtype) __attribute__((always_inline)) {
+        if (dtype == BSR_F32) load_runs<float, WHOLE>(v, p, first, run_of);
+        else if (dtype == BSR_F16) load_runs<f16_t, WHOLE>(v, p, first, run_of);
+        else load_runs<bf16_t, WHOLE>(v, p, first, run_of);
+    };
+    float* const area = areas[wave];
+    // each tile's transpose, by way of the wavefront's own area
+    auto turn = [&](f32x4 (&to)[S], const f32x4 (&v)[S]) __attribute__((always_inline)) {
+        wave_lds_fence();
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) area[(c0 + e) * PITCH + 16 * s + i] = v[s][e];
+        wave_lds_fence();
+#pragma unroll
+        for (int s = 0; s < S; ++s) to[s] = *reinterpret_cast<const f32x4*>(&area[i * PITCH + 16 * s + c0]);
+    };
+    auto barrier = []() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };   // (of LDS alone)
+
+    f32x4 w[S], param[S][1];
+    {
+        f32x4 m[S][1], g[S][1];
+        read(m, d.momentum, BSR_F32);
+        if (d.master) read(param, d.master, BSR_F32);
+        else read(param, d.param, d.dtype);
+        read(g, d.grad, d.grad_dtype);
+        double sum = 0.0;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            float mv[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = g[s][0][e] * grad_scale;
+                mv[e] = fmaf(h.mu, m[s][0][e], x);
+                w[s][e] = h.nesterov ? fmaf(h.mu, mv[e], x) : mv[e];
+                sum += (double)w[s][e] * (double)w[s][e];
+            }
+            store_run4<float, WHOLE>(d.momentum, mv, s, 0, run_of);
+        }
+        for (int x = 1; x < 64; x *= 2) sum = shared_sum(sum, x);
+        if (lane == 0) sums[wave] = sum;
+        barrier();
+        sum = 0.0;
+#pragma unroll
+        for (int l = 0; l < L; ++l) sum += sums[l];
+        const float over = (float)((double)kHeld / (sqrt(sum) + (double)h.eps));
+#pragma unroll
+        for (int s = 0; s < S; ++s) w[s] *= over;
+    }
+    if constexpr (TALL) turn(w, w);
+
+    int region = 0;
+    // This wavefront's row of tiles into the region that is next, of a matrix of `rows` rows of tiles (an odd last one with zeros).
+    auto put = [&](const f32x4 (&v)[S], auto rows) __attribute__((always_inline)) {
+        constexpr int R = decltype(rows)::value;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const parts<true> x = parts_of<true>(v[s], f32x4{});
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                u32x4* const at = &operands[region][part][wave >> 1][s][lane];
+                if (R % 2 == 1 && wave == R - 1) *at = x.p[part];
+                else reinterpret_cast<u32x2*>(at)[wave & 1] = u32x2{x.p[part][0], x.p[part][1]};
+            }
+        }
+    };
+    auto operand = [&](int k, int s) __attribute__((always_inline)) { return parts<true>{{operands[region][0][k][s][lane], operands[region][1][k][s][lane]}}; };
+    // acc[t] += sum over the region's matrix's rows k of left(k)^T (its tile (k, t))
+    auto add = [&](f32x4 (&acc)[S], auto rows, auto left) __attribute__((always_inline)) {
+        constexpr int R = decltype(rows)::value;
+#pragma unroll
+        for (int k = 0; k < (R + 1) / 2; ++k) {
+            parts<true> right[S];
+#pragma unroll
+            for (int t = 0; t < S; ++t) right[t] = operand(k, t);
+            add_row<true, S>(acc, left(k), right);
+        }
+    };
+    const std::integral_constant<int, L> l_rows{};
+    const std::integral_constant<int, S> s_rows{};
+    for (int step = 0; step < h.ns_steps; ++step) {
+        put(w, l_rows);
+        barrier();
+        f32x4 wt[S], g[S], p[S];
+        turn(wt, w);
+        if (wave < S) {                               // row `wave` of G
+#pragma unroll
+            for (int t = 0; t < S; ++t) g[t] = p[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            add(g, l_rows, [&](int k) __attribute__((always_inline)) { return operand(k, wave); });
+        }
+        region ^= 1;
+        if (wave < S) put(g, s_rows);
+        barrier();
+        if (wave < S) {
+            add(p, s_rows, [&](int k) __attribute__((always_inline)) { return operand(k, wave); });
+#pragma unroll
+            for (int t = 0; t < S; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[t][e] = fmaf(b, g[t][e], c * p[t][e]);
+        }
+        region ^= 1;
+        if (wave < S) put(p, s_rows);
+        barrier();
+#pragma unroll
+        for (int t = 0; t < S; ++t) w[t] *= h.a;
+        add(w, s_rows, [&](int k) __attribute__((always_inline)) { return parts_of<true>(wt[2 * k], 2 * k + 1 < S ? wt[2 * k + 1] : f32x4{}); });
+        region ^= 1;
+    }
+    if constexpr (TALL) turn(w, w);
+
+    const float keep = 1.f - lr * d.decay, rate = lr * d.scale / kHeld;
+    const uint32_t base = mix(d.number + key);
+    auto update = [&](auto type, auto has_master) __attribute__((always_inline)) {
+        typedef decltype(type) T;
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        constexpr bool MASTER = decltype(has_master)::value;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            float v[4];
+            T out[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = fmaf(-rate, w[s][e], param[s][0][e] * keep);
+                asm("" : "+v"(v[e]));                 // an fp32 number, of which the stored one is the rounding
+                if constexpr (MASTER || std::is_same<T, float>::value) out[e] = from_f32<T>(v[e]);
+                else out[e] = round_at_random(T{}, v[e], mix(base + (uint32_t)run_of(s, 0, e).at));
+                w[s][e] = (float)out[e];
+            }
+            store_run4<T, WHOLE>(static_cast<T*>(d.param), out, s, 0, run_of);
+            if constexpr (MASTER) store_run4<float, WHOLE>(d.master, v, s, 0, run_of);
+        }
+        if (!d.transposed) return;                    // uniform
+        T* const t = static_cast<T*>(d.transposed) + (size_t)d.place[block] * (size_t)size;
+        if ((bs_r & 3) == 0) {                        // four neighbouring elements of a row of the transpose a lane
+            f32x4 turned[S];
+            turn(turned, w);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const int col = 16 * (TALL ? s : wave) + i, row = 16 * (TALL ? wave : s) + c0;
+                if (col < bs_c && row < bs_r)
+                    *reinterpret_cast<t4*>(t + (size_t)(col * bs_r + row)) = t4{(T)turned[s][0], (T)turned[s][1], (T)turned[s][2], (T)turned[s][3]};
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col_of(s) + e < bs_c && row_of(s) < bs_r) t[(size_t)((col_of(s) + e) * bs_r + row_of(s))] = (T)w[s][e];
+        }
+    };
+    auto update_type = [&](auto type) __attribute__((always_inline)) {
+        if (d.master) update(type, std::true_type{});
+        else update(type, std::false_type{});
+    };
+    if (d.dtype == BSR_F32) update(0.f, std::false_type{});
+    else if (d.dtype == BSR_F16) update_type(f16_t{});
+    else update_type(bf16_t{});
+}
+
 // Whether X's singular values, 1 at most, stay below 3.9 through the steps, and P's below 2^15: the steps take a singular value s to
 // a s + b s^3 + c s^5, whose largest value over 0 .. s is at the end or where its slope a + 3 b s^2 + 5 c s^4 is 0.
 bool stays_small(const bsr_muon_hyper& y)
@@ -695,6 +902,9 @@ bsr_status create_muon(bsr_muon** out, int64_t n, const bsr_muon_tensor* tensors
     return BSR_OK;
 }
 
+// Up to so many chunks of two large blocks, which do not fill the CUs with a wavefront each, a block has a workgroup (both sides: at
+// bsr_muon_team).  The two add a product's terms in another order: which one a tensor gets depends on the list's blocks of its tiles.
+constexpr int kFewChunks = 512;
 template <int RT, int CT, int MODE> bsr_status launch_tiles(const bsr_muon* opt, const bsr_muon::launch_t& l, const muon_args& h, hipStream_t stream)
 {
     auto go = [&](auto kernel) {
@@ -702,6 +912,14 @@ template <int RT, int CT, int MODE> bsr_status launch_tiles(const bsr_muon* opt,
         return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
     };
     const bool whole = l.kind % 2;
+    if constexpr (RT > 2 && CT > 2)
+        if (h.small && l.count <= kFewChunks) {
+            auto team = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)l.count * waves_of(RT, CT)), dim3(64 * std::max(RT, CT)), 0, stream, opt->descs, opt->chunks + l.first, h);
+                return hipGetLastError() == hipSuccess ? BSR_OK : BSR_ERR_HIP;
+            };
+            return whole ? team(bsr_muon_team<RT, CT, true>) : team(bsr_muon_team<RT, CT, false>);
+        }
     if constexpr (MODE != 2)
         if (whole) return h.small ? go(bsr_muon_blocks<RT, CT, MODE, true, true>) : go(bsr_muon_blocks<RT, CT, MODE, true, false>);
     return h.small ? go(bsr_muon_blocks<RT, CT, MODE, false, true>) : go(bsr_muon_blocks<RT, CT, MODE, false, false>);

@@ -247,6 +247,27 @@ def test_coefficients(shape, abc, steps):
     assert err.max() <= 8 * ref.max() + 2.0 ** -22 * size, (err.max(), ref.max())
 
 
+@pytest.mark.parametrize("count", [1, 5, 1100])
+@pytest.mark.parametrize("shape", [(48, 48), (64, 64), (41, 50), (64, 48), (48, 61)])
+def test_large_blocks_few_and_many(shape, count):
+    """A workgroup a block up to 1024 of them, a wavefront a block beyond."""
+    import torch
+    import paper_2007_13055_amd as lib
+    params, grads, momentum = _make([count], shape, "f32", "f32", 10)
+    params[0].zero_()
+    held = _f64(momentum[0])
+    perm = np.random.default_rng(2).permutation(count)
+    turned = torch.full((count, shape[1], shape[0]), 7.0, device="cuda")
+    opt = lib.bsr_muon_create(params, grads, momentum=momentum, scale=1.0, transposed=[(turned, perm)])
+    lib.bsr_muon_step(opt, 1, lr=1.0, momentum=0.9)
+    now = _f64(opt.momentum[0]).reshape(held.shape)
+    g = _f64(grads[0])
+    want = g + 0.9 * held
+    assert np.all(np.abs(now - want) <= 2.0 ** -24 * (3 * np.abs(want) + 2 * np.abs(held) + 2 * np.abs(g)))
+    _check_update(-_f64(params[0]), g + 0.9 * now, shape)
+    assert torch.equal(turned, params[0][torch.from_numpy(perm).cuda()].transpose(1, 2))
+
+
 def test_dropped_while_a_step_on_another_stream_is_still_to_run():
     """Its tables, momentum and master copies are no one else's before that step is done."""
     import torch
