@@ -263,8 +263,10 @@ __device__ __forceinline__ void finish(const epilogue_args& ep, float (&v)[N], i
     finish<T, O>(ep, bias, reads, v, i, j, n);
 }
 
-// Gated sums g, u of a piece of row i, whose columns in W's order begin at j and j + unit: Z stored if wanted, H into g.
-template <typename T, typename O, bool NT = true, int N>
+// Gated sums g, u of a piece of row i, whose columns in W's order begin at j and j + unit: Z stored if wanted, H into g.  NT: past
+// the caches, for kernels whose pieces of a half are 64 bytes or more beside one another; shorter ones become lines in L2 (bf16
+// 16x16, 4096 x (1024, 2 x 4096): 51.6 us, past it 55.9).
+template <typename T, typename O, bool NT = false, int N>
 __device__ __forceinline__ void finish_gate(const gated_args& ep, const bias_run<T, N>& bg, const bias_run<T, N>& bu, float (&g)[N], float (&u)[N], int i,
                                             int j, int unit, int n)
 {

@@ -265,7 +265,7 @@ __global__ __launch_bounds__(64 * (kWaves + kLoaders), 3) void bsr_mfma_sweep(
                         u[e] += b[e];
                     }
                 }
-                finish_gate<T, O, false>(ep, bg, bu, g, u, i, col, bs_r, n);
+                finish_gate<T, O>(ep, bg, bu, g, u, i, col, bs_r, n);
                 store_run(Y + (size_t)i * (size_t)(n / 2) + (size_t)(column[q0] / 2 + c0), g);
             }
         }

@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256, E::gated ? gated_waves<T>(BS_R, BS_C) : 1) voi
                 load_run<float>(g, reinterpret_cast<const float*>(fl + (size_t)row * FS) + at);
                 load_run<float>(u, reinterpret_cast<const float*>(fl + (size_t)row * FS) + BS_R + at);
                 if (i >= m) continue;
-                finish_gate<T, O>(ep, bg, bu, g, u, i, j, BS_R, n);
+                finish_gate<T, O, true>(ep, bg, bu, g, u, i, j, BS_R, n);
                 store_run<true>(Y + (size_t)i * (size_t)(n / 2) + (r * BS_R + at), g);
             }
         }
