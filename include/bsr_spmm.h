@@ -550,7 +550,7 @@ bsr_status bsr_residual_norm_backward(int64_t m, int64_t n, bsr_dtype s_dtype, c
 /*
  * One step over the stored blocks of many matrices whose update is orthogonalised block by block: every singular value of a
  * block's update is brought near 1 by Newton-Schulz steps, products alone, whose errors are those of fp32 arithmetic (on the matrix
- * cores, of numbers in two fp16 parts where a, b and c keep X's singular values below 3.9, in three bf16 parts or fp32 elsewhere).
+ * cores, of numbers in two fp16 parts where |a| >= 1 and a, b, c keep X's singular values below 3.9, in three bf16 parts or fp32 elsewhere).
  * With g the gradient times grad_scale,
  *     M = momentum M + g                 V = g + momentum M (nesterov) or M
  *     X = V / (|V| + eps), |V| the block's Frobenius norm;  ns_steps times  X = a X + b (X X^T) X + c (X X^T)^2 X

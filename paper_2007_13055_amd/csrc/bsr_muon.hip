@@ -749,10 +749,12 @@ __global__ __launch_bounds__(64 * std::max(RT, CT), 3) void bsr_muon_team(const 
 }
 
 // Whether X's singular values, 1 at most, stay below 3.9 through the steps, and P's below 2^15: the steps take a singular value s to
-// a s + b s^3 + c s^5, whose largest value over 0 .. s is at the end or where its slope a + 3 b s^2 + 5 c s^4 is 0.
+// a s + b s^3 + c s^5, whose largest value over 0 .. s is at the end or where its slope a + 3 b s^2 + 5 c s^4 is 0.  And a is 1 at
+// least, so that small ones do not shrink from step to step below what fp16 parts tell apart (near 0 they become a s).
 bool stays_small(const bsr_muon_hyper& y)
 {
     const double a = y.a, b = y.b, c = y.c;
+    if (std::fabs(a) < 1.0) return false;
     double most = 1.0 + 0x1p-10;                      // (roundings)
     for (int step = 0; step < y.ns_steps; ++step) {
         if (std::fabs(b) * most * most + std::fabs(c) * most * most * most * most > 0x1p15) return false;

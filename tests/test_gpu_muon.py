@@ -247,6 +247,21 @@ def test_coefficients(shape, abc, steps):
     assert err.max() <= 8 * ref.max() + 2.0 ** -22 * size, (err.max(), ref.max())
 
 
+@pytest.mark.parametrize("shape", [(16, 16), (64, 64), (32, 48)])
+def test_steps_that_shrink(shape):
+    """X = X X^T X twice: numbers far below 1 keep their relative accuracy (27 roundings' worth and as many of the sums')."""
+    import torch
+    import paper_2007_13055_amd as lib
+    g = torch.randn((5, *shape), generator=torch.Generator(device="cuda").manual_seed(11), device="cuda")
+    p = torch.zeros_like(g)
+    abc = (0.0, 1.0, 0.0)
+    lib.bsr_muon_step(lib.bsr_muon_create([p], [g], scale=1.0), 1, lr=1.0, momentum=0.0, ns_steps=2, coefficients=abc, eps=1e-6)
+    want, plain = (_orthogonal(_f64(g), T, steps=2, eps=1e-6, abc=abc) for T in (np.float64, np.float32))
+    err, ref = np.abs(-_f64(p) - want), np.abs(plain - want)
+    assert np.abs(want).max() < 2.0 ** -8
+    assert err.max() <= 8 * ref.max() + 2.0 ** -19 * np.abs(want).max(), (err.max(), ref.max())
+
+
 @pytest.mark.parametrize("count", [1, 5, 1100])
 @pytest.mark.parametrize("shape", [(48, 48), (64, 64), (41, 50), (64, 48), (48, 61)])
 def test_large_blocks_few_and_many(shape, count):
