@@ -6,8 +6,8 @@
 // S' before its rounding.  And the gradient: with g = GS + pre'(GU) the gradient of S',
 //
 //     dS = beta g      t = alpha gate g      dB = post'(t)
-//     norm'(G) = r (Gw - mean(Gw) - x c),  x the (centred) input, r = 1 / sqrt(mean(x^2) + eps), Gw = G weight,
-//                c = r^2 mean(Gw x); without the mean of Gw for the root mean square
+//     norm'(G) = r (Gw - mean(Gw) - x r c),  x the (centred) input, r = 1 / sqrt(mean(x^2) + eps), Gw = G weight,
+//                c = r mean(Gw x); without the mean of Gw for the root mean square
 //     sums over the rows: of GU x r and GU (pre's weight and bias), alpha g post(B) (gate), t x r and t (post's)
 //
 // Work split: T lanes share a row, eight neighbouring columns a lane (T = 8 to 64: several rows a wavefront; 128 to 1024: a
@@ -64,7 +64,13 @@ template <int T, int N> struct row_sums {
     }
 };
 
-__device__ __forceinline__ float inverse_root(float mean_square, float eps) { return __builtin_amdgcn_rsqf(mean_square + eps); }
+// 1 / sqrt(mean_square + eps): the instruction's, which is up to 2^-22 off, and a Newton step (gradients of rows of a few columns
+// cancel to a small part of their terms).  A sum of 0 or infinity keeps the instruction's.
+__device__ __forceinline__ float inverse_root(float mean_square, float eps)
+{
+    const float v = mean_square + eps, r = __builtin_amdgcn_rsqf(v), off = fmaf(-(v * r), r, 1.f);
+    return fabsf(off) < 1.f ? fmaf(0.5f * r, off, r) : r;
+}
 
 template <typename WT> __device__ __forceinline__ void load_vec(any_run<WT, V>& r, const void* p, int col, int count, float absent)
 {
@@ -193,6 +199,20 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void bsr_norm_rows(const ST* S, 
 // What the gradients of a row's columns are made of.
 struct row_stats { float mean, r, c, shift; };        // of the input; r and c as above; shift: mean of Gw (layer norm)
 
+// A product that is rounded wherever it is taken, so that what a mean subtracts is what the mean was made of: a row of one column
+// has a layer norm's gradient of exactly 0, rows of a few lose no more than the formulas do.
+__device__ __forceinline__ float rounded_product(float a, float b)
+{
+    float p = a * b;
+    asm("" : "+v"(p));
+    return p;
+}
+// The gradient of S' in one column, from gw = GU weight.
+__device__ __forceinline__ float sum_gradient(const norm_args& a, const row_stats& pre, float x, float gw, float gs)
+{
+    return a.pre == BSR_NORM_NONE ? gs : fmaf(pre.r, fmaf(-rounded_product(x - pre.mean, pre.r), pre.c, gw - pre.shift), gs);
+}
+
 // One column's part: from x, GU, GS, b to g, dS, dB and what the five sums get.
 struct column_parts { float ds, db, sum[kSums]; };
 __device__ __forceinline__ column_parts column_gradient(const norm_args& a, const row_stats& pre, const row_stats& post, float x, float gu, float gs,
@@ -200,17 +220,16 @@ __device__ __forceinline__ column_parts column_gradient(const norm_args& a, cons
 {
     column_parts out;
     const float xm = x - pre.mean;
-    float g = gs;
-    if (a.pre != BSR_NORM_NONE) g += pre.r * (fmaf(gu, wq, -pre.shift) - xm * pre.c);
+    const float g = sum_gradient(a, pre, x, rounded_product(gu, wq), gs);
     out.sum[3] = gu * (xm * pre.r);
     out.sum[4] = gu;
     out.ds = a.beta * g;
-    const float bh = (b - post.mean) * post.r, ag = a.alpha * g;
+    const float bh = rounded_product(b - post.mean, post.r), ag = rounded_product(a.alpha, g);
     out.sum[2] = ag * fmaf(bh, wp, bp);
-    const float t = ag * gate;
+    const float t = rounded_product(ag, gate);
     out.sum[0] = t * bh;
     out.sum[1] = t;
-    out.db = a.post == BSR_NORM_NONE ? t : post.r * (fmaf(t, wp, -post.shift) - (b - post.mean) * post.c);
+    out.db = a.post == BSR_NORM_NONE ? t : post.r * fmaf(-bh, post.c, rounded_product(t, wp) - post.shift);
     return out;
 }
 
@@ -294,7 +313,7 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void bsr_norm_grad_rows(const ST
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             each([&](int j, int e) {
                 const bool there = e < count[j];
-                const float xm = there ? x[j][e] - pre.mean : 0.f, bm = there ? b[j][e] - post.mean : 0.f, gw = gu[j][e] * wq[j][e];
+                const float xm = there ? x[j][e] - pre.mean : 0.f, bm = there ? b[j][e] - post.mean : 0.f, gw = rounded_product(gu[j][e], wq[j][e]);
                 v[0] = fmaf(xm, xm, v[0]);
                 v[1] = fmaf(gw, xm, v[1]);
                 v[2] += gw;
@@ -303,7 +322,7 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void bsr_norm_grad_rows(const ST
             row_sums<T, 4>::add(v, slots, phase);
             if (a.pre != BSR_NORM_NONE) {
                 pre.r = inverse_root(v[0] * a.over_n, a.eps);
-                pre.c = pre.r * pre.r * (v[1] * a.over_n);
+                pre.c = pre.r * (v[1] * a.over_n);
                 if (a.pre == BSR_NORM_LAYER) pre.shift = v[2] * a.over_n;
             }
             if (a.post != BSR_NORM_NONE) post.r = inverse_root(v[3] * a.over_n, a.eps);
@@ -313,14 +332,13 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void bsr_norm_grad_rows(const ST
             each([&](int j, int e) {
                 const bool there = e < count[j];
                 const float bm = there ? b[j][e] - post.mean : 0.f;
-                float g = gs[j][e];
-                if (a.pre != BSR_NORM_NONE) g += pre.r * (fmaf(gu[j][e], wq[j][e], -pre.shift) - (x[j][e] - pre.mean) * pre.c);
-                const float gw = there ? a.alpha * g * gate[j][e] * wp[j][e] : 0.f;
+                const float g = sum_gradient(a, pre, x[j][e], rounded_product(gu[j][e], wq[j][e]), gs[j][e]);
+                const float gw = there ? rounded_product(rounded_product(rounded_product(a.alpha, g), gate[j][e]), wp[j][e]) : 0.f;
                 v[0] = fmaf(gw, bm, v[0]);
                 v[1] += gw;
             });
             row_sums<T, 2>::add(v, slots, phase);
-            post.c = post.r * post.r * (v[0] * a.over_n);
+            post.c = post.r * (v[0] * a.over_n);
             if (a.post == BSR_NORM_LAYER) post.shift = v[1] * a.over_n;
         }
         if constexpr (!kAll) {

@@ -286,3 +286,16 @@ def test_refusals():
                  lambda: lib.bsr_residual_norm_backward(S, b, S.clone(), b.clone(), gate=w, grads={"gate": w})):
         with pytest.raises(lib.BsrError):
             call()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layer_norm_of_one_column_has_no_gradient(dtype):
+    """x - mean(x) is 0 whatever x is: nothing passes, not even a rounding (times 1 / sqrt(eps))."""
+    import torch
+    import paper_2007_13055_amd as lib
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    S, B, GS, GU = (torch.randn((51, 1), generator=gen, device="cuda").to(torch_dtype(dtype)) for _ in range(4))
+    v = {k: torch.randn(1, generator=gen, device="cuda") for k in ("post_weight", "gate", "pre_weight")}
+    ds, db, sums = lib.bsr_residual_norm_backward(S, B, GS, GU, post="layer", pre="layer", **v)
+    assert torch.equal(ds, GS) and bool((db == 0).all())
+    assert float(sums["pre_weight"].abs().max()) == 0 and float(sums["post_weight"].abs().max()) == 0
