@@ -13,9 +13,9 @@
 // symmetric, so that its tiles serve as either operand of G^2; P's tiles are W P's right operand.  Its left one is W^T's tiles,
 // which W passes through LDS for, written once a step by columns and read back 16 bytes a lane; the wavefront's own area, no barrier.
 //
-// What bounds it (40 million elements, bf16 with a master copy, 805 MB; a large copy moves 5.2 bytes a ps): memory, and in the largest
-// blocks registers, which leave two wavefronts a SIMD to cover its latency.  With 0 and 5 steps, us: 16x16 146, 198; 32x32 158, 189;
-// 64x32 165, 176; 64x64 215, 285.  (16x16 with products of fp32 numbers 235; 64x64, fp32 gradients and W^T's copy with it, 318, and
+// What bounds it (40 million elements, bf16 with a master copy, 805 MB; a large copy moves 5.2 bytes a ps): memory, beside it in
+// 16x16 blocks the vector units (splitting into parts), in the largest blocks registers, which leave two wavefronts a SIMD to cover its
+// latency.  With 0 and 5 steps, us: 16x16 147, 198; 32x32 158, 191; 64x32 165, 176 to 192; 64x64 215, 285.  (16x16 with products of fp32 numbers 235; 64x64, fp32 gradients and W^T's copy with it, 318, and
 // 456 with products of three bf16 parts.)
 #include <algorithm>
 #include <cmath>
