@@ -9,6 +9,8 @@ import sys
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
+from . import check_waits
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
@@ -27,9 +29,13 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-
 
 
 # Kernels in these files issue loads from inline assembly and place the waits themselves; the compiler
-# does not know such a register is still being filled, so a spill of one would store garbage.  The
-# build therefore fails if any kernel of these files spills a vector register.
+# does not know such a register is still being filled, so a spill of one would store garbage, and so
+# would a copy.  The build therefore fails if any kernel of these files spills a vector register, or
+# if its code names one between the load into it and the wait.
 NO_SPILL = ("bsr_mfma_ksplit.hip", "bsr_mfma_tile.hip", "bsr_mfma_small.hip", "bsr_mfma_group.hip", "bsr_mfma_sweep.hip")
+# Those whose loads and waits are the same on every path through a kernel; elsewhere both hang on the same conditions, and only
+# what happens on all paths can be told from the code.
+SAME_ON_EVERY_PATH = ("bsr_mfma_tile.hip",)
 
 
 def _spilling_kernels(remarks: str):
@@ -45,6 +51,11 @@ def _spilling_kernels(remarks: str):
             if int(text.split(":", 1)[1].split("[")[0].strip()) != 0 and name not in bad:
                 bad.append(name)
     return bad
+
+
+def _touching_early(src, obj):
+    """{kernel: addresses} where src's object touches a register in flight."""
+    return check_waits.check(obj, every_path=os.path.basename(src) not in SAME_ON_EVERY_PATH)
 
 
 def sources():
@@ -66,6 +77,10 @@ def _compile(src, force, plain=False):
         if bad:
             os.remove(obj)
             raise RuntimeError(f"{src}: kernels with hand-placed loads spill registers: {bad}")
+        early = _touching_early(src, obj) if r.returncode == 0 else {}
+        if early:
+            os.remove(obj)
+            raise RuntimeError(f"{src}: kernels touch registers that a load is still to fill: {sorted(early)}")
         keep, skip = [], 0
         for l in r.stderr.splitlines():          # drop the remarks and the source excerpts printed under them
             if "kernel-resource-usage" in l:

@@ -882,7 +882,7 @@ static std::vector<tuned_choice> tune_candidates(const bsr_matrix* W, int64_t m,
         }
         if (mfma_group_supports(W) && m >= 64) add(BSR_PATH_MFMA, 5, 0, 0, 0, 0);   // long rows in row groups + tile kernel
         if (W->bs_r >= 32 && m >= 128) {
-            for (int depth : {2, 3, 4}) add(BSR_PATH_MFMA, 3, 0, 1, depth, 0);
+            for (int depth = 2; depth <= mfma_tile_most_depth(W); ++depth) add(BSR_PATH_MFMA, 3, 0, 1, depth, 0);
             for (int depth : {1, 2}) add(BSR_PATH_MFMA, 3, 0, 2, depth, 0);
         }
         for (int tm : {1, 2, 4})

@@ -259,6 +259,8 @@ bool upload_landed(hipEvent_t ev, std::atomic<bool>& landed);
 bool upload_words(int32_t* dev, const std::vector<int32_t>& host, hipStream_t stream, hipEvent_t& ev, std::atomic<bool>& landed);
 bool is_capturing(hipStream_t stream);
 bsr_status launch_mfma_tile(const spmm_args& a, const tune_opts& t);
+// Most blocks that it keeps in flight (with one tile along m): spmm settings beyond that are taken as that many.
+int mfma_tile_most_depth(const bsr_matrix* W);
 // Row-group kernel: the grouped (longest) block-rows of a W with 64x64 blocks of a 16-bit type; the caller
 // launches the tile kernel with first_slot = W->grp_slots for the rest
 bsr_status launch_mfma_group(const spmm_args& a, const tune_opts& t);

@@ -352,6 +352,15 @@ __global__ __launch_bounds__(256, E::gated ? gated_waves<T>(BS_R, BS_C) : 1) voi
     }
 }
 
+// Most blocks in flight, with one tile along m: their 16-byte pieces take 160 registers of a thread at most.  Four fp32 64x64
+// blocks would take 192; the compiler then moves pieces to accumulation registers right behind their loads, which it takes for
+// done, and addresses of later loads into registers that the earlier ones are still to fill.
+template <typename T> constexpr int most_depth(int bs_r, int bs_c)
+{
+    const int row = bs_c * (int)sizeof(T) / 16, pieces = 128 * row / 256 + (bs_r * row + 255) / 256;
+    return std::min(4, 160 / (4 * pieces));
+}
+
 template <typename T, typename O, int BS_R, int BS_C>
 bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
 {
@@ -416,12 +425,14 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
         // the same sums -- each further one is 18 more kernels of this file, which takes longest to compile)
         // Gated: one, which leaves room for more wavefronts beside two halves' sums (two, us, and one: 4096 x (1024, 2 x 4096) bf16
         // 32x32 5 % 24.4, 22.0; fp32 64x64 10 % 88, 84; 2048 x (4096, 2 x 4096) fp32 32x32 10 % 152, 141; f16 64x64 within 3 %).
-        const int depth = std::min(tune.a > 0 ? tune.a : a.gated ? 1 : 2, a.epilogue || a.gated ? 2 : 4);
+        constexpr int kMostDepth = most_depth<T>(BS_R, BS_C);
+        const int depth = std::min(tune.a > 0 ? tune.a : a.gated ? 1 : 2, a.epilogue || a.gated ? 2 : kMostDepth);
         if (tune.mt == 1) {
             if (depth == 1) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
             if (depth == 2) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});
-            if (depth == 3) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 3>{});
-            return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+            if constexpr (kMostDepth >= 4)
+                if (depth == 4) return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+            return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 3>{});
         }
         // two tiles along m: at most two blocks in flight -- a third does not fit the register file for
         // the largest fp32 blocks, and the loads are written in assembly, so a spilled register that a
@@ -432,6 +443,8 @@ bsr_status launch_tile_shape(const spmm_args& a, const tune_opts& tune)
 }
 
 }  // namespace
+
+int mfma_tile_most_depth(const bsr_matrix* W) { return W->dtype == BSR_F32 ? most_depth<float>(W->bs_r, W->bs_c) : most_depth<_Float16>(W->bs_r, W->bs_c); }
 
 bsr_status launch_mfma_tile(const spmm_args& a, const tune_opts& t)
 {
