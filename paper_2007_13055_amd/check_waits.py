@@ -26,14 +26,30 @@ _OTHERS = ("global_store", "flat_store", "buffer_store", "scratch_store", "globa
 _MOST, _LANDED = 64, 1 << 20                # operations since a register's load, counted so far (a wait's N is below it); none in flight
 
 
-def listing(obj: str) -> str:
-    """The AMD code of an object file that hipcc made."""
+def _printed(obj: str, *tool) -> str:
+    """What one of LLVM's tools prints of the AMD code in an object file that hipcc made."""
     with tempfile.TemporaryDirectory() as tmp:
         bundle, code = os.path.join(tmp, "bundle"), os.path.join(tmp, "code")
         run = lambda *cmd: subprocess.run([os.path.join(LLVM, cmd[0]), *cmd[1:]], check=True, capture_output=True, text=True).stdout  # noqa: E731
         run("llvm-objcopy", f"--dump-section=.hip_fatbin={bundle}", obj, os.devnull)
         run("clang-offload-bundler", "--type=o", "--unbundle", "--targets=hipv4-amdgcn-amd-amdhsa--gfx950", f"--input={bundle}", f"--output={code}")
-        return run("llvm-objdump", "-d", code)
+        return run(*tool, code)
+
+
+def listing(obj: str) -> str:
+    return _printed(obj, "llvm-objdump", "-d")
+
+
+def accumulation_registers(obj: str) -> dict:
+    """{kernel: accumulation registers that it takes}"""
+    out, count = {}, 0
+    for line in _printed(obj, "llvm-readelf", "--notes").splitlines():
+        key, _, value = line.strip().removeprefix("- ").partition(":")
+        if key == ".agpr_count":
+            count = int(value)
+        elif key == ".name" and "  - " not in line and value.strip().startswith("_Z"):
+            out[value.strip()] = count
+    return out
 
 
 def kernels(text: str):

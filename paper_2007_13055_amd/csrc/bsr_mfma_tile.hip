@@ -108,22 +108,23 @@ __global__ __launch_bounds__(256, E::gated ? gated_waves<T>(BS_R, BS_C) : 1) voi
 
     typedef f32x16 acc_t;
     acc_t acc[NA][MT], first[E::gated ? NA : 1][E::gated ? MT : 1];   // first: the gate's sums, once they are done
-    auto clear = [&]() {
+    // (zeroed in place here and below: by a function that both call, kernels that call it once keep the zeros in registers of their own)
 #pragma unroll
-        for (int u = 0; u < NA; ++u)
+    for (int u = 0; u < NA; ++u)
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[u][t][e] = 0.f;
-    };
-    clear();
+            for (int e = 0; e < 16; ++e) acc[u][t][e] = 0.f;
     auto next_half = [&]() {
         if constexpr (E::gated) {
 #pragma unroll
             for (int u = 0; u < NA; ++u)
 #pragma unroll
-                for (int t = 0; t < MT; ++t) first[u][t] = acc[u][t];
-            clear();
+                for (int t = 0; t < MT; ++t) {
+                    first[u][t] = acc[u][t];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[u][t][e] = 0.f;
+                }
         }
     };
     if (E::gated) next_half();
