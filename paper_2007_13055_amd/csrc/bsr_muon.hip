@@ -124,6 +124,13 @@ __device__ __forceinline__ double shared_sum(double v, int lane_xor)
     return v + __builtin_bit_cast(double, (unsigned long long)(unsigned)lo | ((unsigned long long)(unsigned)hi << 32));
 }
 
+__device__ __forceinline__ bool finite_sum(double sum) { return sum - sum == 0.0; }
+// held / (|V| + eps) from the sum of squares; NaN where V is not finite (an infinity's 0 would leave the block's other elements 0)
+__device__ __forceinline__ float inverse_norm(double sum, float eps, float held)
+{
+    return finite_sum(sum) ? (float)((double)held / (sqrt(sum) + (double)eps)) : __builtin_nanf("");
+}
+
 // fp32 products on the 16-bit matrix cores, which take a sixteenth of the time.  A lane's eight terms are those of two tiles, four each.
 // F16: x = hi + lo, two fp16 numbers, to 2^-23 of x's power of two, and of the four products of two such sums the three largest (the
 // fourth is below 2^-22 of hi hi); for numbers that are known to stay in fp16's range.  Else: x = hi + mid + lo, three bf16 numbers,
@@ -300,13 +307,13 @@ __global__ __launch_bounds__(64 * waves_of(RT, CT), 2) void bsr_muon_blocks(cons
                 store_run4<float, WHOLE>(d.momentum, mv, J, I, run_of);
             }
     }
-    // A block that is not finite takes no part in the steps of those beside it, whose zeros its numbers would meet; it ends as NaN.
+    // A block that is not finite ends as NaN (by |V|, so that it does with no steps, too).  It takes no part in the steps of those
+    // beside it, whose zeros its numbers would meet.
     uint32_t spoilt = 0;                              // bit e: column c0 + e is of such a block
     // |V|: squares and their sum in 64 bits, which hold those of any fp32 numbers
     {
         float over[4];                                // of the lane's four columns (MODE 2: they may be of four blocks)
-        auto inverse = [&](double sum) { return (float)((double)kHeld / (sqrt(sum) + (double)h.eps)); };
-        auto finite_sum = [&](double sum) { return sum - sum == 0.0; };
+        auto inverse = [&](double sum) { return inverse_norm(sum, h.eps, kHeld); };
         if constexpr (MODE == 2) {
             double* const sums = reinterpret_cast<double*>(area);
 #pragma unroll
@@ -634,7 +641,7 @@ __global__ __launch_bounds__(64 * std::max(RT, CT), 3) void bsr_muon_team(const 
         sum = 0.0;
 #pragma unroll
         for (int l = 0; l < L; ++l) sum += sums[l];
-        const float over = (float)((double)kHeld / (sqrt(sum) + (double)h.eps));
+        const float over = inverse_norm(sum, h.eps, kHeld);
 #pragma unroll
         for (int s = 0; s < S; ++s) w[s] *= over;
     }
