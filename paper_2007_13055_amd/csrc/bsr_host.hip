@@ -638,7 +638,7 @@ bsr_status check_product_args(const bsr_matrix* W, int64_t m, const void* X_dev,
     if (y_dtype != W->dtype && y_dtype != BSR_F32) return BSR_ERR_DTYPE;
     if (m == 0 || W->n == 0) return BSR_OK;
     if (!Y_dev || (W->k > 0 && !X_dev)) return BSR_ERR_NULL;
-    if (m * std::max<int64_t>(W->k, W->n) >= kInt32Limit) return BSR_ERR_SHAPE;
+    if (too_many_rows(W, m)) return BSR_ERR_SHAPE;
     if (!aligned16(X_dev) || !aligned16(Y_dev)) return BSR_ERR_ALIGN;
     return BSR_OK;
 }
@@ -782,7 +782,7 @@ static size_t gated_sums_bytes(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype
 static bsr_status check_gated_args(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype)
 {
     if (!W) return BSR_ERR_NULL;
-    if (m < 0 || W->R % 2 != 0 || m * std::max<int64_t>(W->k, W->n) >= kInt32Limit) return BSR_ERR_SHAPE;
+    if (m < 0 || W->R % 2 != 0 || too_many_rows(W, m)) return BSR_ERR_SHAPE;
     if (h_dtype != W->dtype && h_dtype != BSR_F32) return BSR_ERR_DTYPE;
     return BSR_OK;
 }

@@ -196,6 +196,13 @@ struct bsr_matrix {
     std::map<std::pair<int64_t, int>, tuned_choice> tuned;
 };
 
+// Whether the offsets of m rows of X or Y leave 32 bits (m of any size: its product with a row may leave 64).
+inline bool too_many_rows(const bsr_matrix* W, int64_t m)
+{
+    const int64_t row = W->k > W->n ? W->k : W->n;
+    return row > 0 && m > (((int64_t)1 << 31) - 1) / row;
+}
+
 // Arguments every kernel launcher takes.
 struct spmm_args {
     const bsr_matrix* W;

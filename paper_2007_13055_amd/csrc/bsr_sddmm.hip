@@ -508,7 +508,7 @@ extern "C" bsr_status bsr_sddmm_ws(const bsr_matrix* W, int64_t m, const void* G
     if (d_dtype != W->dtype && d_dtype != BSR_F32) return BSR_ERR_DTYPE;
     if (W->nnzb == 0) return BSR_OK;
     if (!D_dev || (m > 0 && (!G_dev || !X_dev))) return BSR_ERR_NULL;
-    if (m * std::max<int64_t>(W->k, W->n) >= ((int64_t)1 << 31)) return BSR_ERR_SHAPE;
+    if (too_many_rows(W, m)) return BSR_ERR_SHAPE;
     if (((uintptr_t)G_dev | (uintptr_t)X_dev | (uintptr_t)D_dev | (uintptr_t)workspace_dev) & 15u) return BSR_ERR_ALIGN;
     hipStream_t stream = (hipStream_t)hip_stream;
     order_after_upload(stream, W->plan_uploaded, W->plan_landed);
