@@ -753,11 +753,11 @@ static gated_kernel gated_choice(const bsr_matrix* W, int64_t m, bsr_dtype h_dty
     // 8-wide blocks: where whole 16x16 tiles hold them (or outputs would have to be summed again, bsr_mfma_sweep.hip); it reads X
     // once for all outputs and is quicker than the kernel of tiles and a pass behind it from 16 rows on in all of 40 products
     // (64 x (512, 2 x 768) bf16 8x8 5 %: 4.4 us, 6.3; 64 x (1024, 2 x 2048) fp32 8x8 20 % 8.1, 11.4), below that by estimates
-    const bool sweeps = mfma_small_supports(W) && mfma_sweep_supports(W) && (m >= 16 || sweep_gates_quicker(W, m, h_dtype));
+    const bool sweeps = mfma_small_supports(W) && sweep_gates(W) && (m >= 16 || sweep_gates_quicker(W, m, h_dtype));
     if (W->env_tune.from_env && W->env_tune.variant > 0) {
         const int v = W->env_tune.variant;
         return v == 2 && mfma_supports(W) ? gated_kernel::ksplit : v == 3 && mfma_supports(W) && W->bs_r >= 32 ? gated_kernel::tile
-             : v == 6 && mfma_sweep_supports(W) ? gated_kernel::sweep : v == 7 ? gated_kernel::wave : gated_kernel::sums;
+             : v == 6 && sweep_gates(W) ? gated_kernel::sweep : v == 7 ? gated_kernel::wave : gated_kernel::sums;
     }
     if (W->nnzb == 0 || (auto_path(W, m, h_dtype) == BSR_PATH_WAVE && !sweeps)) return gated_kernel::wave;
     if (mfma_supports(W)) {
@@ -770,12 +770,11 @@ static gated_kernel gated_choice(const bsr_matrix* W, int64_t m, bsr_dtype h_dty
     return sweeps ? gated_kernel::sweep : gated_kernel::sums;
 }
 
-// Bytes of the fp32 sums that a gated product leaves in its workspace: none where a kernel makes H by itself, whatever is
-// captured (the sweep kernel's plan may not be there then: 16x16 blocks have the k-split kernel).
-static size_t gated_sums_bytes(const bsr_matrix* W, int64_t m, bsr_dtype h_dtype)
+// Bytes of the fp32 sums that a gated product leaves in its workspace: none where kernel g makes H by itself, whatever is
+// captured (16x16 blocks have the k-split kernel while the sweep kernel's plan is not there; 8-wide ones need the sums until then).
+static size_t gated_sums_bytes(const bsr_matrix* W, int64_t m, gated_kernel g)
 {
-    const gated_kernel g = gated_choice(W, m, h_dtype);
-    if (g != gated_kernel::sums && (g != gated_kernel::sweep || W->sw_created || (mfma_supports(W) && mfma_ksplit_reaches(W)))) return 0;
+    if (g != gated_kernel::sums && (g != gated_kernel::sweep || (mfma_supports(W) && mfma_ksplit_reaches(W)) || sweep_landed(W))) return 0;
     return ((size_t)m * (size_t)W->n * sizeof(float) + 255) & ~(size_t)255;
 }
 
@@ -792,7 +791,7 @@ bsr_status bsr_spmm_gated_workspace_size(const bsr_matrix* W, int64_t m, bsr_dty
     if (!bytes) return BSR_ERR_NULL;
     *bytes = 0;
     const bsr_status st = check_gated_args(W, m, h_dtype);
-    if (st == BSR_OK) *bytes = gated_sums_bytes(W, m, h_dtype);
+    if (st == BSR_OK) *bytes = gated_sums_bytes(W, m, gated_choice(W, m, h_dtype));
     return st;
 }
 
@@ -809,7 +808,8 @@ bsr_status bsr_spmm_gated(const bsr_matrix* W, int64_t m, const void* X_dev, voi
     for (const void* p : {X_dev, (const void*)H_dev, e.bias_dev, (const void*)e.z_dev, (const void*)workspace_dev})
         if (!aligned16(p)) return BSR_ERR_ALIGN;
     const bool in_place = e.z_dev && h_dtype == BSR_F32;              // Z itself takes the fp32 sums
-    const size_t need = in_place ? 0 : gated_sums_bytes(W, m, h_dtype);
+    const gated_kernel choice = gated_choice(W, m, h_dtype);
+    const size_t need = in_place ? 0 : gated_sums_bytes(W, m, choice);
     if (need && (!workspace_dev || workspace_bytes < need)) return BSR_ERR_WORKSPACE;
     const size_t h_size = h_dtype == BSR_F32 ? 4 : 2, x_size = W->dtype == BSR_F32 ? 4 : 2, sums = (size_t)m * (size_t)W->n;
     const byte_range x{X_dev, (size_t)m * (size_t)W->k * x_size}, bias{e.bias_dev, (size_t)W->n * (e.bias_dtype == BSR_F32 ? 4 : 2)};
@@ -820,7 +820,6 @@ bsr_status bsr_spmm_gated(const bsr_matrix* W, int64_t m, const void* X_dev, voi
     int dev = -1;
     if (hipGetDevice(&dev) != hipSuccess || dev != W->device) return BSR_ERR_DEVICE;
     hipStream_t stream = (hipStream_t)hip_stream;
-    const gated_kernel choice = gated_choice(W, m, h_dtype);
     if (choice != gated_kernel::sums) {
         order_after_upload(stream, W->plan_uploaded, W->plan_landed);
         if (W->debug && (st = debug_check_device_arrays(W, stream)) != BSR_OK) return st;
@@ -834,6 +833,7 @@ bsr_status bsr_spmm_gated(const bsr_matrix* W, int64_t m, const void* X_dev, voi
             if (st != BSR_ERR_UNSUPPORTED) return st;
             // its plan is not there (a capture behind bsr_create, or no host memory): nothing was launched
             if (mfma_supports(W) && mfma_ksplit_reaches(W)) return launch_mfma_ksplit(a, t);
+            if (!need && !in_place) return st;        // (its plan was there: no sums have a place)
         } else {
             if (choice == gated_kernel::tile) t.mt = 1;
             return choice == gated_kernel::tile ? launch_mfma_tile(a, t) : launch_mfma_ksplit(a, t);

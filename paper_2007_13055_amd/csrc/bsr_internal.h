@@ -315,6 +315,8 @@ void build_sweep_plan(const bsr_matrix* W, const int32_t* index_pointer_host, co
 // Whether the plan is there for what `stream` is given next: builds it and queues its upload if need be.  A stream that is
 // being captured takes it only once it has landed (what is recorded cannot wait for it).
 bool sweep_ready(const bsr_matrix* W, hipStream_t stream);
+bool sweep_landed(const bsr_matrix* W);             // from then on sweep_ready() is true, captures included
+bool sweep_gates(const bsr_matrix* W);              // whether its gated form takes W
 int32_t sweep_windows(const bsr_matrix* W);
 size_t sweep_plan_words(int64_t n, int64_t k, int32_t bs_r, int32_t bs_c, int64_t nnzb);
 size_t mfma_thin_scratch_bytes(const bsr_matrix* W, int64_t m);   // bytes of the transposed copy of X

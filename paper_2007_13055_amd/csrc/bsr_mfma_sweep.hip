@@ -428,6 +428,7 @@ bsr_status launch_types(const spmm_args& a, const tune_opts& tune)
 }  // namespace
 
 bool mfma_sweep_supports(const bsr_matrix* W) { return W->sw_base != nullptr; }
+bool sweep_gates(const bsr_matrix* W) { return mfma_sweep_supports(W) && (W->bs_r != 8 || mfma_small_supports(W)); }
 
 // Rounds of all quads and of the longest, without the plan (a window has as many as the longest of a quad's groups has
 // entries), and the 16x16 tiles of W that hold a block, of all tile-rows and of the longest.  May throw.
@@ -740,4 +741,11 @@ bool sweep_ready(const bsr_matrix* W, hipStream_t stream)
     p.sent = p.host.size() <= W->sw_words && upload_words(W->sw_base, p.host, stream, p.uploaded, p.landed);
     if (!p.sent) (void)hipGetLastError();             // nothing was launched, and another kernel will be
     return p.sent;
+}
+
+bool sweep_landed(const bsr_matrix* W)
+{
+    if (W->sw_created || W->sw.landed.load(std::memory_order_acquire)) return true;
+    std::lock_guard<std::mutex> lock(W->sw_mu);
+    return W->sw.sent && upload_landed(W->sw.uploaded, W->sw.landed);
 }
