@@ -56,6 +56,25 @@ size_t plan_bytes(int64_t R, int64_t nnzb, int32_t bs_r, int32_t bs_c, int64_t k
     return (b + 255) & ~(size_t)255;
 }
 
+// 0 .. n - 1 by count(i), most first, equal ones as they come.  Counted into place: with a comparison sort of the pairs a bsr_create of
+// 8192 block-rows of 16 takes 642 us in place of 516, of 4096 block-rows of 32 220 in place of 136.  (Unless some count is far beyond n:
+// a few rows of many blocks.)
+template <typename F> std::vector<int32_t> most_first(int32_t n, F count)
+{
+    std::vector<int32_t> order((size_t)n);
+    int32_t most = 0;
+    for (int32_t i = 0; i < n; ++i) most = std::max(most, count(i));
+    if (most > 4096 && most / 4 > n) {
+        std::iota(order.begin(), order.end(), 0);
+        std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return count(a) > count(b); });
+        return order;
+    }
+    std::vector<int32_t> place((size_t)most + 2, 0);
+    for (int32_t i = 0; i < n; ++i) ++place[(size_t)(most - count(i)) + 1];
+    for (size_t c = 1; c < place.size(); ++c) place[c] += place[c - 1];
+    for (int32_t i = 0; i < n; ++i) order[(size_t)place[(size_t)(most - count(i))]++] = i;
+    return order;
+}
 
 }  // namespace
 
@@ -473,10 +492,7 @@ static bsr_status create(bsr_matrix** out, int64_t n, int64_t k, int32_t bs_r, i
     if (R % 2 == 0 && mfma_supports(W)) {             // gated products: pairs of block-rows, most stored blocks first
         const size_t at = words;
         W->staging.resize(at + 2 * (size_t)R + 64, 0);
-        std::vector<int32_t> order((size_t)R / 2);
-        std::iota(order.begin(), order.end(), 0);
-        auto blocks = [&](int32_t q) { return index_pointer_host[2 * q + 2] - index_pointer_host[2 * q]; };
-        std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return blocks(a) > blocks(b); });
+        const std::vector<int32_t> order = most_first((int32_t)(R / 2), [&](int32_t q) { return index_pointer_host[2 * q + 2] - index_pointer_host[2 * q]; });
         for (size_t i = 0; i < order.size(); ++i)
             for (int e = 0; e < 4; ++e) W->staging[at + 4 * i + (size_t)e] = e == 0 ? order[i] : index_pointer_host[2 * order[i] + e - 1];
         W->gate_pairs = W->row_order + at;
