@@ -128,7 +128,7 @@ __device__ __forceinline__ bool finite_sum(double sum) { return sum - sum == 0.0
 // held / (|V| + eps) from the sum of squares; NaN where V is not finite (an infinity's 0 would leave the block's other elements 0)
 __device__ __forceinline__ float inverse_norm(double sum, float eps, float held)
 {
-    return finite_sum(sum) ? (float)((double)held / (sqrt(sum) + (double)eps)) : __builtin_nanf("");
+    return (float)((double)held / (sqrt(sum + (sum - sum)) + (double)eps));
 }
 
 // fp32 products on the 16-bit matrix cores, which take a sixteenth of the time.  A lane's eight terms are those of two tiles, four each.
