@@ -10,10 +10,12 @@
 //                c = r mean(Gw x); without the mean of Gw for the root mean square
 //     sums over the rows: of GU x r and GU (pre's weight and bias), alpha g post(B) (gate), t x r and t (post's)
 //
-// Work split: T lanes share a row, eight neighbouring columns a lane (T = 8 to 64: several rows a wavefront; 128 to 1024: a
-// workgroup a row), so a row is read once and stays in registers through its norms.  A workgroup walks over rows, with the
-// next row's reads under way while one is summed, and keeps the five vectors' parts -- and in the backward pass the five sums
-// -- of its columns in registers.  Its sums are written once, and a second launch adds the workgroups' in a fixed order (no
+// Work split: T lanes share a row, eight neighbouring columns a lane (T = 8 to 64: several rows a wavefront; 128 to 512: a
+// workgroup a row), two or four runs of eight where a row has more than 4096, so a row is read once and stays in registers through
+// its norms.  A workgroup walks over rows and keeps the five vectors' parts -- and in the backward pass the five sums -- of its
+// columns in registers, with the next row's reads under way while one is summed.  Not so in rows of more than 4096 columns, whose
+// registers hold one row alone: the forward pass reads the vectors again in every row (7400 x 9683 f16 with all five in fp32: 294 us,
+// a copy's time is 110), and the backward pass keeps up to 190 of its registers in memory.  Its sums are written once, and a second launch adds the workgroups' in a fixed order (no
 // atomics: the same bits every time).  In the backward pass the sums of more than 8192 columns do not fit a workgroup's registers:
 // one launch makes the rows' means and a second, eight columns a lane, the gradients from them.
 #include <algorithm>
@@ -199,37 +201,42 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void bsr_norm_rows(const ST* S, 
 // What the gradients of a row's columns are made of.
 struct row_stats { float mean, r, c, shift; };        // of the input; r and c as above; shift: mean of Gw (layer norm)
 
-// A product that is rounded wherever it is taken, so that what a mean subtracts is what the mean was made of: a row of one column
-// has a layer norm's gradient of exactly 0, rows of a few lose no more than the formulas do.
-__device__ __forceinline__ float rounded_product(float a, float b)
+// A product; PIN: rounded wherever it is taken, so that what a mean subtracts is what the mean was made of: a row of one column
+// has a layer norm's gradient of exactly 0, rows of a few lose no more than the formulas do.  (Not in rows of more than 4096 columns,
+// whose sums have no such cancellation and whose registers are short: pinned products wait there, in memory, from one use to the next.
+// 12598 x 6886 bf16, fp32 weights 564 us pinned, 429 not; 4096 x 8192 fp32 335, 232; 4096 x 12288 bf16 445, 359.)
+template <bool PIN> __device__ __forceinline__ float rounded_product(float a, float b)
 {
     float p = a * b;
-    asm("" : "+v"(p));
+    if constexpr (PIN) asm("" : "+v"(p));
     return p;
 }
 // The gradient of S' in one column, from gw = GU weight.
-__device__ __forceinline__ float sum_gradient(const norm_args& a, const row_stats& pre, float x, float gw, float gs)
+template <bool PIN> __device__ __forceinline__ float sum_gradient(const norm_args& a, const row_stats& pre, float x, float gw, float gs)
 {
-    return a.pre == BSR_NORM_NONE ? gs : fmaf(pre.r, fmaf(-rounded_product(x - pre.mean, pre.r), pre.c, gw - pre.shift), gs);
+    if (a.pre == BSR_NORM_NONE) return gs;
+    if constexpr (PIN) return fmaf(pre.r, fmaf(-rounded_product<PIN>(x - pre.mean, pre.r), pre.c, gw - pre.shift), gs);
+    return fmaf(pre.r, fmaf(-(x - pre.mean), pre.r * pre.c, gw - pre.shift), gs);
 }
 
 // One column's part: from x, GU, GS, b to g, dS, dB and what the five sums get.
 struct column_parts { float ds, db, sum[kSums]; };
+template <bool PIN>
 __device__ __forceinline__ column_parts column_gradient(const norm_args& a, const row_stats& pre, const row_stats& post, float x, float gu, float gs,
                                                         float b, float wp, float bp, float gate, float wq)
 {
     column_parts out;
     const float xm = x - pre.mean;
-    const float g = sum_gradient(a, pre, x, rounded_product(gu, wq), gs);
+    const float g = sum_gradient<PIN>(a, pre, x, rounded_product<PIN>(gu, wq), gs);
     out.sum[3] = gu * (xm * pre.r);
     out.sum[4] = gu;
     out.ds = a.beta * g;
-    const float bh = rounded_product(b - post.mean, post.r), ag = rounded_product(a.alpha, g);
+    const float bh = rounded_product<PIN>(b - post.mean, post.r), ag = rounded_product<PIN>(a.alpha, g);
     out.sum[2] = ag * fmaf(bh, wp, bp);
-    const float t = rounded_product(ag, gate);
+    const float t = rounded_product<PIN>(ag, gate);
     out.sum[0] = t * bh;
     out.sum[1] = t;
-    out.db = a.post == BSR_NORM_NONE ? t : post.r * fmaf(-bh, post.c, rounded_product(t, wp) - post.shift);
+    out.db = a.post == BSR_NORM_NONE ? t : post.r * fmaf(-bh, post.c, rounded_product<PIN>(t, wp) - post.shift);
     return out;
 }
 
@@ -243,7 +250,7 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void bsr_norm_grad_rows(const ST
     constexpr int BLOCK = T <= 64 ? 256 : T, TEAMS = BLOCK / T;
     __shared__ float slots[T > 64 ? 2 * (T / 64) * kMostAtOnce : 1];
     __shared__ float red[TEAMS > 1 ? BLOCK * V : 1];
-    constexpr bool kAll = K < 4;
+    constexpr bool kAll = K < 4, PIN = K == 1;
     int phase = 0;
     const int t = (int)threadIdx.x % T, team = (int)threadIdx.x / T;
     int col[K], count[K];
@@ -313,7 +320,7 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void bsr_norm_grad_rows(const ST
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             each([&](int j, int e) {
                 const bool there = e < count[j];
-                const float xm = there ? x[j][e] - pre.mean : 0.f, bm = there ? b[j][e] - post.mean : 0.f, gw = rounded_product(gu[j][e], wq[j][e]);
+                const float xm = there ? x[j][e] - pre.mean : 0.f, bm = there ? b[j][e] - post.mean : 0.f, gw = rounded_product<PIN>(gu[j][e], wq[j][e]);
                 v[0] = fmaf(xm, xm, v[0]);
                 v[1] = fmaf(gw, xm, v[1]);
                 v[2] += gw;
@@ -332,8 +339,8 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void bsr_norm_grad_rows(const ST
             each([&](int j, int e) {
                 const bool there = e < count[j];
                 const float bm = there ? b[j][e] - post.mean : 0.f;
-                const float g = sum_gradient(a, pre, x[j][e], rounded_product(gu[j][e], wq[j][e]), gs[j][e]);
-                const float gw = there ? rounded_product(rounded_product(rounded_product(a.alpha, g), gate[j][e]), wp[j][e]) : 0.f;
+                const float g = sum_gradient<PIN>(a, pre, x[j][e], rounded_product<PIN>(gu[j][e], wq[j][e]), gs[j][e]);
+                const float gw = there ? rounded_product<PIN>(rounded_product<PIN>(rounded_product<PIN>(a.alpha, g), gate[j][e]), wp[j][e]) : 0.f;
                 v[0] = fmaf(gw, bm, v[0]);
                 v[1] += gw;
             });
@@ -357,7 +364,7 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void bsr_norm_grad_rows(const ST
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const column_parts p =
-                        column_gradient(a, pre, post, x[j][e], gu[j][e], gs[j][e], b[j][e], wp[j][e], bp[j][e], gate[j][e], wq[j][e]);
+                        column_gradient<PIN>(a, pre, post, x[j][e], gu[j][e], gs[j][e], b[j][e], wp[j][e], bp[j][e], gate[j][e], wq[j][e]);
                     ds.set(e, p.ds);
                     db.set(e, p.db);
 #pragma unroll
@@ -427,7 +434,7 @@ __global__ __launch_bounds__(256) void bsr_norm_grad_cols(const ST* S, const XT*
         gu.load(GU + at, GU ? count : 0);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const column_parts p = column_gradient(a, pre, post, x[e], gu[e], gs[e], b[e], wp[e], bp[e], gate[e], wq[e]);
+            const column_parts p = column_gradient<false>(a, pre, post, x[e], gu[e], gs[e], b[e], wp[e], bp[e], gate[e], wq[e]);
             ds.set(e, p.ds);
             db.set(e, p.db);
 #pragma unroll
