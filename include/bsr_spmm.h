@@ -453,10 +453,12 @@ void bsr_adamw_destroy(bsr_adamw* opt);
  *   H_dev          DEVICE, m*n elements of h_dtype (W's dtype or BSR_F32), every one written
  *   gated (HOST)   act; bias_dev: DEVICE, 2n elements of bias_dtype (W's dtype or BSR_F32), or NULL; z_dev: DEVICE, Z, m*2n
  *                  elements of h_dtype, every one written, or NULL
- *   workspace_dev  DEVICE, bsr_spmm_gated_workspace_size() bytes (0: none, it may be NULL), overwritten.  Calls that may run at
- *                  the same time, replayed graphs among them, need one each
- * Streams, captures and choices of kernel as bsr_spmm().  H, Z and the workspace must overlap neither one another nor an input,
- * nor the handle's arrays, its workspace and what has been lent as scratch.
+ *   workspace_dev  DEVICE, bsr_spmm_gated_workspace_size() bytes (0: none, it may be NULL; blocks with a side of 8 may need one
+ *                  until a product has run, and none from then on), overwritten.  Calls that may run at the same time, replayed
+ *                  graphs among them, need one each
+ * Streams and captures as bsr_spmm().  The kernel is the library's choice by W and m; what bsr_tune() remembered is for the other
+ * products, and for a gated one where it leaves its sums in the workspace or in Z.  H, Z and the workspace must overlap neither one
+ * another nor an input, nor the handle's arrays, its workspace and what has been lent as scratch.
  * Errors: as bsr_spmm_epilogue(), plus SHAPE (an odd number of block-rows) and WORKSPACE.
  */
 typedef struct {
@@ -549,8 +551,10 @@ bsr_status bsr_residual_norm_backward(int64_t m, int64_t n, bsr_dtype s_dtype, c
 
 /*
  * One step over the stored blocks of many matrices whose update is orthogonalised block by block: every singular value of a
- * block's update is brought near 1 by Newton-Schulz steps, products alone, whose errors are those of fp32 arithmetic (on the matrix
- * cores, of numbers in two fp16 parts where |a| >= 1 and a, b, c keep X's singular values below 3.9, in three bf16 parts or fp32 elsewhere).
+ * block's update is brought near 1 by Newton-Schulz steps, products alone, on the matrix cores with fp32 sums: of numbers in two
+ * fp16 parts, to 2^-23 of their powers of two, where |a| >= 1 and a, b, c keep X's singular values below 3.9; in three bf16 parts (24
+ * bits) or fp32 elsewhere.  With the parts of fp16 an update's root mean square error is 1.0 to 1.5 times that of the same steps in
+ * plain fp32 arithmetic, its largest up to 1.8 times.
  * With g the gradient times grad_scale,
  *     M = momentum M + g                 V = g + momentum M (nesterov) or M
  *     X = V / (|V| + eps), |V| the block's Frobenius norm;  ns_steps times  X = a X + b (X X^T) X + c (X X^T)^2 X

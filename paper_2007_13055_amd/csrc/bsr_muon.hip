@@ -15,8 +15,9 @@
 //
 // What bounds it (40 million elements, bf16 with a master copy, 805 MB; a large copy moves 5.2 bytes a ps): memory, beside it in
 // 16x16 blocks the vector units (splitting into parts), in the largest blocks registers, which leave two wavefronts a SIMD to cover its
-// latency.  With 0 and 5 steps, us: 16x16 147, 198; 32x32 158, 191; 64x32 165, 176 to 192; 64x64 215, 285.  (16x16 with products of fp32 numbers 235; 64x64, fp32 gradients and W^T's copy with it, 318, and
-// 456 with products of three bf16 parts.)
+// latency; 64x64 blocks are 30 short of them, which wait in memory (100 bytes a lane; 900 where bs_c is no multiple of 4).  With 0
+// and 5 steps, us: 16x16 147, 198; 32x32 158, 191; 64x32 165, 176 to 192; 64x64 215, 285.  (16x16 with products of fp32 numbers 235;
+// 64x64, fp32 gradients and W^T's copy with it, 312, and 456 with products of three bf16 parts.)
 #include <algorithm>
 #include <cmath>
 #include <memory>

@@ -14,10 +14,11 @@
 // workgroup a row), two or four runs of eight where a row has more than 4096, so a row is read once and stays in registers through
 // its norms.  A workgroup walks over rows and keeps the five vectors' parts -- and in the backward pass the five sums -- of its
 // columns in registers, with the next row's reads under way while one is summed.  Not so in rows of more than 4096 columns, whose
-// registers hold one row alone: the forward pass reads the vectors again in every row (7400 x 9683 f16 with all five in fp32: 294 us,
-// a copy's time is 110), and the backward pass keeps up to 190 of its registers in memory.  Its sums are written once, and a second launch adds the workgroups' in a fixed order (no
-// atomics: the same bits every time).  In the backward pass the sums of more than 8192 columns do not fit a workgroup's registers:
-// one launch makes the rows' means and a second, eight columns a lane, the gradients from them.
+// registers hold one row alone: the forward pass reads the vectors again in every row (7400 x 9683 f16 with all five: 293 us, a
+// copy's time is 110), and the backward pass keeps 1 to 190 of its registers in memory.  Its sums are written once, and a second
+// launch adds the workgroups' in a fixed order (no atomics: the same bits every time).  In the backward pass the sums of more than
+// 8192 columns do not fit a workgroup's registers: one launch makes the rows' means and a second, eight columns a lane, the
+// gradients from them.
 #include <algorithm>
 
 #include "bsr_rows.h"

@@ -20,12 +20,12 @@ def test_every_depth_has_the_same_sums(oracle_mod, monkeypatch, bs_r, bs_c):
     p = _problem(300, bs_r, bs_c)
     Yo, So = oracle_mod.bsr_spmm(p.X, p.block_data, p.block_indices, p.index_pointer, p.n)
     first = None
-    for depth in (1, 2, 3, 4, 9):
-        monkeypatch.setenv("BSR_SPMM_TUNE", f"variant=3,mt=1,a={depth}")
+    for tiles, depth in ((1, 1), (1, 2), (1, 3), (1, 4), (1, 9), (2, 1), (2, 2)):
+        monkeypatch.setenv("BSR_SPMM_TUNE", f"variant=3,mt={tiles},a={depth}")
         Y, _ = gpu_product(p, path=lib.PATH_MFMA)
-        check(Y, Yo, So, p.tau, f"depth {depth}")
+        check(Y, Yo, So, p.tau, f"{tiles} tiles, depth {depth}")
         first = Y if first is None else first
-        assert np.array_equal(Y, first), depth
+        assert np.array_equal(Y, first), (tiles, depth)
 
 
 def test_tuned_product_of_the_largest_blocks(oracle_mod):
